@@ -314,6 +314,148 @@ headkv_status headkv_timing_collect(headkv_t h, double* kernel_ms, int64_t* laun
 headkv_status headkv_export_retained(headkv_t h, int32_t layer, uint8_t* mask,
                                      int32_t* count, void* stream);
 
+/* ---- Paged caches of 16, 8 or 4 bits, attention over them with shared
+ * prefixes, and the scores of sampled tokens.
+ *
+ * For sequences that share a prompt (many images of one prompt, guidance
+ * pairs), whose own tokens are held in fewer bits.  These calls need no handle;
+ * the conventions above hold, and every call is asynchronous on its stream.
+ *
+ * A cache is a pool of pages; a page holds page_tokens tokens of one key/value
+ * head.  A list is a sequence of pages of one (list number, kv head): a batch
+ * row's own tokens, or a prefix that several rows share.  Every list has its own
+ * length, so heads may keep different numbers of tokens.  A page number outside
+ * [0, num_pages), -1 by custom, is a page that has been dropped: its tokens are
+ * neither stored, read nor attended, the others keep their places.
+ *
+ * What a page holds for a token's key and value rows (d values each, x):
+ *   HEADKV_KV_BF16  x as it is.
+ *   HEADKV_KV_INT8  n in [-127, 127] and one scale s per row: s = max|x| / 127
+ *                   rounded to bf16, n = x / s rounded to the nearest, ties to
+ *                   even; the row stands for n s.  s = 0 gives n = 0.
+ *   HEADKV_KV_FP4   per 32 values a power of two s = 2^e, the smallest e >= -126
+ *                   with max|x| <= 6 s, and n = x / s rounded to the nearest of
+ *                   0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, ties to the
+ *                   one whose last bit is 0; they stand for n s.
+ * A row (FP4: 32 values) with an infinity or a NaN reads back as NaN. */
+
+#define HEADKV_KV_BF16 0
+#define HEADKV_KV_INT8 1
+#define HEADKV_KV_FP4 2
+
+#define HEADKV_MAX_GROUP 16 /* query heads of one key/value head */
+#define HEADKV_MAX_TOP 32   /* alternatives of headkv_token_logprobs */
+
+typedef struct headkv_paged_config {
+    int32_t kv_type;     /* HEADKV_KV_* */
+    int32_t head_dim;    /* d: 64 or 128 */
+    int32_t kv_heads;    /* key/value heads, 1..1024 */
+    int32_t group;       /* query heads of each, 1..HEADKV_MAX_GROUP; query
+                            head kv_head * group + g reads kv_head */
+    int32_t page_tokens; /* 32, 64, 128 or 256 */
+    int32_t num_pages;   /* pages of the pool, >= 1 */
+} headkv_paged_config;
+
+typedef struct headkv_paged_lists {
+    const int32_t* pages; /* [lists][kv_heads][max_pages], device */
+    const int32_t* len;   /* [lists][kv_heads] tokens of each list, device, or
+                             NULL: none */
+    const int32_t* first; /* [lists][kv_heads], device, or NULL: tokens before it
+                             are not attended (a sliding window) */
+    int32_t lists;        /* >= 1 */
+    int32_t max_pages;    /* pages of a table row, >= 1 */
+    int32_t extra;        /* >= 0, added to every len: a decoder that appends one
+                             token per step counts on the host */
+    int32_t max_len;      /* >= 0, no list has more tokens than this (len +
+                             extra); tokens past it are not read or attended */
+} headkv_paged_lists;
+
+/* Bytes of a page and of the pool (device, 256-byte aligned, the caller's). */
+headkv_status headkv_paged_plan(const headkv_paged_config* cfg, size_t* page_bytes,
+                                size_t* pool_bytes);
+
+/* Appends tokens: token i of list l becomes token len + extra + i of the list's
+ * heads, i < tokens and, with counts ([lists] int32, device, else NULL), i <
+ * counts[l].  k, v: bf16, device, 16-byte aligned; the row of (list l, token i,
+ * head h) starts list_stride l + token_stride i + head_stride h elements on,
+ * strides >= 0 and multiples of 8.  Tokens past the table and on dropped pages
+ * are not stored.  No length changes: the next calls pass a larger extra, or
+ * other lengths.  Lists must not share a page that this call writes. */
+headkv_status headkv_paged_write(const headkv_paged_config* cfg, void* pool,
+                                 const headkv_paged_lists* lists, const uint16_t* k,
+                                 const uint16_t* v, int64_t list_stride, int64_t token_stride,
+                                 int64_t head_stride, int32_t tokens, const int32_t* counts,
+                                 void* stream);
+
+/* Reads back, rounded to bf16 (FP4 and BF16 values are bf16 numbers): row (l, i,
+ * h) of k and v, laid out as for headkv_paged_write, receives token begin + i,
+ * or with begin < 0 token len + extra + begin + i, of list (l, h); zeros where
+ * the list has no such token. */
+headkv_status headkv_paged_read(const headkv_paged_config* cfg, const void* pool,
+                                const headkv_paged_lists* lists, int32_t begin, int32_t tokens,
+                                uint16_t* k, uint16_t* v, int64_t list_stride,
+                                int64_t token_stride, int64_t head_stride, void* stream);
+
+/* Bytes of the workspace of headkv_paged_attn for `own` and `shared` (NULL:
+ * none) with lengths up to their max_len (the pointers in them are not used);
+ * it does not shrink as a max_len grows. */
+headkv_status headkv_paged_attn_plan(const headkv_paged_config* cfg,
+                                     const headkv_paged_lists* own,
+                                     const headkv_paged_lists* shared, size_t* workspace_bytes);
+
+/* Attention of one query per batch row and query head, Eq. (1): o = softmax(q
+ * K^T / sqrt(d)) V over the tokens [first, len + extra) of the row's own list
+ * (batch = own->lists) and, if share[b] (int32, device) is the number of a list
+ * of `shared`, those of that list, whose keys and values are read once for all
+ * the rows that share it.  shared and share are both NULL or both given; a
+ * share[b] outside [0, shared->lists) shares nothing.
+ * q: bf16, device, 16-byte aligned, row b at q + b q_stride (a multiple of 8, >=
+ * 0), there [kv_heads * group][d].  out: [batch][kv_heads * group][d] fp32,
+ * 16-byte aligned.  lse: [batch][kv_heads * group] fp32 natural log of the sum
+ * of exponentials, or NULL.  A query with nothing to attend gets out = 0 and
+ * lse = -infinity.  fp32 sums, and weights of 24 bits.
+ * workspace: device, 256-byte aligned, headkv_paged_attn_plan bytes, zeroed by
+ * the caller before its first use (every launch leaves its counters zero);
+ * calls that overlap need one each. */
+headkv_status headkv_paged_attn(const headkv_paged_config* cfg, const void* pool,
+                                const headkv_paged_lists* own, const headkv_paged_lists* shared,
+                                const int32_t* share, const uint16_t* q, int64_t q_stride,
+                                float* out, float* lse, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* Types of logits. */
+#define HEADKV_LOGITS_BF16 0
+#define HEADKV_LOGITS_F32 1
+
+/* Bytes of the workspace of headkv_token_logprobs; it grows with each argument. */
+headkv_status headkv_logprobs_plan(int32_t rows, int32_t vocab, int32_t top,
+                                   size_t* workspace_bytes);
+
+/* Scores of given tokens under softmax(x / temperature), for each row x of
+ * `logits` ([rows] rows of `vocab` values, row_stride elements apart, >= vocab;
+ * device, aligned to their type):
+ *   logprob[r]     log p of tokens[r] (int32, device); -inf for a token outside
+ *                  [0, vocab)
+ *   entropy[r]     -sum p log p in nats
+ *   rank[r]        number of logits greater than the token's, -1 for a token
+ *                  outside [0, vocab)
+ *   top_logprob, top_index [r][top]: the `top` (0..HEADKV_MAX_TOP, at most
+ *                  vocab) largest log p, largest first, and their tokens, among
+ *                  equal ones the lowest first
+ * (fp32 and int32, device; entropy and rank may be NULL, the last two are NULL if
+ * top is 0).  Logits of -inf have p = 0; in a row that has no other, log p is
+ * -inf and the entropy 0.  A row with a NaN or +inf gets NaN in every fp32 and
+ * -1 in every int32 result.  temperature > 0.  Sums in fp32.
+ * workspace: device, 256-byte aligned, headkv_logprobs_plan bytes, zeroed by the
+ * caller before its first use (every launch leaves its counters zero); calls
+ * that overlap need one each. */
+headkv_status headkv_token_logprobs(const void* logits, int32_t logits_type, int32_t rows,
+                                    int32_t vocab, int64_t row_stride, const int32_t* tokens,
+                                    float temperature, int32_t top, float* logprob,
+                                    float* entropy, int32_t* rank, float* top_logprob,
+                                    int32_t* top_index, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* headkv_last_error(void);
 

@@ -44,6 +44,16 @@ HEADKV_ATTN_GROUPED = 2
 ATTN_STRATEGIES = {"varlen": HEADKV_ATTN_VARLEN, "padded": HEADKV_ATTN_PADDED,
                    "grouped": HEADKV_ATTN_GROUPED}
 
+HEADKV_KV_BF16 = 0
+HEADKV_KV_INT8 = 1
+HEADKV_KV_FP4 = 2
+KV_TYPES = {"bf16": HEADKV_KV_BF16, "int8": HEADKV_KV_INT8, "fp4": HEADKV_KV_FP4}
+HEADKV_MAX_GROUP = 16
+HEADKV_MAX_TOP = 32
+
+HEADKV_LOGITS_BF16 = 0
+HEADKV_LOGITS_F32 = 1
+
 EXPORTED = (
     "headkv_plan", "headkv_create", "headkv_destroy", "headkv_prefill", "headkv_prefill_attn",
     "headkv_append_and_evict", "headkv_score_heads", "headkv_assign_budgets",
@@ -51,6 +61,8 @@ EXPORTED = (
     "headkv_decode_step",
     "headkv_export_retained",
     "headkv_run_steps", "headkv_timing_reserve", "headkv_timing_collect",
+    "headkv_paged_plan", "headkv_paged_write", "headkv_paged_read", "headkv_paged_attn_plan",
+    "headkv_paged_attn", "headkv_logprobs_plan", "headkv_token_logprobs",
     "headkv_last_error",
 )
 
@@ -68,6 +80,22 @@ class HeadKVConfig(ctypes.Structure):
         ("attn_strategy", ctypes.c_int32), ("score_mode", ctypes.c_int32),
         ("cfg_pairs", ctypes.c_int32),
         ("tau", ctypes.c_double),
+    ]
+
+
+class PagedConfig(ctypes.Structure):
+    _fields_ = [
+        ("kv_type", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32), ("group", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+    ]
+
+
+class PagedListsArg(ctypes.Structure):
+    _fields_ = [
+        ("pages", ctypes.c_void_p), ("len", ctypes.c_void_p), ("first", ctypes.c_void_p),
+        ("lists", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("extra", ctypes.c_int32),
+        ("max_len", ctypes.c_int32),
     ]
 
 
@@ -236,3 +264,88 @@ def headkv_timing_collect(h: int):
     dr = ctypes.c_int64()
     _check(load().headkv_timing_collect(h, ms, n, b, ctypes.byref(dr)), "headkv_timing_collect")
     return [(ms[i], n[i], b[i]) for i in range(K)], dr.value
+
+
+# ---- paged caches and token scores -----------------------------------------
+_paged = None
+
+
+def load_paged() -> ctypes.CDLL:
+    """The library with the signatures of the paged and scoring calls, bound on
+    their first use."""
+    global _paged
+    L = load()
+    if _paged is L:
+        return L
+    P, I, Z, S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int64
+    cfg, lists, size = (ctypes.POINTER(t) for t in (PagedConfig, PagedListsArg, Z))
+    sig = {
+        "headkv_paged_plan": [cfg, size, size],
+        "headkv_paged_write": [cfg, P, lists, P, P, S, S, S, I, P, P],
+        "headkv_paged_read": [cfg, P, lists, I, I, P, P, S, S, S, P],
+        "headkv_paged_attn_plan": [cfg, lists, lists, size],
+        "headkv_paged_attn": [cfg, P, lists, lists, P, P, S, P, P, P, Z, P],
+        "headkv_logprobs_plan": [I, I, I, size],
+        "headkv_token_logprobs": [P, I, I, I, S, P, ctypes.c_float, I, P, P, P, P, P, P, Z, P],
+    }
+    for name, args in sig.items():
+        f = getattr(L, name)
+        f.argtypes = args
+        f.restype = ctypes.c_int32
+    _paged = L
+    return L
+
+
+def headkv_paged_plan(cfg: PagedConfig) -> Tuple[int, int]:
+    """(bytes of a page, bytes of the pool)."""
+    page, pool = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load_paged().headkv_paged_plan(cfg, page, pool), "headkv_paged_plan")
+    return page.value, pool.value
+
+
+def headkv_paged_write(cfg: PagedConfig, pool: int, lists: PagedListsArg, k: int, v: int,
+                       strides: Sequence[int], tokens: int, counts: Optional[int] = None,
+                       stream: int = 0) -> None:
+    """strides: elements between lists, tokens and heads of k and v."""
+    _check(load_paged().headkv_paged_write(cfg, pool, lists, k, v, *strides, tokens, counts,
+                                           stream), "headkv_paged_write")
+
+
+def headkv_paged_read(cfg: PagedConfig, pool: int, lists: PagedListsArg, begin: int, tokens: int,
+                      k: int, v: int, strides: Sequence[int], stream: int = 0) -> None:
+    _check(load_paged().headkv_paged_read(cfg, pool, lists, begin, tokens, k, v, *strides, stream),
+           "headkv_paged_read")
+
+
+def headkv_paged_attn_plan(cfg: PagedConfig, own: PagedListsArg,
+                           shared: Optional[PagedListsArg] = None) -> int:
+    size = ctypes.c_size_t()
+    _check(load_paged().headkv_paged_attn_plan(cfg, own, shared, size), "headkv_paged_attn_plan")
+    return size.value
+
+
+def headkv_paged_attn(cfg: PagedConfig, pool: int, own: PagedListsArg,
+                      shared: Optional[PagedListsArg], share: Optional[int], q: int,
+                      q_stride: int, out: int, lse: Optional[int], workspace: Optional[int],
+                      workspace_bytes: int, stream: int = 0) -> None:
+    _check(load_paged().headkv_paged_attn(cfg, pool, own, shared, share, q, q_stride, out, lse,
+                                          workspace, workspace_bytes, stream),
+           "headkv_paged_attn")
+
+
+def headkv_logprobs_plan(rows: int, vocab: int, top: int) -> int:
+    size = ctypes.c_size_t()
+    _check(load_paged().headkv_logprobs_plan(rows, vocab, top, size), "headkv_logprobs_plan")
+    return size.value
+
+
+def headkv_token_logprobs(logits: int, logits_type: int, rows: int, vocab: int, row_stride: int,
+                          tokens: int, temperature: float, top: int, logprob: int,
+                          entropy: Optional[int], rank: Optional[int],
+                          top_logprob: Optional[int], top_index: Optional[int],
+                          workspace: Optional[int], workspace_bytes: int,
+                          stream: int = 0) -> None:
+    _check(load_paged().headkv_token_logprobs(
+        logits, logits_type, rows, vocab, row_stride, tokens, temperature, top, logprob, entropy,
+        rank, top_logprob, top_index, workspace, workspace_bytes, stream),
+        "headkv_token_logprobs")

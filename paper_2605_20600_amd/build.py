@@ -14,7 +14,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheadkv.so")
 PROBE = os.path.join(HERE, "stream_probe")
 SOURCES = ["cache_kernels.hip", "attn_kernels.hip", "prefill_attn.hip", "scratch.hip",
-           "headkv_abi.cpp"]
+           "paged_cache.hip", "paged_attn.hip", "token_logprobs.hip", "headkv_abi.cpp",
+           "paged_abi.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",

@@ -18,6 +18,7 @@
 #include <vector>
 
 #include "../../include/headkv.h"
+#include "abi_error.h"
 #include "layout.h"
 #include "scratch.h"
 
@@ -27,9 +28,17 @@ namespace {
 
 thread_local std::string g_err;
 
-headkv_status fail(headkv_status code, const std::string& msg) {
+}  // namespace
+
+headkv_status headkv::set_error(headkv_status code, const std::string& msg) {
     g_err = msg;
     return code;
+}
+
+namespace {
+
+headkv_status fail(headkv_status code, const std::string& msg) {
+    return headkv::set_error(code, msg);
 }
 
 headkv_status ok() { return HEADKV_OK; }

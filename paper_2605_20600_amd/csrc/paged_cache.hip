@@ -1,0 +1,396 @@
+// Writing keys and values into a paged cache, quantised on the way, and reading
+// them back (formats and layout: headkv.h, paged.h).
+//
+// A task is the up to eight tokens of one aligned block of eight (one row of V
+// cells) of one list and head, taken by d / 2 lanes.  For K a lane holds 16 dims
+// of one token and stores them contiguously; for V it holds two dims of the
+// eight tokens, which are its two cells (FP4: its cell), so that a full block's
+// cells leave as whole 16-byte pieces without any exchange between lanes.  The
+// largest value of a row (FP4: of 32 dims) is found with lane exchanges, for V
+// on two tokens' bits at a time.  Both kernels are bound by their bytes.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "paged.h"
+#include "paged_device.h"
+
+namespace headkv {
+namespace {
+
+using namespace dev;
+
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a),
+                                                        __builtin_bit_cast(u16x2_t, b)));
+}
+
+// Maximum of each half over groups of LANES adjacent lanes.
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    if (LANES > 1) v = pk_max(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false));
+    if (LANES > 2) v = pk_max(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false));
+    if (LANES > 4) v = pk_max(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false));
+    if (LANES > 8) v = pk_max(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false));
+    if (LANES > 16) v = pk_max(v, (uint32_t)__shfl_xor((int)v, 16));
+    if (LANES > 32) v = pk_max(v, (uint32_t)__shfl_xor((int)v, 32));
+    return v;
+}
+
+// The eight-token block of a task: its list and head, first position and page.
+template <int D>
+struct Task {
+    static constexpr int LANES = D / 2;
+    int lane;        // of the task
+    int l, h;
+    int64_t lh;
+    bool any;        // a task at all
+    __device__ Task(int lists, int heads, int blocks, int* blk) {
+        const int64_t i = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+        lane = threadIdx.x % LANES;
+        any = i < (int64_t)lists * heads * blocks;
+        h = (int)(i % heads);  // heads of a token are neighbours in memory
+        *blk = (int)(i / heads % blocks);
+        l = (int)(i / heads / blocks);
+        lh = (int64_t)l * heads + h;
+    }
+};
+
+template <int TYPE, int D>
+__global__ __launch_bounds__(kThreads) void k_paged_write(PagedDims c, char* pool, PagedLists ls,
+                                                          const uint16_t* __restrict__ k,
+                                                          const uint16_t* __restrict__ v,
+                                                          PagedRows r, int tokens, int blocks,
+                                                          const int32_t* __restrict__ counts) {
+    int blk;
+    const Task<D> task(ls.lists, c.heads, blocks, &blk);
+    if (!task.any) return;
+    const int64_t base = (int64_t)(ls.len ? max(ls.len[task.lh], 0) : 0) + ls.extra;
+    const int64_t end = base + (counts ? min(max(counts[task.l], 0), tokens) : tokens);
+    const int64_t p0 = ((base >> 3) + blk) * 8;
+    if (p0 >= end) return;
+    char* page = const_cast<char*>(list_page(c, ls, pool, task.lh, p0));
+    if (!page) return;
+    const int tp = (int)(p0 & (c.ptok - 1)), lane = task.lane;
+    const int64_t row0 = task.l * r.list + task.h * r.head + (p0 - base) * r.token;
+
+    {  // K: 16 dims of one token
+        const int t = lane / (D / 16), piece = lane % (D / 16);
+        const bool there = p0 + t >= base && p0 + t < end;
+        uint32_t w[8] = {};
+        if (there) {
+            const uint4* src = reinterpret_cast<const uint4*>(k + row0 + t * r.token + piece * 16);
+            const uint4 a = src[0], b = src[1];
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+            w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+        }
+        if constexpr (TYPE == kBf16) {
+            if (there) {
+                uint4* dst = reinterpret_cast<uint4*>(page + (tp + t) * (2 * D) + piece * 32);
+                dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+        } else {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = pk_max(m, w[i] & 0x7fff7fffu);
+            m = lanes_max<TYPE == kInt8 ? D / 16 : 2>(m);
+            const uint32_t top = max(m & 0xffffu, m >> 16);
+            if constexpr (TYPE == kInt8) {
+                const uint16_t s = int8_scale(top);
+                uint32_t o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    o[i] = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t x = w[2 * i + e / 2] >> (16 * (e & 1)) & 0xffffu;
+                        o[i] |= (uint32_t)(int8_code(x, s) & 0xff) << (8 * e);
+                    }
+                }
+                if (there) {
+                    *reinterpret_cast<uint4*>(page + (tp + t) * D + piece * 16) =
+                        make_uint4(o[0], o[1], o[2], o[3]);
+                    if (piece == 0) reinterpret_cast<uint16_t*>(page + c.ks_off)[tp + t] = s;
+                }
+            } else {
+                const uint32_t e = fp4_scale(top);
+                const float s = fp4_power(e);
+                uint32_t o[2] = {};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t* p = w + 4 * i;
+                    auto lo = [](uint32_t u) { return __uint_as_float(u << 16); };
+                    auto hi = [](uint32_t u) { return __uint_as_float(u & 0xffff0000u); };
+                    o[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o[i], lo(p[0]), hi(p[0]), s, 0);
+                    o[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o[i], lo(p[1]), hi(p[1]), s, 1);
+                    o[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o[i], lo(p[2]), hi(p[2]), s, 2);
+                    o[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o[i], lo(p[3]), hi(p[3]), s, 3);
+                }
+                if (there) {
+                    *reinterpret_cast<uint2*>(page + (tp + t) * (D / 2) + piece * 8) =
+                        make_uint2(o[0], o[1]);
+                    if (piece % 2 == 0)
+                        page[c.ks_off + (tp + t) * (D / 32) + piece / 2] = (char)e;
+                }
+            }
+        }
+    }
+
+    // V: two dims of eight tokens
+    uint32_t w[8];
+    bool there[8], full = true;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        there[t] = p0 + t >= base && p0 + t < end;
+        full = full && there[t];
+        w[t] = there[t] ? *reinterpret_cast<const uint32_t*>(v + row0 + t * r.token + 2 * lane) : 0u;
+    }
+    char* cells = page + c.v_off + (tp >> 3) * 8 * (c.v_off / c.ptok);
+    if constexpr (TYPE == kBf16) {
+        char* dst = cells + lane * 32;
+        if (full) {
+            uint32_t o[8];
+#pragma unroll
+            for (int t = 0; t < 8; t += 2) {
+                o[t / 2] = (w[t] & 0xffffu) | w[t + 1] << 16;
+                o[4 + t / 2] = w[t] >> 16 | (w[t + 1] & 0xffff0000u);
+            }
+            reinterpret_cast<uint4*>(dst)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            reinterpret_cast<uint4*>(dst)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (there[t]) {
+                    reinterpret_cast<uint16_t*>(dst)[t] = (uint16_t)w[t];
+                    reinterpret_cast<uint16_t*>(dst)[8 + t] = (uint16_t)(w[t] >> 16);
+                }
+        }
+        return;
+    }
+    uint32_t m[4];  // largest bits of tokens t (low half) and t + 4
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const uint32_t a = w[t] & 0x7fff7fffu, b = w[t + 4] & 0x7fff7fffu;
+        m[t] = pk_max((a & 0xffffu) | b << 16, a >> 16 | (b & 0xffff0000u));
+        m[t] = lanes_max<TYPE == kInt8 ? D / 2 : 16>(m[t]);
+    }
+    if constexpr (TYPE == kInt8) {
+        uint32_t o[4] = {};
+        uint16_t mine = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const uint16_t s = int8_scale(t < 4 ? m[t] & 0xffffu : m[t - 4] >> 16);
+            if (lane == t) mine = s;
+            const uint32_t a = int8_code(w[t] & 0xffffu, s) & 0xff, b = int8_code(w[t] >> 16, s) & 0xff;
+            o[t / 4] |= a << (8 * (t % 4));
+            o[2 + t / 4] |= b << (8 * (t % 4));
+        }
+        char* dst = cells + lane * 16;
+        if (full) {
+            *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (there[t]) {
+                    dst[t] = (char)(o[t / 4] >> (8 * (t % 4)));
+                    dst[8 + t] = (char)(o[2 + t / 4] >> (8 * (t % 4)));
+                }
+        }
+        if (lane < 8 && p0 + lane >= base && p0 + lane < end)
+            reinterpret_cast<uint16_t*>(page + c.vs_off)[tp + lane] = mine;
+    } else {
+        uint32_t o[2] = {};
+        uint32_t mine = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const uint32_t e = fp4_scale(t < 4 ? m[t] & 0xffffu : m[t - 4] >> 16);
+            if (lane % 16 == t) mine = e;
+            const uint32_t b =
+                __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, __uint_as_float(w[t] << 16),
+                                                         __uint_as_float(w[t] & 0xffff0000u),
+                                                         fp4_power(e), 0) & 0xffu;
+            o[t / 4] |= b << (8 * (t % 4));
+        }
+        char* dst = cells + lane * 8;
+        if (full) {
+            *reinterpret_cast<uint2*>(dst) = make_uint2(o[0], o[1]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (there[t]) dst[t] = (char)(o[t / 4] >> (8 * (t % 4)));
+        }
+        const int t = lane % 16;
+        if (t < 8 && p0 + t >= base && p0 + t < end)
+            page[c.vs_off + lane / 16 * c.ptok + tp + t] = (char)mine;
+    }
+}
+
+template <int TYPE, int D>
+__global__ __launch_bounds__(kThreads) void k_paged_read(PagedDims c, const char* pool,
+                                                         PagedLists ls, int begin, int tokens,
+                                                         int blocks, uint16_t* __restrict__ k,
+                                                         uint16_t* __restrict__ v, PagedRows r) {
+    int blk;
+    const Task<D> task(ls.lists, c.heads, blocks, &blk);
+    if (!task.any) return;
+    const int len = list_len(ls, c.ptok, task.lh);
+    const int64_t from = begin >= 0 ? begin : (int64_t)len + begin;  // position of output row 0
+    const int64_t p0 = ((from >> 3) + blk) * 8;
+    if (p0 >= from + tokens) return;
+    const char* page = p0 < len ? list_page(c, ls, pool, task.lh, p0) : nullptr;
+    const int tp = (int)(p0 & (c.ptok - 1)), lane = task.lane;
+    const int64_t row0 = task.l * r.list + task.h * r.head + (p0 - from) * r.token;
+
+    {  // K: 16 dims of one token
+        const int t = lane / (D / 16), piece = lane % (D / 16);
+        const bool out = p0 + t >= from && p0 + t < from + tokens;
+        uint32_t w[8] = {};
+        if (page && p0 + t < len) {
+            if constexpr (TYPE == kBf16) {
+                const uint4* src =
+                    reinterpret_cast<const uint4*>(page + (tp + t) * (2 * D) + piece * 32);
+                const uint4 a = src[0], b = src[1];
+                w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+                w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+            } else if constexpr (TYPE == kInt8) {
+                const uint4 a = *reinterpret_cast<const uint4*>(page + (tp + t) * D + piece * 16);
+                const uint32_t in[4] = {a.x, a.y, a.z, a.w};
+                const float s =
+                    bf16_value(reinterpret_cast<const uint16_t*>(page + c.ks_off)[tp + t]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t u = in[i / 2] >> (16 * (i & 1));
+                    w[i] = bf16_round((float)(int8_t)u * s) |
+                           (uint32_t)bf16_round((float)(int8_t)(u >> 8) * s) << 16;
+                }
+            } else {
+                const uint2 a = *reinterpret_cast<const uint2*>(page + (tp + t) * (D / 2) + piece * 8);
+                const uint32_t in[2] = {a.x, a.y};
+                const float s =
+                    fp4_power((uint8_t)page[c.ks_off + (tp + t) * (D / 32) + piece / 2]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const f32x2_t x =
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(in[i / 4] >> (8 * (i % 4)), 1.f, 0);
+                    w[i] = bf16_round(x[0] * s) | (uint32_t)bf16_round(x[1] * s) << 16;
+                }
+            }
+        }
+        if (out) {
+            uint4* dst = reinterpret_cast<uint4*>(k + row0 + t * r.token + piece * 16);
+            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+
+    // V: two dims of eight tokens
+    uint32_t w[8] = {};
+    if (page) {
+        const char* cells = page + c.v_off + (tp >> 3) * 8 * (c.v_off / c.ptok);
+        if constexpr (TYPE == kBf16) {
+            const uint4 a = reinterpret_cast<const uint4*>(cells + lane * 32)[0];
+            const uint4 b = reinterpret_cast<const uint4*>(cells + lane * 32)[1];
+            const uint32_t lo[4] = {a.x, a.y, a.z, a.w}, hi[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int t = 0; t < 8; t += 2) {
+                w[t] = (lo[t / 2] & 0xffffu) | hi[t / 2] << 16;
+                w[t + 1] = lo[t / 2] >> 16 | (hi[t / 2] & 0xffff0000u);
+            }
+        } else if constexpr (TYPE == kInt8) {
+            const uint4 a = *reinterpret_cast<const uint4*>(cells + lane * 16);
+            const uint32_t lo[2] = {a.x, a.y}, hi[2] = {a.z, a.w};
+            const uint4 sc =
+                *reinterpret_cast<const uint4*>(page + c.vs_off + 2 * tp);  // tp: a multiple of 8
+            const uint32_t ss[4] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const float s = bf16_value(ss[t / 2] >> (16 * (t & 1)) & 0xffffu);
+                w[t] = bf16_round((float)(int8_t)(lo[t / 4] >> (8 * (t % 4))) * s) |
+                       (uint32_t)bf16_round((float)(int8_t)(hi[t / 4] >> (8 * (t % 4))) * s) << 16;
+            }
+        } else {
+            const uint2 a = *reinterpret_cast<const uint2*>(cells + lane * 8);
+            const uint32_t in[2] = {a.x, a.y};
+            const uint2 sc =
+                *reinterpret_cast<const uint2*>(page + c.vs_off + lane / 16 * c.ptok + tp);
+            const uint32_t ss[2] = {sc.x, sc.y};
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const float s = fp4_power(ss[t / 4] >> (8 * (t % 4)) & 0xffu);
+                const f32x2_t x =
+                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(in[t / 4] >> (8 * (t % 4)), 1.f, 0);
+                w[t] = bf16_round(x[0] * s) | (uint32_t)bf16_round(x[1] * s) << 16;
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+        if (p0 + t >= from && p0 + t < from + tokens)
+            *reinterpret_cast<uint32_t*>(v + row0 + t * r.token + 2 * lane) =
+                p0 + t < len ? w[t] : 0u;
+}
+
+// Blocks of eight positions that `tokens` tokens starting anywhere can touch.
+int token_blocks(int tokens) { return (int)(((int64_t)tokens + 14) / 8); }
+
+template <int D>
+int grid_of(const PagedLists& l, int heads, int blocks, unsigned* grid) {
+    const int64_t n = (int64_t)l.lists * heads * blocks;
+    const int64_t g = (n + kThreads / (D / 2) - 1) / (kThreads / (D / 2));
+    if (g > 0x7fffffff) return (int)hipErrorInvalidValue;
+    *grid = (unsigned)g;
+    return 0;
+}
+
+template <int TYPE, int D>
+int write_launch(const PagedDims& c, char* pool, const PagedLists& l, const uint16_t* k,
+                 const uint16_t* v, const PagedRows& r, int tokens, const int32_t* counts,
+                 void* stream) {
+    unsigned grid;
+    const int blocks = token_blocks(tokens);
+    if (int e = grid_of<D>(l, c.heads, blocks, &grid)) return e;
+    k_paged_write<TYPE, D><<<grid, kThreads, 0, (hipStream_t)stream>>>(c, pool, l, k, v, r, tokens,
+                                                                       blocks, counts);
+    return (int)hipGetLastError();
+}
+
+template <int TYPE, int D>
+int read_launch(const PagedDims& c, const char* pool, const PagedLists& l, int begin, int tokens,
+                uint16_t* k, uint16_t* v, const PagedRows& r, void* stream) {
+    unsigned grid;
+    const int blocks = token_blocks(tokens);
+    if (int e = grid_of<D>(l, c.heads, blocks, &grid)) return e;
+    k_paged_read<TYPE, D><<<grid, kThreads, 0, (hipStream_t)stream>>>(c, pool, l, begin, tokens,
+                                                                      blocks, k, v, r);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+#define PAGED_DISPATCH(fn, ...)                                              \
+    (c.d == 128 ? (c.type == kBf16   ? fn<kBf16, 128>(__VA_ARGS__)           \
+                   : c.type == kInt8 ? fn<kInt8, 128>(__VA_ARGS__)           \
+                                     : fn<kFp4, 128>(__VA_ARGS__))           \
+                : (c.type == kBf16   ? fn<kBf16, 64>(__VA_ARGS__)            \
+                   : c.type == kInt8 ? fn<kInt8, 64>(__VA_ARGS__)            \
+                                     : fn<kFp4, 64>(__VA_ARGS__)))
+
+int launch_paged_write(const PagedDims& c, char* pool, const PagedLists& l, const uint16_t* k,
+                       const uint16_t* v, const PagedRows& r, int tokens, const int32_t* counts,
+                       void* stream) {
+    return PAGED_DISPATCH(write_launch, c, pool, l, k, v, r, tokens, counts, stream);
+}
+
+int launch_paged_read(const PagedDims& c, const char* pool, const PagedLists& l, int begin,
+                      int tokens, uint16_t* k, uint16_t* v, const PagedRows& r, void* stream) {
+    return PAGED_DISPATCH(read_launch, c, pool, l, begin, tokens, k, v, r, stream);
+}
+
+}  // namespace headkv

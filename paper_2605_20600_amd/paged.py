@@ -1,0 +1,194 @@
+"""A paged key/value cache of 16, 8 or 4 bits, decode attention over it with
+prefixes that rows share, and the scores of sampled tokens.
+
+PyTorch supplies device memory and the stream, as for Session; every
+computation is a call into libheadkv.so through the binding.
+"""
+from __future__ import annotations
+
+from typing import Dict, Optional, Tuple
+
+import torch
+
+from . import binding as B
+from .session import Session, _ptr
+
+
+def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape}, got "
+                         f"{t.dtype} {tuple(t.shape)}")
+    return t
+
+
+class Lists:
+    """Page lists of (list, key/value head): a table of page numbers with the
+    lengths, and for sliding windows the first token that is attended."""
+
+    def __init__(self, pages: torch.Tensor, length: Optional[torch.Tensor], max_len: int,
+                 first: Optional[torch.Tensor] = None, extra: int = 0):
+        """pages: int32 [lists][kv_heads][max_pages], -1 for a dropped page;
+        length, first: int32 [lists][kv_heads] or None; max_len: no list is
+        longer; extra: added to every length."""
+        if pages.dim() != 3:
+            raise ValueError("pages must be [lists][kv_heads][max_pages]")
+        n, heads, per = pages.shape
+        # kept alive with the pointers into them
+        self.pages = _device_int32(pages, (n, heads, per), "pages")
+        self.length = None if length is None else _device_int32(length, (n, heads), "length")
+        self.first = None if first is None else _device_int32(first, (n, heads), "first")
+        self.arg = B.PagedListsArg(_ptr(pages), _ptr(length), _ptr(first), n, per, extra, max_len)
+        self.kv_heads = heads
+
+    @property
+    def extra(self) -> int:
+        return self.arg.extra
+
+    def advance(self, tokens: int = 1) -> None:
+        """Every list has grown by `tokens` (after a write): counted on the host."""
+        self.arg.extra += tokens
+        self.arg.max_len += tokens
+
+
+class PagedKV:
+    """A pool of pages and the workspace of its attention.  Use one per stream."""
+
+    def __init__(self, kv_type: str, head_dim: int, kv_heads: int, num_pages: int,
+                 page_tokens: int = 64, group: int = 1, device: str = "cuda"):
+        """kv_type: "bf16", "int8" or "fp4"; group: query heads per kv head."""
+        self.cfg = B.PagedConfig(B.KV_TYPES[kv_type], head_dim, kv_heads, group, page_tokens,
+                                 num_pages)
+        self.page_bytes, pool_bytes = B.headkv_paged_plan(self.cfg)
+        self.device = device
+        self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=device)
+        self._ws = torch.zeros(256, dtype=torch.uint8, device=device)
+        self._planned = None
+
+    def lists(self, pages: torch.Tensor, length: Optional[torch.Tensor], max_len: int,
+              first: Optional[torch.Tensor] = None, extra: int = 0) -> Lists:
+        got = Lists(pages, length, max_len, first, extra)
+        if got.kv_heads != self.cfg.kv_heads:
+            raise ValueError(f"lists of {got.kv_heads} kv heads for a cache of "
+                             f"{self.cfg.kv_heads}")
+        return got
+
+    def _rows(self, k, v, lists: Lists) -> Tuple[int, Tuple[int, int, int]]:
+        shape = (lists.arg.lists, k.shape[1], self.cfg.kv_heads, self.cfg.head_dim)
+        for t in (k, v):
+            if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or t.stride(3) != 1:
+                raise ValueError(f"k and v must be bf16 [lists][tokens][kv_heads][head_dim] = "
+                                 f"{shape} with contiguous rows, got {t.dtype} {tuple(t.shape)}")
+        # the stride of a dimension of one is never used, and may be anything
+        ks, vs = (tuple(st if n > 1 else 0 for st, n in zip(t.stride(), shape[:3]))
+                  for t in (k, v))
+        if ks != vs:
+            raise ValueError("k and v must have the same strides")
+        return shape[1], ks
+
+    def write(self, lists: Lists, k: torch.Tensor, v: torch.Tensor,
+              counts: Optional[torch.Tensor] = None) -> None:
+        """Appends k, v (bf16 [lists][tokens][kv_heads][head_dim], any strides)
+        behind the lists' tokens; counts: int32 [lists], tokens of each list."""
+        tokens, strides = self._rows(k, v, lists)
+        if counts is not None:
+            _device_int32(counts, (lists.arg.lists,), "counts")
+        B.headkv_paged_write(self.cfg, self.pool.data_ptr(), lists.arg, k.data_ptr(),
+                             v.data_ptr(), strides, tokens, _ptr(counts), Session.stream())
+
+    def read(self, lists: Lists, tokens: int, begin: int = 0, k: Optional[torch.Tensor] = None,
+             v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Tokens begin .. begin + tokens of every list (begin < 0: counted from
+        its end) as bf16 [lists][tokens][kv_heads][head_dim], zeros past the end."""
+        if k is None:
+            k = torch.empty((lists.arg.lists, tokens, self.cfg.kv_heads, self.cfg.head_dim),
+                            dtype=torch.bfloat16, device=self.device)
+        if v is None:
+            v = torch.empty_like(k)
+        got, strides = self._rows(k, v, lists)
+        if got != tokens:
+            raise ValueError(f"k and v hold {got} tokens, {tokens} are read")
+        B.headkv_paged_read(self.cfg, self.pool.data_ptr(), lists.arg, begin, tokens,
+                            k.data_ptr(), v.data_ptr(), strides, Session.stream())
+        return k, v
+
+    def _workspace(self, own: Lists, shared: Optional[Lists]) -> torch.Tensor:
+        """Planned once for the lists' tables, for any length that they can hold."""
+        key = (own.arg.lists, own.arg.max_pages,
+               *(() if shared is None else (shared.arg.lists, shared.arg.max_pages)))
+        if key != self._planned:
+            most = []
+            for l in (own, shared):
+                a = None
+                if l is not None:
+                    a = B.PagedListsArg(None, None, None, l.arg.lists, l.arg.max_pages, 0,
+                                        l.arg.max_pages * self.cfg.page_tokens)
+                most.append(a)
+            need = B.headkv_paged_attn_plan(self.cfg, *most)
+            if need > self._ws.numel():
+                self._ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            self._planned = key
+        return self._ws
+
+    def attn(self, own: Lists, q: torch.Tensor, shared: Optional[Lists] = None,
+             share: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+             lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of q (bf16 [batch][kv_heads * group][head_dim], rows of any
+        stride) over the rows' own lists and the shared ones that `share` (int32
+        [batch], list number or -1) names; fp32 out, and lse if given."""
+        c = self.cfg
+        batch, heads = own.arg.lists, c.kv_heads * c.group
+        if (q.dtype != torch.bfloat16 or tuple(q.shape) != (batch, heads, c.head_dim)
+                or q.stride(2) != 1 or (heads > 1 and q.stride(1) != c.head_dim)):
+            raise ValueError(f"q must be bf16 {(batch, heads, c.head_dim)} with contiguous rows")
+        if out is None:
+            out = torch.empty((batch, heads, c.head_dim), dtype=torch.float32, device=self.device)
+        for t, shape in ((out, (batch, heads, c.head_dim)), (lse, (batch, heads))):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape
+                                  or not t.is_contiguous()):
+                raise ValueError(f"out / lse must be contiguous float32 of shape {shape}")
+        if share is not None:
+            _device_int32(share, (batch,), "share")
+        ws = self._workspace(own, shared)
+        B.headkv_paged_attn(c, self.pool.data_ptr(), own.arg,
+                            None if shared is None else shared.arg, _ptr(share), q.data_ptr(),
+                            q.stride(0) if batch > 1 else 0, out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(),
+                            Session.stream())
+        return out
+
+
+_score_ws: Dict[Tuple[int, int], torch.Tensor] = {}  # per device and stream
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
+                   temperature: float = 1.0) -> Dict[str, torch.Tensor]:
+    """Scores of `tokens` (int32 [rows]) under softmax(logits / temperature),
+    logits [rows][vocab] bf16 or float32 with rows of any stride: "logprob",
+    "entropy" and "rank" per row, and with top > 0 "top_logprob" and "top_index"
+    [rows][top]."""
+    types = {torch.bfloat16: B.HEADKV_LOGITS_BF16, torch.float32: B.HEADKV_LOGITS_F32}
+    if logits.dim() != 2 or logits.dtype not in types or logits.stride(1) != 1:
+        raise ValueError("logits must be bf16 or float32 [rows][vocab] with contiguous rows")
+    rows, vocab = logits.shape
+    _device_int32(tokens, (rows,), "tokens")
+    dev = logits.device
+    f32 = lambda *s: torch.empty(s, dtype=torch.float32, device=dev)
+    i32 = lambda *s: torch.empty(s, dtype=torch.int32, device=dev)
+    res = {"logprob": f32(rows), "entropy": f32(rows), "rank": i32(rows)}
+    if top > 0:
+        res["top_logprob"], res["top_index"] = f32(rows, top), i32(rows, top)
+    stream = Session.stream()
+    need = B.headkv_logprobs_plan(rows, vocab, top)
+    ws = None
+    if need:
+        key = (dev.index or 0, stream)
+        ws = _score_ws.get(key)
+        if ws is None or ws.numel() < need:
+            ws = _score_ws[key] = torch.zeros(need, dtype=torch.uint8, device=dev)
+    B.headkv_token_logprobs(logits.data_ptr(), types[logits.dtype], rows, vocab,
+                            logits.stride(0) if rows > 1 else vocab, tokens.data_ptr(),
+                            temperature, top,
+                            res["logprob"].data_ptr(), res["entropy"].data_ptr(),
+                            res["rank"].data_ptr(), _ptr(res.get("top_logprob")),
+                            _ptr(res.get("top_index")), _ptr(ws), 0 if ws is None else ws.numel(),
+                            stream)
+    return res
