@@ -1,8 +1,32 @@
-// Decode attention over a paged cache, with prefixes that several rows share.
-// One wavefront per (batch row, query head): a lane scores one token at a time,
-// 64 tokens share a running maximum, then every lane sums its own dims.
+// Decode attention over a paged cache, with prefixes that several rows share
+// (formulas and formats: headkv.h; page layout: paged.h).
+//
+// All query vectors that read one list of keys and values are the columns of one
+// small matrix: the group's query heads for a row's own list, those of every row
+// that shares it for a prefix.  A wavefront takes NB * 16 columns and steps of 32
+// tokens (a step lies in one page); per step, on 16x16x32 bf16 matrix
+// instructions,
+//   S^T = K Q^T   A = the keys as they lie in the page: lane l holds 16 bytes of
+//                 one token's row at a time.  Which dims a lane's part of the
+//                 contraction stands for is free as long as Q^T agrees, so a
+//                 load is contiguous; which token a row of A stands for is free
+//                 too, and is chosen so that the eight scores a lane gets are
+//                 those of the eight tokens of one V cell.
+//   softmax       online, per column in fp32 (exp2), a running maximum per
+//                 wavefront
+//   O^T += V^T P^T  A = V cells (eight tokens of a dim) as they lie in the page,
+//                 B = the lane's eight weights as they are.  A weight enters as
+//                 three bf16 numbers that sum to it exactly (24 bits), so P keeps
+//                 fp32's precision.
+// Nothing goes through LDS or between lanes but the maximum.  Codes of 8 and 4
+// bits are exact in bf16; an INT8 scale multiplies its token's score or weight,
+// an FP4 scale enters with the conversion.
+// The wavefronts of a block split its tokens and meet in LDS; blocks split a list
+// into chunks, whose parts (maximum, sum, unnormalised output) k_merge joins in
+// chunk order.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -14,109 +38,690 @@ namespace {
 
 using namespace dev;
 
-// Value of dim i of token tp of a page: K rows (V false) or V cells.
-template <int TYPE, int D, bool V>
-__device__ __forceinline__ float element(const PagedDims& c, const char* page, int tp, int i) {
-    const char* base = V ? page + c.v_off : page;
-    if constexpr (TYPE == kBf16) {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(base);
-        return bf16_value(V ? p[((tp >> 3) * D + i) * 8 + (tp & 7)] : p[tp * D + i]);
-    } else if constexpr (TYPE == kInt8) {
-        const int8_t* p = reinterpret_cast<const int8_t*>(base);
-        const float s = bf16_value(
-            reinterpret_cast<const uint16_t*>(page + (V ? c.vs_off : c.ks_off))[tp]);
-        return (float)(V ? p[((tp >> 3) * D + i) * 8 + (tp & 7)] : p[tp * D + i]) * s;
-    } else {
-        const uint8_t* p = reinterpret_cast<const uint8_t*>(base);
-        const uint32_t b =
-            V ? p[((tp >> 3) * (D / 2) + i / 2) * 8 + (tp & 7)] : p[tp * (D / 2) + i / 2];
-        const uint32_t e = (uint8_t)(V ? page[c.vs_off + i / 32 * c.ptok + tp]
-                                       : page[c.ks_off + tp * (D / 32) + i / 32]);
-        const f32x2_t x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(b, 1.f, 0);
-        return x[i & 1] * fp4_power(e);
-    }
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kStep = 32;                          // tokens of a wavefront's step
+constexpr int kUnit = kStep * kWaves;              // and of a block's
+constexpr int kMaxChunk = 64 * kUnit;              // a lane per step holds its page number
+
+// One attention call as the kernels see it.
+struct AttnCall {
+    PagedDims c;
+    const char* pool;
+    PagedLists own, shared;
+    const int32_t* share;
+    const uint16_t* q;
+    int64_t q_stride;
+    float* out;
+    float* lse;
+    f32x2_t* ml;   // [batch][query heads][parts] maximum (log2) and sum
+    float* part;   // [batch][query heads][parts][d]
+    int own_chunk, own_parts;        // tokens of a chunk, chunks at most
+    int shared_chunk, shared_parts;  // (0: no shared lists)
+    int tiles;                       // column tiles in the grid, per shared list
+};
+
+__device__ __forceinline__ u32x4_t nt16(const char* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
 }
 
+// What a step reads of a page: lane l has i = l % 16 and quarter = l / 16.
 template <int TYPE, int D>
-__global__ __launch_bounds__(64) void k_paged_attn(PagedDims c, const char* pool, PagedLists own,
-                                                   PagedLists shared, const int32_t* share,
-                                                   const uint16_t* q, int64_t q_stride, float* out,
-                                                   float* lse) {
-    const int hq = blockIdx.x % (c.heads * c.group), b = blockIdx.x / (c.heads * c.group);
-    const int h = hq / c.group, lane = threadIdx.x;
-    __shared__ float qs[D];
-    const float scale = (float)(1.0 / __builtin_sqrt((double)D));
-    for (int i = lane; i < D; i += 64) qs[i] = bf16_value(q[b * q_stride + hq * D + i]) * scale;
-    __syncthreads();
-    float m = -INFINITY, sum = 0.f, acc[D / 64] = {};
-    auto visit = [&](const PagedLists& p, int64_t lh) {
-        const int len = list_len(p, c.ptok, lh);
-        const int first = p.first ? max(p.first[lh], 0) : 0;
-        for (int t0 = first & ~31; t0 < len; t0 += 32) {  // 32 tokens lie in one page
-            const char* page = list_page(c, p, pool, lh, t0);
-            if (!page) continue;
-            const int tp = t0 & (c.ptok - 1), t = t0 + lane;
-            float s = -INFINITY;
-            if (lane < 32 && t >= first && t < len) {
-                s = 0.f;
-                for (int i = 0; i < D; ++i)
-                    s = fmaf(qs[i], element<TYPE, D, false>(c, page, tp + lane, i), s);
+struct Tile {
+    static constexpr int KN = TYPE == kBf16 ? D / 32 : TYPE == kInt8 ? D / 64 : 1;
+    static constexpr int VN = TYPE == kBf16 ? D / 16 : TYPE == kInt8 ? D / 32 : D / 64;
+    u32x4_t k[2][KN];
+    u32x4_t v[VN];
+    u32x4_t ks, vs;     // INT8: scales of the quarter's eight tokens
+    uint32_t ke[2];     // FP4: exponents of the lane's key rows
+    u32x2_t ve[D / 64]; // and of its eight tokens of each V load
+
+    __device__ __forceinline__ void load(const PagedDims& c, const char* page, int tp, int lane) {
+        const int i = lane & 15, quarter = lane >> 4;
+        const char* vp = page + c.v_off;
+        if constexpr (TYPE == kBf16) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
+#pragma unroll
+                for (int j = 0; j < KN; ++j) k[u][j] = nt16(page + row * (2 * D) + (4 * j + quarter) * 16);
             }
-            float mx = s;
-            for (int o = 1; o < 64; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o));
-            mx = fmaxf(mx, m);
-            if (mx == -INFINITY) mx = 0.f;  // nothing seen yet: exp of -inf stays 0
-            const float f = expf(m - mx), w = expf(s - mx);
-            m = mx;
-            sum = sum * f + w;
-            for (float& a : acc) a *= f;
-            for (int j = 0; j < 32; ++j) {
-                if (t0 + j < first || t0 + j >= len) continue;
-                const float wj = __shfl(w, j);
-                for (int e = 0; e < D / 64; ++e)
-                    acc[e] = fmaf(wj, element<TYPE, D, true>(c, page, tp + j, lane + 64 * e), acc[e]);
+#pragma unroll
+            for (int j = 0; j < VN; ++j)
+                v[j] = nt16(vp + ((tp >> 3) + quarter) * (D * 16) + (16 * j + i) * 16);
+        } else if constexpr (TYPE == kInt8) {
+            ks = *reinterpret_cast<const u32x4_t*>(page + c.ks_off + 2 * (tp + 8 * quarter));
+            vs = *reinterpret_cast<const u32x4_t*>(page + c.vs_off + 2 * (tp + 8 * quarter));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
+#pragma unroll
+                for (int j = 0; j < KN; ++j) k[u][j] = nt16(page + row * D + (4 * j + quarter) * 16);
+            }
+#pragma unroll
+            for (int j = 0; j < VN; ++j)
+                v[j] = nt16(vp + ((tp >> 3) + quarter) * (D * 8) + (32 * j + 2 * i) * 8);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
+                ke[u] = (uint8_t)page[c.ks_off + row * (D / 32) + (D == 128 ? quarter : quarter >> 1)];
+                if constexpr (D == 128) {
+                    k[u][0] = nt16(page + row * (D / 2) + quarter * 16);
+                } else {
+                    const u32x2_t w = __builtin_nontemporal_load(
+                        reinterpret_cast<const u32x2_t*>(page + row * (D / 2) + quarter * 8));
+                    k[u][0] = u32x4_t{w[0], w[1], 0, 0};
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < VN; ++j) {
+                ve[j] = *reinterpret_cast<const u32x2_t*>(
+                    page + c.vs_off + (2 * j + (i >> 3)) * c.ptok + tp + 8 * quarter);
+                v[j] = nt16(vp + ((tp >> 3) + quarter) * (D * 4) + (32 * j + 2 * i) * 8);
             }
         }
-    };
-    visit(own, (int64_t)b * c.heads + h);
-    if (share) {
-        const int l = share[b];
-        if (l >= 0 && l < shared.lists) visit(shared, (int64_t)l * c.heads + h);
     }
-    for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
-    const int64_t row = (int64_t)b * c.heads * c.group + hq;
-    for (int e = 0; e < D / 64; ++e)
-        out[row * D + lane + 64 * e] = sum == 0.f ? 0.f : acc[e] / sum;
-    if (lse && lane == 0) lse[row] = sum == 0.f ? -INFINITY : m + logf(sum);
+
+    // Nothing that times a zero weight is not zero, for the lane's tokens n whose
+    // bit n of `seen` is 0 (never written, perhaps).
+    __device__ __forceinline__ void blank(uint32_t seen) {
+        if constexpr (TYPE == kFp4) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m |= seen >> (4 * h + e) & 1 ? 0xffu << (8 * e) : 0u;
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) ve[j][h] &= m;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t m = (seen >> (2 * e) & 1 ? 0xffffu : 0u) |
+                                   (seen >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+                if constexpr (TYPE == kInt8) {
+                    vs[e] &= m;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VN; ++j) v[j][e] &= m;
+                }
+            }
+        }
+    }
+};
+
+// First of the eight dims of key step s that a lane of `quarter` holds.
+template <int TYPE, int D>
+__device__ __forceinline__ int key_dim(int s, int quarter) {
+    if (TYPE == kBf16) return 32 * s + 8 * quarter;
+    if (TYPE == kInt8) return 64 * (s >> 1) + 16 * quarter + 8 * (s & 1);
+    return D / 4 * quarter + 8 * s;
+}
+
+__device__ __forceinline__ uint32_t pack_high(uint32_t lo, uint32_t hi) {  // bits 31:16 of each
+    return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+__device__ __forceinline__ uint32_t pack_low(uint32_t lo, uint32_t hi) {
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+// A loaded word as it is: without this the compiler keeps the bytes that are used
+// later apart from the load on, in a register each (INT8, d = 128: 347 instead of
+// 155 registers).
+__device__ __forceinline__ uint32_t whole(uint32_t w) {
+    asm("" : "+v"(w));
+    return w;
+}
+// four int8 codes as bf16 (exact)
+__device__ __forceinline__ void int8_pack(uint32_t in, uint32_t* o) {
+    const uint32_t w = whole(in);
+    const uint32_t a = __float_as_uint((float)(int8_t)w), b = __float_as_uint((float)(int8_t)(w >> 8));
+    const uint32_t c = __float_as_uint((float)(int8_t)(w >> 16)), d = __float_as_uint((float)(int8_t)(w >> 24));
+    o[0] = pack_high(a, b);
+    o[1] = pack_high(c, d);
+}
+template <int SEL>
+__device__ __forceinline__ uint32_t fp4_pack(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+}
+__device__ __forceinline__ bf16x8_t operand(const uint32_t* w) {
+    return __builtin_bit_cast(bf16x8_t, u32x4_t{w[0], w[1], w[2], w[3]});
 }
 
 template <int TYPE, int D>
-int attn_launch(const PagedDims& c, const char* pool, const PagedLists& own,
-                const PagedLists* shared, const int32_t* share, const uint16_t* q,
-                int64_t q_stride, float* out, float* lse, void* stream) {
-    const unsigned grid = (unsigned)own.lists * c.heads * c.group;
-    k_paged_attn<TYPE, D><<<grid, 64, 0, (hipStream_t)stream>>>(
-        c, pool, own, shared ? *shared : PagedLists{}, share, q, q_stride, out, lse);
+__device__ __forceinline__ bf16x8_t key_operand(const Tile<TYPE, D>& t, int u, int s) {
+    if constexpr (TYPE == kBf16) return __builtin_bit_cast(bf16x8_t, t.k[u][s]);
+    uint32_t o[4];
+    if constexpr (TYPE == kInt8) {
+        int8_pack(t.k[u][s >> 1][2 * (s & 1)], o);
+        int8_pack(t.k[u][s >> 1][2 * (s & 1) + 1], o + 2);
+    } else {
+        const float e = fp4_power(t.ke[u]);
+        const uint32_t w = t.k[u][0][s];
+        o[0] = fp4_pack<0>(w, e);
+        o[1] = fp4_pack<1>(w, e);
+        o[2] = fp4_pack<2>(w, e);
+        o[3] = fp4_pack<3>(w, e);
+    }
+    return operand(o);
+}
+
+// V^T operands of load j: one for each of the dims it holds (1, 2 or 4).
+template <int TYPE, int D>
+__device__ __forceinline__ void value_operands(const Tile<TYPE, D>& t, int j, bf16x8_t* a) {
+    if constexpr (TYPE == kBf16) {
+        a[0] = __builtin_bit_cast(bf16x8_t, t.v[j]);
+    } else if constexpr (TYPE == kInt8) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            uint32_t o[4];
+            int8_pack(t.v[j][2 * x], o);
+            int8_pack(t.v[j][2 * x + 1], o + 2);
+            a[x] = operand(o);
+        }
+    } else {
+        float e[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w = whole(t.ve[j][h]);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) e[4 * h + n] = fp4_power(w >> (8 * n) & 0xffu);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            uint32_t w[8], lo[4], hi[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t b = t.v[j][2 * x + h];
+                w[4 * h] = fp4_pack<0>(b, e[4 * h]);
+                w[4 * h + 1] = fp4_pack<1>(b, e[4 * h + 1]);
+                w[4 * h + 2] = fp4_pack<2>(b, e[4 * h + 2]);
+                w[4 * h + 3] = fp4_pack<3>(b, e[4 * h + 3]);
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                lo[n] = pack_low(w[2 * n], w[2 * n + 1]);
+                hi[n] = pack_high(w[2 * n], w[2 * n + 1]);
+            }
+            a[2 * x] = operand(lo);
+            a[2 * x + 1] = operand(hi);
+        }
+    }
+}
+
+// State of a wavefront: column i = lane % 16 of each of its NB tiles.
+template <int TYPE, int D, int NB>
+struct Wave {
+    static constexpr int KS = D / 32;  // key steps
+    static constexpr int DB = D / 16;  // blocks of 16 output rows
+    static constexpr int VX = DB / Tile<TYPE, D>::VN;  // dims of a V load
+    bf16x8_t q[NB][KS];
+    f32x4_t acc[NB][DB];  // block VX j + x: rows 16 of load j, dim x of each
+    float m[NB], sum[NB];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            m[b] = -INFINITY;
+            sum[b] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DB; ++j) acc[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // partial: not all tokens are attended, bit n of `seen` is set if token n of
+    // the lane's eight is
+    __device__ __forceinline__ void step(const Tile<TYPE, D>& t, bool partial, uint32_t seen) {
+        constexpr float kScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0));
+        f32x4_t st[NB][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) st[b][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                if (s % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                const bf16x8_t a = key_operand<TYPE, D>(t, u, s);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    st[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[b][s], st[b][u], 0, 0, 0);
+            }
+        }
+        float ks[8], vs[8];  // INT8: scales of the lane's tokens
+#pragma unroll
+        for (int n = 0; n < 8; ++n) ks[n] = kScale;
+        if constexpr (TYPE == kInt8) {
+#pragma unroll
+            for (int n = 0; n < 8; n += 2) {
+                const uint32_t k = whole(t.ks[n / 2]), v = whole(t.vs[n / 2]);
+                ks[n] *= __uint_as_float(k << 16);
+                ks[n + 1] *= __uint_as_float(k & 0xffff0000u);
+                vs[n] = __uint_as_float(v << 16);
+                vs[n + 1] = __uint_as_float(v & 0xffff0000u);
+            }
+        }
+        // pieces of the weights: B operands, three for each column tile
+        bf16x8_t p[NB][3];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float s[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) s[n] = st[b][n / 4][n % 4] * ks[n];
+            if (partial) {
+#pragma unroll
+                for (int n = 0; n < 8; ++n) s[n] = seen >> n & 1 ? s[n] : -INFINITY;
+            }
+            float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])),
+                             fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            if (__builtin_amdgcn_ballot_w64(mx > m[b]) != 0) {
+                const float now = fmaxf(mx, m[b]);
+                const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[b] - now);
+                m[b] = now;
+                sum[b] *= f;
+#pragma unroll
+                for (int j = 0; j < DB; ++j) acc[b][j] *= f;
+            }
+            const float less = m[b] == -INFINITY ? 0.f : m[b];
+            uint32_t w[3][4];
+#pragma unroll
+            for (int n = 0; n < 8; n += 2) {
+                uint32_t hi[2], mid[2], lo[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = __builtin_amdgcn_exp2f(s[n + e] - less);
+                    sum[b] += x;
+                    if constexpr (TYPE == kInt8) x *= vs[n + e];
+                    hi[e] = __float_as_uint(x);
+                    const float r = x - __uint_as_float(hi[e] & 0xffff0000u);
+                    mid[e] = __float_as_uint(r);
+                    lo[e] = __float_as_uint(r - __uint_as_float(mid[e] & 0xffff0000u));
+                }
+                w[0][n / 2] = pack_high(hi[0], hi[1]);
+                w[1][n / 2] = pack_high(mid[0], mid[1]);
+                w[2][n / 2] = pack_high(lo[0], lo[1]);
+            }
+#pragma unroll
+            for (int e = 0; e < 3; ++e) p[b][e] = operand(w[e]);
+        }
+#pragma unroll
+        for (int j = 0; j < Tile<TYPE, D>::VN; ++j) {
+            __builtin_amdgcn_sched_barrier(0);  // one load's conversions at a time: registers
+            bf16x8_t a[VX];
+            value_operands<TYPE, D>(t, j, a);
+#pragma unroll
+            for (int x = 0; x < VX; ++x)
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+                        acc[b][VX * j + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            a[x], p[b][e], acc[b][VX * j + x], 0, 0, 0);
+        }
+    }
+
+    // Tokens [t0, t1) of a list, t0 a multiple of 32, those before `first` not
+    // attended; this wavefront takes every fourth step.
+    __device__ __forceinline__ void run(const PagedDims& c, const char* pool, const int32_t* pages,
+                                        int t0, int t1, int first, int wave, int lane) {
+        // lane n: the page of the wavefront's n-th step, if it is there
+        const int mine = t0 + (wave + kWaves * lane) * kStep;
+        int page = -1;
+        if (mine < t1) page = pages[mine >> c.pshift];
+        uint64_t todo = __builtin_amdgcn_ballot_w64(page >= 0 && page < c.num_pages);
+        if (!todo) return;
+        auto fetch = [&](Tile<TYPE, D>& t, int n) {
+            const int pg = __builtin_amdgcn_readlane(page, n);
+            const int at = t0 + (wave + kWaves * n) * kStep;
+            t.load(c, pool + pg * c.page_bytes, at & (c.ptok - 1), lane);
+        };
+        Tile<TYPE, D> now, next;
+        int n = __builtin_ctzll(todo);
+        fetch(now, n);
+        for (;;) {
+            todo &= todo - 1;
+            const int after = todo ? __builtin_ctzll(todo) : -1;
+            if (after >= 0) fetch(next, after);
+            const int at = t0 + (wave + kWaves * n) * kStep;
+            const bool partial = at < first || at + kStep > t1;
+            uint32_t seen = 0xffu;
+            if (partial) {
+                // of the lane's eight tokens those of [first, t1)
+                const int tk = at + 8 * (lane >> 4);
+                const int lo = min(max(first - tk, 0), 8), hi = min(max(t1 - tk, 0), 8);
+                seen = 0xffu >> (8 - hi) & 0xffu << lo;
+                now.blank(seen);
+            }
+            step(now, partial, seen);
+            if (after < 0) break;
+            now = next;
+            n = after;
+        }
+    }
+};
+
+// Joins the wavefronts of a block, column tile by column tile, and gives every
+// column's maximum, sum and output to `store(column, d, four outputs, m, sum)`.
+template <int TYPE, int D, int NB, typename Store>
+__device__ __forceinline__ void join_waves(Wave<TYPE, D, NB>& w, float* lds, int wave, int lane,
+                                           Store store) {
+    constexpr int ROW = D + 4;  // floats of a column in LDS: 16-byte writes of 16 columns do not meet
+    constexpr int VX = Wave<TYPE, D, NB>::VX, VN = Tile<TYPE, D>::VN;
+    float* o = lds;                              // [wave][16][ROW]
+    float* ms = lds + kWaves * 16 * ROW;         // [wave][16] maximum, then sum
+    const int i = lane & 15, quarter = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float sum = w.sum[b];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16) {
+            ms[wave * 16 + lane] = w.m[b];
+            ms[(kWaves + wave) * 16 + lane] = sum;
+        }
+        float* row = o + (wave * 16 + i) * ROW;
+#pragma unroll
+        for (int j = 0; j < VN; ++j) {
+            const f32x4_t* a = w.acc[b] + VX * j;
+            if constexpr (VX == 1) {
+                *reinterpret_cast<f32x4_t*>(row + 16 * j + 4 * quarter) = a[0];
+            } else if constexpr (VX == 2) {
+                f32x4_t* p = reinterpret_cast<f32x4_t*>(row + 32 * j + 8 * quarter);
+                p[0] = f32x4_t{a[0][0], a[1][0], a[0][1], a[1][1]};
+                p[1] = f32x4_t{a[0][2], a[1][2], a[0][3], a[1][3]};
+            } else {
+                f32x4_t* p = reinterpret_cast<f32x4_t*>(row + 64 * j + 16 * quarter);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] = f32x4_t{a[0][r], a[1][r], a[2][r], a[3][r]};
+            }
+        }
+        __syncthreads();
+        const int tid = wave * 64 + lane;
+#pragma unroll
+        for (int k0 = 0; k0 < 16 * D / 4; k0 += kThreads) {
+            const int k = k0 + tid, col = k / (D / 4), d = k % (D / 4) * 4;
+            float m = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < kWaves; ++x) m = fmaxf(m, ms[x * 16 + col]);
+            f32x4_t v{0.f, 0.f, 0.f, 0.f};
+            float s = 0.f;
+#pragma unroll
+            for (int x = 0; x < kWaves; ++x) {
+                const float mx = ms[x * 16 + col];
+                const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m);
+                s += f * ms[(kWaves + x) * 16 + col];
+                v += f * *reinterpret_cast<const f32x4_t*>(o + (x * 16 + col) * ROW + d);
+            }
+            store(16 * b + col, d, v, m, s);
+        }
+        __syncthreads();
+    }
+}
+
+template <int D>
+constexpr int lds_floats() {
+    return kWaves * 16 * (D + 4) + 2 * kWaves * 16;
+}
+
+__device__ __forceinline__ void write_out(const AttnCall& a, int64_t row, int d, int D, f32x4_t v,
+                                          float m, float sum) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    *reinterpret_cast<f32x4_t*>(a.out + row * D + d) = v * inv;
+    if (a.lse && d == 0)
+        a.lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+// The chunks of a list: its tokens from the step of `first` on.
+struct Span {
+    int len, first, start, chunks;
+};
+__device__ __forceinline__ Span span_of(const PagedLists& p, int ptok, int64_t lh, int chunk) {
+    Span s;
+    s.len = list_len(p, ptok, lh);
+    s.first = p.first ? max(p.first[lh], 0) : 0;
+    s.start = s.first & ~(kStep - 1);
+    s.chunks = s.len > s.first ? (s.len - s.start + chunk - 1) / chunk : 0;
+    return s;
+}
+
+// A row's own list: one block per (row, kv head, chunk).
+template <int TYPE, int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_own(AttnCall a) {
+    __shared__ __align__(16) float lds[lds_floats<D>()];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lists = a.own.lists * a.c.heads;
+    const int lh = blockIdx.x % lists, chunk = blockIdx.x / lists;
+    const int b = lh / a.c.heads, h = lh % a.c.heads;
+    const Span s = span_of(a.own, a.c.ptok, lh, a.own_chunk);
+    const bool whole = a.own_parts == 1 && a.shared_parts == 0;  // nothing to merge
+    if (chunk >= s.chunks && !(whole && s.chunks == 0)) return;
+    const int t0 = s.start + chunk * a.own_chunk, t1 = min(s.len, t0 + a.own_chunk);
+    const int hq = a.c.heads * a.c.group;
+    const int64_t row0 = (int64_t)b * hq + h * a.c.group;
+
+    Wave<TYPE, D, 1> w;
+    w.clear();
+    const int g = lane & 15;
+    const uint16_t* q = a.q + b * a.q_stride + (h * a.c.group + min(g, a.c.group - 1)) * D;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)
+        w.q[0][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
+    if (t0 < t1)
+        w.run(a.c, a.pool, a.own.pages + (int64_t)lh * a.own.max_pages, t0, t1, s.first, wave, lane);
+    const int parts = a.own_parts + a.shared_parts;
+    join_waves(w, lds, wave, lane, [&](int col, int d, f32x4_t v, float m, float sum) {
+        if (col >= a.c.group) return;
+        const int64_t row = row0 + col;
+        if (whole) {
+            write_out(a, row, d, D, v, m, sum);
+        } else {
+            const int64_t slot = row * parts + chunk;
+            *reinterpret_cast<f32x4_t*>(a.part + slot * D + d) = v;
+            if (d == 0) a.ml[slot] = f32x2_t{m, sum};
+        }
+    });
+}
+
+// A shared list: one block per (list, kv head, chunk) and column tile, which
+// takes every `tiles`-th tile of the NB * 16 columns (members * group of them).
+template <int TYPE, int D, int NB>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(NB == 4 ? 1 : 2)))
+void k_attn_shared(AttnCall a) {
+    constexpr int COLS = 16 * NB;
+    __shared__ __align__(16) float lds[lds_floats<D>()];
+    __shared__ int row_of[COLS + 1];
+    __shared__ int found[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lists = a.shared.lists * a.c.heads;
+    const int per_tile = lists * a.shared_parts;
+    const int tile0 = blockIdx.x / per_tile, item = blockIdx.x % per_tile;
+    const int lh = item % lists, chunk = item / lists;
+    const int list = lh / a.c.heads, h = lh % a.c.heads, group = a.c.group;
+    const Span s = span_of(a.shared, a.c.ptok, lh, a.shared_chunk);
+    if (chunk >= s.chunks) return;
+    const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
+    const int hq = a.c.heads * group, parts = a.own_parts + a.shared_parts;
+
+    for (int tile = tile0;; tile += a.tiles) {
+        // the members that the tile's columns belong to: ranks [rank0, rank1)
+        const int c0 = tile * COLS, rank0 = c0 / group, rank1 = (c0 + COLS - 1) / group + 1;
+        int members = 0;
+        for (int b0 = 0; b0 < a.own.lists && members < rank1; b0 += kThreads) {
+            const int b = b0 + tid;
+            const bool is = b < a.own.lists && a.share[b] == list;
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(is);
+            if (lane == 0) found[wave] = __builtin_popcountll(mask);
+            __syncthreads();
+            int rank = members + __builtin_popcountll(mask & ((1ull << lane) - 1));
+            for (int x = 0; x < kWaves; ++x) {
+                if (x < wave) rank += found[x];
+                members += found[x];
+            }
+            if (is && rank >= rank0 && rank < rank1) row_of[rank - rank0] = b;
+            __syncthreads();
+        }
+        const int cols = min(COLS, members * group - c0);  // of this tile
+        if (cols <= 0) return;
+
+        Wave<TYPE, D, NB> w;
+        w.clear();
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const int col = c0 + min(16 * n + (lane & 15), cols - 1);
+            const uint16_t* q = a.q + row_of[col / group - rank0] * a.q_stride +
+                                (h * group + col % group) * D;
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+                w.q[n][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
+        }
+        w.run(a.c, a.pool, a.shared.pages + (int64_t)lh * a.shared.max_pages, t0, t1, s.first, wave,
+              lane);
+        join_waves(w, lds, wave, lane, [&](int n, int d, f32x4_t v, float m, float sum) {
+            if (n >= cols) return;
+            const int col = c0 + n;
+            const int64_t row =
+                (int64_t)row_of[col / group - rank0] * hq + h * group + col % group;
+            const int64_t slot = row * parts + a.own_parts + chunk;
+            *reinterpret_cast<f32x4_t*>(a.part + slot * D + d) = v;
+            if (d == 0) a.ml[slot] = f32x2_t{m, sum};
+        });
+    }
+}
+
+// Joins the parts of every query: D / 4 lanes each, in the order of the parts.
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_merge(AttnCall a) {
+    constexpr int LANES = D / 4;
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+    const int hq = a.c.heads * a.c.group;
+    if (row >= (int64_t)a.own.lists * hq) return;
+    const int d = threadIdx.x % LANES * 4, b = (int)(row / hq), h = (int)(row % hq) / a.c.group;
+    const int own = span_of(a.own, a.c.ptok, (int64_t)b * a.c.heads + h, a.own_chunk).chunks;
+    int shared = 0;
+    if (a.shared_parts) {
+        const int l = a.share[b];
+        if (l >= 0 && l < a.shared.lists)
+            shared = span_of(a.shared, a.c.ptok, (int64_t)l * a.c.heads + h, a.shared_chunk).chunks;
+    }
+    const int64_t slot0 = row * (a.own_parts + a.shared_parts);
+    float m = -INFINITY;
+    auto slot = [&](int i) { return slot0 + (i < own ? i : a.own_parts + i - own); };
+    for (int i = 0; i < own + shared; ++i) m = fmaxf(m, a.ml[slot(i)][0]);
+    f32x4_t v{0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int i = 0; i < own + shared; ++i) {
+        const f32x2_t ml = a.ml[slot(i)];
+        const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
+        sum += f * ml[1];
+        v += f * *reinterpret_cast<const f32x4_t*>(a.part + slot(i) * D + d);
+    }
+    write_out(a, row, d, D, v, m, sum);
+}
+
+// ------------------------------------------------------------------- launch
+constexpr int kCus = 256;
+
+// Tokens of a chunk, so that `items` lists of up to max_len tokens give the chip
+// about two blocks per CU; at least two steps of a block.
+int chunk_of(int64_t items, int max_len) {
+    const int64_t want = std::max<int64_t>(1, 2 * kCus / items);
+    int64_t chunk = (max_len + want - 1) / want;
+    chunk = (chunk + kUnit - 1) / kUnit * kUnit;
+    return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), kMaxChunk);
+}
+
+int parts_of(int max_len, int chunk) { return (max_len + chunk - 1) / chunk; }
+
+struct Split {
+    int own_chunk, own_parts, shared_chunk, shared_parts;
+    size_t ml_bytes, bytes;
+};
+
+Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shared) {
+    Split s{};
+    s.own_chunk = chunk_of((int64_t)own.lists * c.heads, own.max_len);
+    s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
+    if (shared) {
+        s.shared_chunk = chunk_of((int64_t)shared->lists * c.heads, shared->max_len);
+        s.shared_parts = std::max(1, parts_of(shared->max_len, s.shared_chunk));
+    }
+    const size_t parts = s.own_parts + s.shared_parts;
+    if (parts > 1) {
+        const size_t rows = (size_t)own.lists * c.heads * c.group;
+        s.ml_bytes = (rows * parts * sizeof(f32x2_t) + 255) / 256 * 256;
+        s.bytes = s.ml_bytes + rows * parts * c.d * sizeof(float);
+    }
+    return s;
+}
+
+template <int TYPE, int D>
+int attn_launch(const AttnCall& a, hipStream_t st) {
+    if (a.shared_parts) {
+        const int64_t cols = (int64_t)a.own.lists * a.c.group;  // at most, per list
+        const int64_t mean = (cols + a.shared.lists - 1) / a.shared.lists;
+        const int nb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
+        AttnCall b = a;
+        b.tiles = (int)((mean + 16 * nb - 1) / (16 * nb));
+        const int64_t grid = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * b.tiles;
+        if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+        if (nb == 1) k_attn_shared<TYPE, D, 1><<<(unsigned)grid, kThreads, 0, st>>>(b);
+        else if (nb == 2) k_attn_shared<TYPE, D, 2><<<(unsigned)grid, kThreads, 0, st>>>(b);
+        else k_attn_shared<TYPE, D, 4><<<(unsigned)grid, kThreads, 0, st>>>(b);
+        if (int e = (int)hipGetLastError()) return e;
+    }
+    const int64_t grid = (int64_t)a.own.lists * a.c.heads * a.own_parts;
+    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+    k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);
+    if (int e = (int)hipGetLastError()) return e;
+    if (a.own_parts + a.shared_parts > 1) {
+        const int64_t rows = (int64_t)a.own.lists * a.c.heads * a.c.group;
+        const int64_t blocks = (rows * (D / 4) + kThreads - 1) / kThreads;
+        k_merge<D><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    }
     return (int)hipGetLastError();
 }
 
 }  // namespace
 
-size_t paged_attn_workspace(const PagedDims&, const PagedLists&, const PagedLists*) { return 0; }
+size_t paged_attn_workspace(const PagedDims& c, const PagedLists& own, const PagedLists* shared) {
+    return split_of(c, own, shared).bytes;
+}
 
 int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& own,
                       const PagedLists* shared, const int32_t* share, const uint16_t* q,
-                      int64_t q_stride, float* out, float* lse, void*, void* stream) {
-    auto run = [&](auto fn) {
-        return fn(c, pool, own, shared, share, q, q_stride, out, lse, stream);
-    };
+                      int64_t q_stride, float* out, float* lse, void* ws, void* stream) {
+    const Split s = split_of(c, own, shared);
+    AttnCall a{};
+    a.c = c;
+    a.pool = pool;
+    a.own = own;
+    if (shared) a.shared = *shared;
+    a.share = share;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.out = out;
+    a.lse = lse;
+    a.ml = static_cast<f32x2_t*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + s.ml_bytes);
+    a.own_chunk = s.own_chunk;
+    a.own_parts = s.own_parts;
+    a.shared_chunk = s.shared_chunk;
+    a.shared_parts = s.shared_parts;
+    hipStream_t st = (hipStream_t)stream;
     if (c.d == 128)
-        return c.type == kBf16   ? run(attn_launch<kBf16, 128>)
-               : c.type == kInt8 ? run(attn_launch<kInt8, 128>)
-                                 : run(attn_launch<kFp4, 128>);
-    return c.type == kBf16   ? run(attn_launch<kBf16, 64>)
-           : c.type == kInt8 ? run(attn_launch<kInt8, 64>)
-                             : run(attn_launch<kFp4, 64>);
+        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, st)
+               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, st)
+                                 : attn_launch<kFp4, 128>(a, st);
+    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, st)
+           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, st)
+                             : attn_launch<kFp4, 64>(a, st);
 }
 
 }  // namespace headkv
