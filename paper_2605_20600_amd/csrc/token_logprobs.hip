@@ -1,11 +1,24 @@
 // Log probabilities of given tokens, entropy, rank and the most likely
-// alternatives.  One block per row, with y = x / temperature and m its largest:
-//   log p_t = (y_t - m) - log S,  S = sum exp(y - m),
-//   entropy = log S - sum exp(y - m) (y - m) / S,
-// then the alternatives one after the other: the largest of the keys (value,
-// lowest index first) below the one before.
+// alternatives (formulas: headkv.h), in one pass over the logits.
+//
+// With y = (x - m) / temperature and m the largest logit,
+//   log p_t = y_t - log S,  S = sum exp(y),  entropy = log S - sum exp(y) y / S.
+// A block takes a segment of a row into registers (aligned 16-byte loads), finds
+// its maximum, then the sums relative to it and the number of logits above the
+// token's.  The segments of a row meet in the block that finishes last.
+//
+// Alternatives: a segment is 256 groups of 64 logits.  With T such that from
+// `top` to kMaxTop groups have their maximum at T or above, at least `top` values
+// are >= T and all of them belong to those groups, so few are left to rank
+// whatever the distribution.  T is found by bisection on order-preserving
+// integers, counting with ballots, from the least maximum of 32 sets of groups
+// on; where equal maxima leave no such T, it is the one below which too few are
+// left, and of the values equal to it the first in index order are taken.
+//
+// Bound by its bytes for many rows, by latency for few.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -14,105 +27,456 @@
 namespace headkv {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kCus = 256;
+constexpr int kSegment = 16384;  // logits of a block
+constexpr int kMaxTop = HEADKV_MAX_TOP;
+constexpr int kGroups = 256;
+constexpr int kGroupMost = kMaxTop * (kSegment / kGroups);  // logits of kMaxTop groups
+constexpr int kCandidates = kGroupMost + kMaxTop;           // above T, and equal to it
 
-template <typename T>
-__device__ __forceinline__ float value(T x);
-template <>
-__device__ __forceinline__ float value<uint16_t>(uint16_t x) {
-    return __uint_as_float((uint32_t)x << 16);
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
+// What a block knows of its segment: the maximum and the sum of 2^y, the sum of
+// 2^y y (y in log2 units) and the number of logits above the token's.
+struct Part {
+    uint64_t w[2];
+};
+
+// Words that a block of another XCD reads: written through, and read past, the
+// L2s, which are not coherent with each other.  (Fences instead, which write the
+// whole L2 back: 256 rows of 65536 logits 133 us, of 1024 threads a block 489.)
+__device__ __forceinline__ void publish(uint64_t* p, uint64_t v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <>
-__device__ __forceinline__ float value<float>(float x) {
-    return x;
+__device__ __forceinline__ uint64_t read(const uint64_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t pair(uint32_t a, uint32_t b) { return (uint64_t)b << 32 | a; }
+__device__ __forceinline__ uint32_t first_of(uint64_t v) { return (uint32_t)v; }
+__device__ __forceinline__ uint32_t second_of(uint64_t v) { return (uint32_t)(v >> 32); }
+
+// Order of logits: larger keys first; 0 is below every logit.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);  // -0 equals 0
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+    return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ uint64_t key_of(uint32_t order, int index) {
+    return (uint64_t)order << 32 | (uint32_t)~index;
 }
 
-// Order of logits and indices: larger keys first (value down, index up).
-__device__ __forceinline__ uint64_t key_of(float x, int index) {
-    uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);  // -0 equals 0
-    u = u >> 31 ? ~u : u | 0x80000000u;
-    return (uint64_t)u << 32 | (uint32_t)~index;
-}
-__device__ __forceinline__ float key_value(uint64_t k) {
-    uint32_t u = (uint32_t)(k >> 32);
-    u = u >> 31 ? u & 0x7fffffffu : ~u;
-    return __uint_as_float(u);
-}
+template <typename T, int kThreads>
+struct Logits {
+    static constexpr int N = 16 / sizeof(T);              // of a vector
+    static constexpr int NV = kSegment / kThreads / N;    // vectors of a thread
+    u32x4_t w[NV];
 
-template <typename V, typename F>
-__device__ V block_reduce(V v, F f) {
-    __shared__ V part[kThreads];
-    __syncthreads();
-    part[threadIdx.x] = v;
-    __syncthreads();
-    for (int n = kThreads / 2; n > 0; n /= 2) {
-        if ((int)threadIdx.x < n) part[threadIdx.x] = f(part[threadIdx.x], part[threadIdx.x + n]);
-        __syncthreads();
+    __device__ __forceinline__ float at(int v, int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[v][e]);
+        else return __uint_as_float(e & 1 ? w[v][e / 2] & 0xffff0000u : w[v][e / 2] << 16);
     }
-    return part[0];
-}
+    // Vector v of thread tid: elements j0 = (v kThreads + tid) N .. of the
+    // segment, which starts at the 16-byte boundary p; those outside [lo, hi)
+    // are -inf.
+    __device__ __forceinline__ void load(const T* p, int lo, int hi, int tid) {
+        constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int j0 = (v * kThreads + tid) * N;
+            w[v] = u32x4_t{kNone, kNone, kNone, kNone};
+            if (j0 >= lo && j0 + N <= hi) {
+                w[v] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + j0));
+            } else if (j0 + N > lo && j0 < hi) {  // an end of the row
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (j0 + e < lo || j0 + e >= hi) continue;
+                    const uint32_t x = p[j0 + e];
+                    if constexpr (sizeof(T) == 4) w[v][e] = x;
+                    else w[v][e / 2] = e & 1 ? (w[v][e / 2] & 0xffffu) | x << 16
+                                             : (w[v][e / 2] & 0xffff0000u) | x;
+                }
+            }
+        }
+    }
+};
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a) {
-    const int r = blockIdx.x;
-    const T* x = static_cast<const T*>(a.logits) + r * a.row_stride;
-    const int token = a.tokens[r];
-    const bool has = token >= 0 && token < a.vocab;
-    const float xt = has ? value(x[token]) : 0.f;
-    float m = -INFINITY;
-    bool ok = true;
-    for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-        const float v = value(x[i]);
-        m = fmaxf(m, v);
-        ok = ok && v < INFINITY;
-    }
-    m = block_reduce(m, [](float p, float q) { return fmaxf(p, q); });
-    ok = block_reduce((int)ok, [](int p, int q) { return p & q; });
-    const float m0 = m == -INFINITY ? 0.f : m;
-    float s = 0.f, t = 0.f;
-    int above = 0;
-    for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-        const float v = value(x[i]), y = (v - m0) * a.scale, e = expf(y);
-        s += e;
-        if (e > 0.f) t = fmaf(e, y, t);
-        above += v > xt;
-    }
-    auto add = [](auto p, auto q) { return p + q; };
-    s = block_reduce(s, add);
-    t = block_reduce(t, add);
-    above = block_reduce(above, add);
-    const float ls = logf(s);
-    auto logprob = [&](float v) { return v == -INFINITY ? v : (v - m0) * a.scale - ls; };
-    if (threadIdx.x == 0) {
-        a.logprob[r] = !ok ? NAN : has ? logprob(xt) : -INFINITY;
-        if (a.entropy) a.entropy[r] = !ok ? NAN : s > 0.f ? ls - t / s : 0.f;
-        if (a.rank) a.rank[r] = ok && has ? above : -1;
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, F f) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) v = f(v, __shfl_xor(v, o));
+    return v;
+}
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
+// The `top` largest of n keys in LDS, largest first, through out(rank, key): by
+// counting the larger ones while few, else one after the other.  Every thread
+// calls it; `scratch`: a key per wavefront.
+template <int kThreads, typename Out>
+__device__ __forceinline__ void select_top(const uint64_t* keys, int n, int top,
+                                           uint64_t* scratch, int tid, Out out) {
+    constexpr int kWaves = kThreads / 64;
+    if (n <= kThreads) {
+        if (tid < n) {
+            const uint64_t mine = keys[tid];
+            int rank = 0;
+            for (int i = 0; i < n; ++i) rank += keys[i] > mine;
+            if (rank < top) out(rank, mine);
+        }
+        return;
     }
     uint64_t last = ~0ull;
-    for (int j = 0; j < a.top; ++j) {
+    for (int j = 0; j < top; ++j) {
         uint64_t best = 0;
-        for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-            const uint64_t k = key_of(value(x[i]), i);
-            if (k < last && k > best) best = k;
+        for (int i = tid; i < n; i += kThreads)
+            if (keys[i] < last && keys[i] > best) best = keys[i];
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const uint64_t other = __shfl_xor((unsigned long long)best, o);
+            best = other > best ? other : best;
         }
-        best = block_reduce(best, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-        if (threadIdx.x == 0) {
-            a.top_logprob[(int64_t)r * a.top + j] = ok ? logprob(key_value(best)) : NAN;
-            a.top_index[(int64_t)r * a.top + j] = ok ? (int)~(uint32_t)best : -1;
-        }
+        __syncthreads();
+        if ((tid & 63) == 0) scratch[tid >> 6] = best;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) best = scratch[w] > best ? scratch[w] : best;
+        if (tid == 0) out(j, best);
         last = best;
     }
 }
 
+template <typename T, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int segments,
+                                                             Part* parts, uint64_t* part_keys,
+                                                             int* arrived) {
+    constexpr int N = Logits<T, kThreads>::N, NV = Logits<T, kThreads>::NV;
+    constexpr int kWaves = kThreads / 64;
+    constexpr int kPerGroup = kThreads / kGroups, kPerSet = kThreads / kMaxTop;  // threads
+    __shared__ float red[3][kWaves];
+    __shared__ int ired[2][kWaves];
+    __shared__ uint32_t maxima[kGroups], sets[kMaxTop];
+    __shared__ uint64_t keys[kCandidates];
+    __shared__ uint64_t scratch[kWaves], kept[kMaxTop];
+    __shared__ int count;
+    __shared__ uint32_t threshold[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r = blockIdx.x / segments, seg = blockIdx.x % segments;
+    const T* row = static_cast<const T*>(a.logits) + r * a.row_stride;
+    // element j of the row's segments is logit j - lead: vectors are aligned
+    const int lead = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
+    const int begin = seg * kSegment;
+    const int lo = max(lead - begin, 0), hi = min(a.vocab + lead - begin, kSegment);
+    Logits<T, kThreads> x;
+    x.load(row - lead + begin, lo, hi, tid);
+
+    const int token = a.tokens[r];
+    const bool has = token >= 0 && token < a.vocab;
+    float xt = 0.f;
+    if (has) {
+        const T w = row[token];
+        xt = sizeof(T) == 4 ? __uint_as_float((uint32_t)w) : __uint_as_float((uint32_t)w << 16);
+    }
+    const float k = a.scale * 1.4426950408889634f;  // to log2 units
+
+    float mine = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < N; ++e) mine = fmaxf(mine, x.at(v, e));
+    // of the thread, its group and its set; 0: no logits
+    uint32_t om = tid * N < hi ? order_of(mine) : 0u, group = om;
+#pragma unroll
+    for (int o = 1; o < kPerSet; o *= 2) {
+        if (o == kPerGroup) group = om;
+        om = max(om, (uint32_t)__shfl_xor((int)om, o));
+    }
+    if (tid % kPerGroup == 0) maxima[tid / kPerGroup] = group;
+    if (tid % kPerSet == 0) sets[tid / kPerSet] = om;
+    float m = wave_reduce(mine, fmaxf);
+    if (lane == 0) red[0][wave] = m;
+    if (tid == 0) count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, red[0][w]);
+
+    // y = (x - m) k; NaN and +inf in the segment make s NaN
+    float m0 = m == -INFINITY ? 0.f : m;
+    float s = 0.f, t = 0.f;
+    int above = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float xv = x.at(v, e), y = (xv - m0) * k, p = __builtin_amdgcn_exp2f(y);
+            s += p;
+            t = fmaf(p, fmaxf(y, -1e30f), t);
+            above += xv > xt;
+        }
+    s = wave_reduce(s, add);
+    t = wave_reduce(t, add);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) above += __shfl_xor(above, o);
+    if (lane == 0) {
+        red[1][wave] = s;
+        red[2][wave] = t;
+        ired[0][wave] = above;
+    }
+
+    int n = 0;  // candidates
+    if (a.top) {
+        if (wave == 0) {
+            uint32_t mx[kGroups / 64];
+#pragma unroll
+            for (int w = 0; w < kGroups / 64; ++w) mx[w] = maxima[64 * w + lane];
+            // every set has a group at or above the least of them
+            uint32_t low = sets[lane % kMaxTop];
+#pragma unroll
+            for (int o = 1; o < kMaxTop; o *= 2) low = min(low, (uint32_t)__shfl_xor((int)low, o));
+            low = __builtin_amdgcn_readfirstlane(a.top == 1 ? order_of(m) : low);
+            uint32_t high = order_of(m) + 1;  // groups at or above: >= top, < top
+            auto groups = [&](uint32_t at) {
+                int c = 0;
+#pragma unroll
+                for (int w = 0; w < kGroups / 64; ++w)
+                    c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mx[w] >= at));
+                return c;
+            };
+            bool few = low > 0 && groups(low) <= kMaxTop;
+            while (!few && high - low > 1) {
+                const uint32_t mid = low + (high - low) / 2;
+                const int c = groups(mid);
+                if (c < a.top) {
+                    high = mid;
+                } else {
+                    low = mid;
+                    few = c <= kMaxTop;
+                }
+            }
+            if (lane == 0) {
+                threshold[0] = few ? low - 1 : low;  // candidates are above this
+                threshold[1] = few ? 0 : low;        // and of these the first, if any
+            }
+        }
+        __syncthreads();
+        const uint32_t over = threshold[0], equal = threshold[1];
+        if (group > over) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const uint32_t o = order_of(x.at(v, e));
+                    const int j = (v * kThreads + tid) * N + e;
+                    if (o > over && j >= lo && j < hi) {
+                        const int at = atomicAdd(&count, 1);
+                        if (at < kGroupMost) keys[at] = key_of(o, begin + j - lead);
+                    }
+                }
+        }
+        __syncthreads();
+        n = min(count, kGroupMost);  // (more only among NaN)
+        if (equal > 0 && n < a.top) {  // the first values equal to T
+            int want = a.top - n;
+#pragma unroll 1
+            for (int v = 0; v < NV && want > 0; ++v) {
+                u32x4_t w = x.w[0];
+#pragma unroll
+                for (int i = 1; i < NV; ++i) w = v == i ? x.w[i] : w;
+                const int j0 = (v * kThreads + tid) * N;
+                uint32_t ties = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float f = sizeof(T) == 4 ? __uint_as_float(w[e % 4])
+                                    : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+                    ties |= (uint32_t)(order_of(f) == equal && j0 + e >= lo && j0 + e < hi) << e;
+                }
+                int sum = __builtin_popcount(ties);
+#pragma unroll
+                for (int o = 1; o < 64; o *= 2) {
+                    const int up = __shfl_up(sum, o);
+                    if (lane >= o) sum += up;
+                }
+                if (lane == 63) ired[1][wave] = sum;
+                __syncthreads();
+                int before = sum - __builtin_popcount(ties), total = 0;
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) {
+                    if (i < wave) before += ired[1][i];
+                    total += ired[1][i];
+                }
+                for (int e = 0; e < N; ++e) {
+                    if (!(ties >> e & 1)) continue;
+                    if (before < want) keys[n + before] = key_of(equal, begin + j0 + e - lead);
+                    ++before;
+                }
+                total = min(total, want);
+                n += total;
+                want -= total;
+                __syncthreads();
+            }
+        }
+    }
+    __syncthreads();
+    s = t = 0.f;
+    above = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        s += red[1][w];
+        t += red[2][w];
+        above += ired[0][w];
+    }
+
+    if (segments > 1) {
+        // the segment's part, then the last block of the row goes on with all
+        const int64_t at = (int64_t)r * segments + seg;
+        if (a.top) {
+            uint64_t* mine_keys = part_keys + at * a.top;
+            if (tid < a.top && tid >= n) publish(mine_keys + tid, 0);  // fewer logits than asked
+            select_top<kThreads>(keys, n, a.top, scratch, tid, [&](int i, uint64_t key) {
+                if (i < a.top) publish(mine_keys + i, key);
+            });
+        }
+        if (tid == 0) {
+            publish(parts[at].w, pair(__float_as_uint(m), __float_as_uint(s)));
+            publish(parts[at].w + 1, pair(__float_as_uint(t), (uint32_t)above));
+        }
+        // every published word has left before the block counts as arrived
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) {
+            const int got = __hip_atomic_fetch_add(arrived + r, 1, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+            count = got == segments - 1;
+            if (count)  // as it was found
+                __hip_atomic_store(arrived + r, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!count) return;
+        const Part* p = parts + (int64_t)r * segments;
+        // each wavefront for itself, 64 segments at a time
+        m = -INFINITY;
+        for (int i = lane; i < segments; i += 64) m = fmaxf(m, __uint_as_float(first_of(read(p[i].w))));
+        m = wave_reduce(m, fmaxf);
+        m0 = m == -INFINITY ? 0.f : m;
+        s = t = 0.f;
+        above = 0;
+        for (int i = lane; i < segments; i += 64) {
+            const uint64_t u = read(p[i].w), v = read(p[i].w + 1);
+            const float pm = __uint_as_float(first_of(u)), ps = __uint_as_float(second_of(u));
+            const float pt = __uint_as_float(first_of(v));
+            above += (int)second_of(v);
+            // nothing but -inf: ps is 0, or NaN
+            const float shift = pm == -INFINITY ? 0.f : (pm - m0) * k;
+            const float f = __builtin_amdgcn_exp2f(shift);
+            s = fmaf(f, ps, s);
+            t = fmaf(f, fmaf(fmaxf(shift, -1e30f), ps, pt), t);
+        }
+        s = wave_reduce(s, add);
+        t = wave_reduce(t, add);
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) above += __shfl_xor(above, o);
+        if (a.top) {
+            n = 0;
+            const uint64_t* in = part_keys + (int64_t)r * segments * a.top;
+            const int all = segments * a.top;
+            __syncthreads();
+            if (all <= kCandidates) {
+                for (int i = tid; i < all; i += kThreads) keys[i] = read(in + i);
+                n = all;
+            } else {  // too many for LDS at once: segment after segment into the best so far
+                for (int i = 0; i < segments; ++i) {
+                    if (tid < a.top) keys[n + tid] = read(in + (int64_t)i * a.top + tid);
+                    n += a.top;
+                    __syncthreads();
+                    if (n + a.top > kCandidates || i == segments - 1) {
+                        if (tid < a.top) kept[tid] = 0;
+                        __syncthreads();
+                        select_top<kThreads>(keys, n, a.top, scratch, tid, [&](int j, uint64_t key) {
+                            if (key) kept[j] = key;
+                        });
+                        __syncthreads();
+                        if (tid < a.top) keys[tid] = kept[tid];
+                        n = a.top;
+                        __syncthreads();
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+
+    const bool ok = s == s && m < INFINITY;
+    const float log_s = __builtin_amdgcn_logf(s);  // log2
+    constexpr float kLn2 = 0.6931471805599453f;
+    auto logprob = [&](float v) {
+        return v == -INFINITY ? v : (v - m0) * a.scale - log_s * kLn2;
+    };
+    if (tid == 0) {
+        a.logprob[r] = !ok ? NAN : has ? logprob(xt) : -INFINITY;
+        if (a.entropy) a.entropy[r] = !ok ? NAN : s > 0.f ? (log_s - t / s) * kLn2 : 0.f;
+        if (a.rank) a.rank[r] = ok && has ? above : -1;
+    }
+    if (a.top && !ok) {
+        if (tid < a.top) {
+            a.top_logprob[(int64_t)r * a.top + tid] = NAN;
+            a.top_index[(int64_t)r * a.top + tid] = -1;
+        }
+    } else if (a.top) {
+        select_top<kThreads>(keys, n, a.top, scratch, tid, [&](int i, uint64_t key) {
+            const int64_t o = (int64_t)r * a.top + i;
+            a.top_logprob[o] = logprob(value_of((uint32_t)(key >> 32)));
+            a.top_index[o] = (int)~(uint32_t)key;
+        });
+    }
+}
+
+// Segments of a row that starts up to `lead` logits into a vector.
+int segments_of(int vocab, int lead) { return (vocab + lead + kSegment - 1) / kSegment; }
+
+struct ScorePlan {
+    size_t parts, keys, bytes;  // offsets behind the counters, and the total
+};
+
+ScorePlan plan_of(int rows, int vocab, int top) {
+    const size_t segments = segments_of(vocab, 7);
+    ScorePlan p{};
+    if (segments > 1) {
+        auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+        p.parts = up((size_t)rows * sizeof(int));
+        p.keys = p.parts + up(rows * segments * sizeof(Part));
+        p.bytes = p.keys + up(rows * segments * top * sizeof(uint64_t));
+    }
+    return p;
+}
+
 }  // namespace
 
-size_t logprobs_workspace(int, int, int) { return 0; }
+size_t logprobs_workspace(int rows, int vocab, int top) { return plan_of(rows, vocab, top).bytes; }
 
-int launch_token_logprobs(const ScoreArgs& a, int logits_type, void*, void* stream) {
+int launch_token_logprobs(const ScoreArgs& a, int logits_type, void* ws, void* stream) {
+    const ScorePlan p = plan_of(a.rows, a.vocab, a.top);
+    const int size = logits_type == HEADKV_LOGITS_BF16 ? 2 : 4;
+    const bool even = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
+                      (a.rows == 1 || a.row_stride * size % 16 == 0);
+    const int segments = segments_of(a.vocab, even ? 0 : 16 / size - 1);
+    const int64_t grid = (int64_t)a.rows * segments;
+    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+    char* w = static_cast<char*>(ws);
+    auto* parts = reinterpret_cast<Part*>(w + p.parts);
+    auto* keys = reinterpret_cast<uint64_t*>(w + p.keys);
+    auto* arrived = reinterpret_cast<int*>(w);
+    hipStream_t st = (hipStream_t)stream;
+    auto run = [&](auto kernel, int threads) {
+        kernel<<<(unsigned)grid, threads, 0, st>>>(a, segments, parts, keys, arrived);
+    };
+    // Few blocks: as many threads as possible, for latency (8 rows of 16384: 7.2 us,
+    // with 256 threads 17.8).  Many: small blocks, whose phases overlap (18816 rows
+    // of 16384 fp32: 430 us, with 256 threads 212).
+    const bool small = grid <= 2 * kCus;
     if (logits_type == HEADKV_LOGITS_BF16)
-        k_token_logprobs<uint16_t><<<a.rows, kThreads, 0, (hipStream_t)stream>>>(a);
+        small ? run(k_token_logprobs<uint16_t, 1024>, 1024) : run(k_token_logprobs<uint16_t, 256>, 256);
     else
-        k_token_logprobs<float><<<a.rows, kThreads, 0, (hipStream_t)stream>>>(a);
+        small ? run(k_token_logprobs<uint32_t, 1024>, 1024) : run(k_token_logprobs<uint32_t, 256>, 256);
     return (int)hipGetLastError();
 }
 

@@ -142,6 +142,14 @@ def test_row_offsets_past_32_bits():
     _check(x, t, 3, x_dev=view)
 
 
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32))
+def test_a_very_long_row(dtype):
+    x, t = _logits(2, (1 << 21) + 5, dtype, 8)
+    x[1, :1 << 20] = -math.inf
+    t[1] = (1 << 21) + 4
+    _check(x, t, 32)
+
+
 def test_many_rows_and_repeats_are_the_same():
     x, t = _logits(5000, 2000, torch.bfloat16, 5)
     _check(x, t, 2)
