@@ -7,7 +7,7 @@
 // its maximum, then the sums relative to it and the number of logits above the
 // token's.  The segments of a row meet in the block that finishes last.
 //
-// Alternatives: a segment is 256 groups of 64 logits.  With T such that from
+// Alternatives: a segment is 256 groups of up to 64 logits.  With T such that from
 // `top` to kMaxTop groups have their maximum at T or above, at least `top` values
 // are >= T and all of them belong to those groups, so few are left to rank
 // whatever the distribution.  T is found by bisection on order-preserving
@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -28,11 +29,9 @@ namespace headkv {
 namespace {
 
 constexpr int kCus = 256;
-constexpr int kSegment = 16384;  // logits of a block
+constexpr int kMaxSegment = 16384;  // logits of a block
 constexpr int kMaxTop = HEADKV_MAX_TOP;
 constexpr int kGroups = 256;
-constexpr int kGroupMost = kMaxTop * (kSegment / kGroups);  // logits of kMaxTop groups
-constexpr int kCandidates = kGroupMost + kMaxTop;           // above T, and equal to it
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
@@ -67,10 +66,10 @@ __device__ __forceinline__ uint64_t key_of(uint32_t order, int index) {
     return (uint64_t)order << 32 | (uint32_t)~index;
 }
 
-template <typename T, int kThreads>
+template <typename T, int kThreads, int kEpt>
 struct Logits {
-    static constexpr int N = 16 / sizeof(T);              // of a vector
-    static constexpr int NV = kSegment / kThreads / N;    // vectors of a thread
+    static constexpr int N = 16 / sizeof(T);  // of a vector
+    static constexpr int NV = kEpt / N;       // vectors of a thread
     u32x4_t w[NV];
 
     __device__ __forceinline__ float at(int v, int e) const {
@@ -101,6 +100,12 @@ struct Logits {
         }
     }
 };
+
+// m k, 0 for an empty maximum
+__device__ __forceinline__ float product(float m, float k) {
+#pragma clang fp contract(off)
+    return m == -INFINITY ? 0.f : m * k;
+}
 
 template <typename F>
 __device__ __forceinline__ float wave_reduce(float v, F f) {
@@ -146,11 +151,14 @@ __device__ __forceinline__ void select_top(const uint64_t* keys, int n, int top,
     }
 }
 
-template <typename T, int kThreads>
+template <typename T, int kThreads, int kEpt>
 __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int segments,
                                                              Part* parts, uint64_t* part_keys,
                                                              int* arrived) {
-    constexpr int N = Logits<T, kThreads>::N, NV = Logits<T, kThreads>::NV;
+    using Values = Logits<T, kThreads, kEpt>;
+    constexpr int N = Values::N, NV = Values::NV, kSegment = kThreads * kEpt;
+    constexpr int kGroupMost = kMaxTop * (kSegment / kGroups);  // logits of kMaxTop groups
+    constexpr int kCandidates = kGroupMost + kMaxTop > 512 ? kGroupMost + kMaxTop : 512;
     constexpr int kWaves = kThreads / 64;
     constexpr int kPerGroup = kThreads / kGroups, kPerSet = kThreads / kMaxTop;  // threads
     __shared__ float red[3][kWaves];
@@ -167,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
     const int lead = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
     const int begin = seg * kSegment;
     const int lo = max(lead - begin, 0), hi = min(a.vocab + lead - begin, kSegment);
-    Logits<T, kThreads> x;
+    Values x;
     x.load(row - lead + begin, lo, hi, tid);
 
     const int token = a.tokens[r];
@@ -200,19 +208,27 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, red[0][w]);
 
-    // y = (x - m) k; NaN and +inf in the segment make s NaN
-    float m0 = m == -INFINITY ? 0.f : m;
+    // y = x k - mk with mk = m k rounded once for all, which shifts every y, and so
+    // log S, by the same; where m k is not finite, (x - m) k.  NaN and +inf in the
+    // segment make s NaN.
+    float mk = product(m, k);
     float s = 0.f, t = 0.f;
     int above = 0;
+    auto sums = [&](auto far) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float xv = x.at(v, e), y = (xv - m0) * k, p = __builtin_amdgcn_exp2f(y);
-            s += p;
-            t = fmaf(p, fmaxf(y, -1e30f), t);
-            above += xv > xt;
-        }
+            for (int e = 0; e < N; ++e) {
+                const float xv = x.at(v, e);
+                const float y = decltype(far)::value ? (xv - m) * k : fmaf(xv, k, -mk);
+                const float p = __builtin_amdgcn_exp2f(y);
+                s += p;
+                t = fmaf(p, fmaxf(y, -1e30f), t);
+                above += xv > xt;
+            }
+    };
+    if (__builtin_amdgcn_readfirstlane(fabsf(mk) < INFINITY)) sums(std::false_type{});
+    else sums(std::true_type{});
     s = wave_reduce(s, add);
     t = wave_reduce(t, add);
 #pragma unroll
@@ -261,20 +277,21 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
         __syncthreads();
         const uint32_t over = threshold[0], equal = threshold[1];
         if (group > over) {
+            const float least = value_of(max(over + 1, order_of(-INFINITY)));
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const uint32_t o = order_of(x.at(v, e));
+                    if (!(x.at(v, e) >= least)) continue;
                     const int j = (v * kThreads + tid) * N + e;
-                    if (o > over && j >= lo && j < hi) {
-                        const int at = atomicAdd(&count, 1);
-                        if (at < kGroupMost) keys[at] = key_of(o, begin + j - lead);
-                    }
+                    if (j < lo || j >= hi) continue;
+                    const int at = atomicAdd(&count, 1);
+                    if (at < kGroupMost)
+                        keys[at] = key_of(order_of(x.at(v, e)), begin + j - lead);
                 }
         }
         __syncthreads();
-        n = min(count, kGroupMost);  // (more only among NaN)
+        n = min(count, kGroupMost);
         if (equal > 0 && n < a.top) {  // the first values equal to T
             int want = a.top - n;
 #pragma unroll 1
@@ -357,7 +374,7 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
         m = -INFINITY;
         for (int i = lane; i < segments; i += 64) m = fmaxf(m, __uint_as_float(first_of(read(p[i].w))));
         m = wave_reduce(m, fmaxf);
-        m0 = m == -INFINITY ? 0.f : m;
+        mk = product(m, k);
         s = t = 0.f;
         above = 0;
         for (int i = lane; i < segments; i += 64) {
@@ -366,7 +383,9 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
             const float pt = __uint_as_float(first_of(v));
             above += (int)second_of(v);
             // nothing but -inf: ps is 0, or NaN
-            const float shift = pm == -INFINITY ? 0.f : (pm - m0) * k;
+            float shift = product(pm, k) - mk;
+            if (!(fabsf(mk) < INFINITY)) shift = (pm - m) * k;
+            if (pm == -INFINITY) shift = 0.f;
             const float f = __builtin_amdgcn_exp2f(shift);
             s = fmaf(f, ps, s);
             t = fmaf(f, fmaf(fmaxf(shift, -1e30f), ps, pt), t);
@@ -406,10 +425,12 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
     }
 
     const bool ok = s == s && m < INFINITY;
-    const float log_s = __builtin_amdgcn_logf(s);  // log2
     constexpr float kLn2 = 0.6931471805599453f;
+    const float log_s = __builtin_amdgcn_logf(s);  // log2
+    // without the shift by what m k was rounded
+    const float log_true = fabsf(mk) < INFINITY && m > -INFINITY ? log_s - fmaf(m, k, -mk) : log_s;
     auto logprob = [&](float v) {
-        return v == -INFINITY ? v : (v - m0) * a.scale - log_s * kLn2;
+        return v == -INFINITY ? v : (v - m) * a.scale - log_true * kLn2;
     };
     if (tid == 0) {
         a.logprob[r] = !ok ? NAN : has ? logprob(xt) : -INFINITY;
@@ -431,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
 }
 
 // Segments of a row that starts up to `lead` logits into a vector.
-int segments_of(int vocab, int lead) { return (vocab + lead + kSegment - 1) / kSegment; }
+int segments_of(int vocab, int lead) { return (vocab + lead + kMaxSegment - 1) / kMaxSegment; }
 
 struct ScorePlan {
     size_t parts, keys, bytes;  // offsets behind the counters, and the total
@@ -458,7 +479,8 @@ int launch_token_logprobs(const ScoreArgs& a, int logits_type, void* ws, void* s
     const int size = logits_type == HEADKV_LOGITS_BF16 ? 2 : 4;
     const bool even = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
                       (a.rows == 1 || a.row_stride * size % 16 == 0);
-    const int segments = segments_of(a.vocab, even ? 0 : 16 / size - 1);
+    const int lead = even ? 0 : 16 / size - 1;
+    const int segments = segments_of(a.vocab, lead);
     const int64_t grid = (int64_t)a.rows * segments;
     if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
     char* w = static_cast<char*>(ws);
@@ -469,14 +491,19 @@ int launch_token_logprobs(const ScoreArgs& a, int logits_type, void* ws, void* s
     auto run = [&](auto kernel, int threads) {
         kernel<<<(unsigned)grid, threads, 0, st>>>(a, segments, parts, keys, arrived);
     };
-    // Few blocks: as many threads as possible, for latency (8 rows of 16384: 7.2 us,
-    // with 256 threads 17.8).  Many: small blocks, whose phases overlap (18816 rows
-    // of 16384 fp32: 430 us, with 256 threads 212).
-    const bool small = grid <= 2 * kCus;
-    if (logits_type == HEADKV_LOGITS_BF16)
-        small ? run(k_token_logprobs<uint16_t, 1024>, 1024) : run(k_token_logprobs<uint16_t, 256>, 256);
-    else
-        small ? run(k_token_logprobs<uint32_t, 1024>, 1024) : run(k_token_logprobs<uint32_t, 256>, 256);
+    // The smallest segment that holds a row, so that no lane is idle; few blocks
+    // have as many threads as possible, for latency.
+    const int least = a.vocab + lead;
+    auto pick = [&](auto type) {
+        using T = decltype(type);
+        if (least <= 2048) run(k_token_logprobs<T, 256, 8>, 256);
+        else if (least <= 4096) run(k_token_logprobs<T, 256, 16>, 256);
+        else if (least <= 8192) run(k_token_logprobs<T, 512, 16>, 512);
+        else if (grid <= 2 * kCus) run(k_token_logprobs<T, 1024, 16>, 1024);
+        else run(k_token_logprobs<T, 512, 32>, 512);
+    };
+    if (logits_type == HEADKV_LOGITS_BF16) pick(uint16_t{});
+    else pick(uint32_t{});
     return (int)hipGetLastError();
 }
 
