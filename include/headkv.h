@@ -362,6 +362,10 @@ typedef struct headkv_paged_lists {
                              NULL: none */
     const int32_t* first; /* [lists][kv_heads], device, or NULL: tokens before it
                              are not attended (a sliding window) */
+    const int32_t* order; /* [lists * kv_heads], device, or NULL: the numbers list
+                             * kv_heads + head, each once, in the order in which
+                             headkv_paged_attn starts them; longest first is
+                             fastest */
     int32_t lists;        /* >= 1 */
     int32_t max_pages;    /* pages of a table row, >= 1 */
     int32_t extra;        /* >= 0, added to every len: a decoder that appends one
@@ -415,8 +419,8 @@ headkv_status headkv_paged_attn_plan(const headkv_paged_config* cfg,
  * of exponentials, or NULL.  A query with nothing to attend gets out = 0 and
  * lse = -infinity.  fp32 sums, and weights of 24 bits.
  * workspace: device, 256-byte aligned, headkv_paged_attn_plan bytes, zeroed by
- * the caller before its first use (every launch leaves its counters zero);
- * calls that overlap need one each. */
+ * the caller before its first use; any calls may use it one after the other
+ * (every launch leaves its counters zero), calls that overlap need one each. */
 headkv_status headkv_paged_attn(const headkv_paged_config* cfg, const void* pool,
                                 const headkv_paged_lists* own, const headkv_paged_lists* shared,
                                 const int32_t* share, const uint16_t* q, int64_t q_stride,
@@ -447,7 +451,7 @@ headkv_status headkv_logprobs_plan(int32_t rows, int32_t vocab, int32_t top,
  * -inf and the entropy 0.  A row with a NaN or +inf gets NaN in every fp32 and
  * -1 in every int32 result.  temperature > 0.  Sums in fp32.
  * workspace: device, 256-byte aligned, headkv_logprobs_plan bytes, zeroed by the
- * caller before its first use (every launch leaves its counters zero); calls
+ * caller before its first use; any calls may use it one after the other, calls
  * that overlap need one each. */
 headkv_status headkv_token_logprobs(const void* logits, int32_t logits_type, int32_t rows,
                                     int32_t vocab, int64_t row_stride, const int32_t* tokens,

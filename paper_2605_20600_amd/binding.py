@@ -94,7 +94,7 @@ class PagedConfig(ctypes.Structure):
 class PagedListsArg(ctypes.Structure):
     _fields_ = [
         ("pages", ctypes.c_void_p), ("len", ctypes.c_void_p), ("first", ctypes.c_void_p),
-        ("lists", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("extra", ctypes.c_int32),
+        ("order", ctypes.c_void_p), ("lists", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("extra", ctypes.c_int32),
         ("max_len", ctypes.c_int32),
     ]
 

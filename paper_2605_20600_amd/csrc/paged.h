@@ -32,8 +32,17 @@ struct PagedLists {
     const int32_t* pages;
     const int32_t* len;
     const int32_t* first;
+    const int32_t* order;
     int lists, max_pages, extra, max_len;
 };
+
+// Counters at the start of a workspace, zero between launches.  Their number does
+// not depend on a call's sizes, so calls of any sizes can share a workspace: what
+// lies behind them, which no launch expects to find in any state, never comes to
+// lie on them.  A call with more than so many lists or rows runs in several
+// launches.
+constexpr int kCounters = 1 << 16;
+constexpr size_t kCounterBytes = kCounters * sizeof(int32_t);
 
 struct PagedRows {  // bf16 rows of the caller: element strides
     int64_t list, token, head;

@@ -63,9 +63,10 @@ headkv_status make_lists(const PagedDims& c, const headkv_paged_lists* l, bool p
     if (l->max_pages > (1 << 22)) return unsupported("max_pages > 2^22");
     if (l->extra < 0 || l->max_len < 0) return bad("extra and max_len must be >= 0");
     if (pointers && !l->pages) return bad("pages is NULL");
-    if (!aligned(l->pages, 4) || !aligned(l->len, 4) || !aligned(l->first, 4))
-        return bad("pages / len / first not aligned");
-    *out = PagedLists{l->pages, l->len, l->first, l->lists, l->max_pages, l->extra,
+    if (!aligned(l->pages, 4) || !aligned(l->len, 4) || !aligned(l->first, 4) ||
+        !aligned(l->order, 4))
+        return bad("pages / len / first / order not aligned");
+    *out = PagedLists{l->pages, l->len, l->first, l->order, l->lists, l->max_pages, l->extra,
                       (int)std::min<int64_t>(l->max_len, (int64_t)l->max_pages * c.ptok)};
     return HEADKV_OK;
 }

@@ -22,8 +22,9 @@
 // bits are exact in bf16; an INT8 scale multiplies its token's score or weight,
 // an FP4 scale enters with the conversion.
 // The wavefronts of a block split its tokens and meet in LDS; blocks split a list
-// into chunks, whose parts (maximum, sum, unnormalised output) k_merge joins in
-// chunk order.
+// into chunks, whose parts (maximum, sum, unnormalised output) the block of a row's
+// own list that finishes last joins in their order, those of the row's prefix,
+// which ran before, among them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -58,8 +59,12 @@ struct AttnCall {
     int64_t q_stride;
     float* out;
     float* lse;
-    f32x2_t* ml;   // [batch][query heads][parts] maximum (log2) and sum
-    float* part;   // [batch][query heads][parts][d]
+    int* arrived;  // [kCounters] chunks that are done, of the launch's lists in their order
+    f32x2_t* ml;   // [batch][query heads][own parts] maximum (log2) and sum
+    float* part;   // [batch][query heads][own parts][d]
+    f32x2_t* shared_ml;  // [batch][query heads][shared parts]
+    float* shared_part;  // [batch][query heads][shared parts][d]
+    int list0, lists;                // own lists of this launch, in their order
     int own_chunk, own_parts;        // tokens of a chunk, chunks at most
     int shared_chunk, shared_parts;  // (0: no shared lists)
     int tiles;                       // column tiles in the grid, per shared list
@@ -184,6 +189,8 @@ __device__ __forceinline__ void int8_pack(uint32_t in, uint32_t* o) {
     o[0] = pack_high(a, b);
     o[1] = pack_high(c, d);
 }
+// The conversion takes its scale from the exponent; that of byte 255 gives NaN.
+__device__ __forceinline__ float fp4_exponent(uint32_t e) { return __uint_as_float(e << 23); }
 template <int SEL>
 __device__ __forceinline__ uint32_t fp4_pack(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
@@ -200,7 +207,7 @@ __device__ __forceinline__ bf16x8_t key_operand(const Tile<TYPE, D>& t, int u, i
         int8_pack(t.k[u][s >> 1][2 * (s & 1)], o);
         int8_pack(t.k[u][s >> 1][2 * (s & 1) + 1], o + 2);
     } else {
-        const float e = fp4_power(t.ke[u]);
+        const float e = fp4_exponent(t.ke[u]);
         const uint32_t w = t.k[u][0][s];
         o[0] = fp4_pack<0>(w, e);
         o[1] = fp4_pack<1>(w, e);
@@ -229,7 +236,7 @@ __device__ __forceinline__ void value_operands(const Tile<TYPE, D>& t, int j, bf
         for (int h = 0; h < 2; ++h) {
             const uint32_t w = whole(t.ve[j][h]);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) e[4 * h + n] = fp4_power(w >> (8 * n) & 0xffu);
+            for (int n = 0; n < 4; ++n) e[4 * h + n] = fp4_exponent(w >> (8 * n) & 0xffu);
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -251,6 +258,15 @@ __device__ __forceinline__ void value_operands(const Tile<TYPE, D>& t, int j, bf
             a[2 * x + 1] = operand(hi);
         }
     }
+}
+
+// f over the four lanes of a column (lanes i, i + 16, i + 32, i + 48).
+template <typename F>
+__device__ __forceinline__ float over_quarters(float v, F f) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
 // State of a wavefront: column i = lane % 16 of each of its NB tiles.
@@ -279,16 +295,14 @@ struct Wave {
         constexpr float kScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0));
         f32x4_t st[NB][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int s = 0; s < KS; ++s) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) st[b][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                if (s % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            for (int u = 0; u < 2; ++u) {
                 const bf16x8_t a = key_operand<TYPE, D>(t, u, s);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
-                    st[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[b][s], st[b][u], 0, 0, 0);
+                    st[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        a, q[b][s], s == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : st[b][u], 0, 0, 0);
             }
         }
         float ks[8], vs[8];  // INT8: scales of the lane's tokens
@@ -317,8 +331,7 @@ struct Wave {
             }
             float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])),
                              fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            mx = over_quarters(mx, [](float x, float y) { return fmaxf(x, y); });
             if (__builtin_amdgcn_ballot_w64(mx > m[b]) != 0) {
                 const float now = fmaxf(mx, m[b]);
                 const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[b] - now);
@@ -349,20 +362,58 @@ struct Wave {
 #pragma unroll
             for (int e = 0; e < 3; ++e) p[b][e] = operand(w[e]);
         }
+        // four products that do not wait for each other, at a time
+        constexpr int J = VX * NB >= 4 ? 1 : 4 / (VX * NB);
+#pragma unroll
+        for (int j0 = 0; j0 < Tile<TYPE, D>::VN; j0 += J) {
+            bf16x8_t a[J][VX];
+#pragma unroll
+            for (int j = 0; j < J; ++j) value_operands<TYPE, D>(t, j0 + j, a[j]);
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int x = 0; x < VX; ++x)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) {
+                            f32x4_t& o = acc[b][VX * (j0 + j) + x];
+                            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j][x], p[b][e], o, 0, 0, 0);
+                        }
+        }
+    }
+
+    // What the lane has of its column in tile b, dims in order (row: d floats).
+    __device__ __forceinline__ void to_row(int b, int quarter, float* row) const {
 #pragma unroll
         for (int j = 0; j < Tile<TYPE, D>::VN; ++j) {
-            __builtin_amdgcn_sched_barrier(0);  // one load's conversions at a time: registers
-            bf16x8_t a[VX];
-            value_operands<TYPE, D>(t, j, a);
+            const f32x4_t* a = acc[b] + VX * j;
+            if constexpr (VX == 1) {
+                *reinterpret_cast<f32x4_t*>(row + 16 * j + 4 * quarter) = a[0];
+            } else if constexpr (VX == 2) {
+                f32x4_t* p = reinterpret_cast<f32x4_t*>(row + 32 * j + 8 * quarter);
+                p[0] = f32x4_t{a[0][0], a[1][0], a[0][1], a[1][1]};
+                p[1] = f32x4_t{a[0][2], a[1][2], a[0][3], a[1][3]};
+            } else {
+                f32x4_t* p = reinterpret_cast<f32x4_t*>(row + 64 * j + 16 * quarter);
 #pragma unroll
-            for (int x = 0; x < VX; ++x)
-#pragma unroll
-                for (int e = 0; e < 3; ++e)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        acc[b][VX * j + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            a[x], p[b][e], acc[b][VX * j + x], 0, 0, 0);
+                for (int r = 0; r < 4; ++r) p[r] = f32x4_t{a[0][r], a[1][r], a[2][r], a[3][r]};
+            }
         }
+    }
+
+    // The tokens of the step at token `at` that lie in [first, end).
+    __device__ __forceinline__ void step_at(Tile<TYPE, D>& t, int at, int first, int end, int lane) {
+        const bool partial = at < first || at + kStep > end;
+        uint32_t seen = 0xffu;
+        if (partial) {
+            // of the lane's eight tokens
+            const int tk = at + 8 * (lane >> 4);
+            const int lo = min(max(first - tk, 0), 8), hi = min(max(end - tk, 0), 8);
+            seen = 0xffu >> (8 - hi) & 0xffu << lo;
+            t.blank(seen);
+        }
+        step(t, partial, seen);
     }
 
     // Tokens [t0, t1) of a list, t0 a multiple of 32, those before `first` not
@@ -387,17 +438,7 @@ struct Wave {
             todo &= todo - 1;
             const int after = todo ? __builtin_ctzll(todo) : -1;
             if (after >= 0) fetch(next, after);
-            const int at = t0 + (wave + kWaves * n) * kStep;
-            const bool partial = at < first || at + kStep > t1;
-            uint32_t seen = 0xffu;
-            if (partial) {
-                // of the lane's eight tokens those of [first, t1)
-                const int tk = at + 8 * (lane >> 4);
-                const int lo = min(max(first - tk, 0), 8), hi = min(max(t1 - tk, 0), 8);
-                seen = 0xffu >> (8 - hi) & 0xffu << lo;
-                now.blank(seen);
-            }
-            step(now, partial, seen);
+            step_at(now, t0 + (wave + kWaves * n) * kStep, first, t1, lane);
             if (after < 0) break;
             now = next;
             n = after;
@@ -411,35 +452,17 @@ template <int TYPE, int D, int NB, typename Store>
 __device__ __forceinline__ void join_waves(Wave<TYPE, D, NB>& w, float* lds, int wave, int lane,
                                            Store store) {
     constexpr int ROW = D + 4;  // floats of a column in LDS: 16-byte writes of 16 columns do not meet
-    constexpr int VX = Wave<TYPE, D, NB>::VX, VN = Tile<TYPE, D>::VN;
     float* o = lds;                              // [wave][16][ROW]
     float* ms = lds + kWaves * 16 * ROW;         // [wave][16] maximum, then sum
     const int i = lane & 15, quarter = lane >> 4;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        float sum = w.sum[b];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
+        const float sum = over_quarters(w.sum[b], [](float x, float y) { return x + y; });
         if (lane < 16) {
             ms[wave * 16 + lane] = w.m[b];
             ms[(kWaves + wave) * 16 + lane] = sum;
         }
-        float* row = o + (wave * 16 + i) * ROW;
-#pragma unroll
-        for (int j = 0; j < VN; ++j) {
-            const f32x4_t* a = w.acc[b] + VX * j;
-            if constexpr (VX == 1) {
-                *reinterpret_cast<f32x4_t*>(row + 16 * j + 4 * quarter) = a[0];
-            } else if constexpr (VX == 2) {
-                f32x4_t* p = reinterpret_cast<f32x4_t*>(row + 32 * j + 8 * quarter);
-                p[0] = f32x4_t{a[0][0], a[1][0], a[0][1], a[1][1]};
-                p[1] = f32x4_t{a[0][2], a[1][2], a[0][3], a[1][3]};
-            } else {
-                f32x4_t* p = reinterpret_cast<f32x4_t*>(row + 64 * j + 16 * quarter);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = f32x4_t{a[0][r], a[1][r], a[2][r], a[3][r]};
-            }
-        }
+        w.to_row(b, quarter, o + (wave * 16 + i) * ROW);
         __syncthreads();
         const int tid = wave * 64 + lane;
 #pragma unroll
@@ -489,43 +512,131 @@ __device__ __forceinline__ Span span_of(const PagedLists& p, int ptok, int64_t l
     return s;
 }
 
-// A row's own list: one block per (row, kv head, chunk).
+// Parts that a block of another XCD reads in the same launch: written through,
+// and read past, the L2s.
+__device__ __forceinline__ void publish(void* p, uint32_t lo, uint32_t hi) {
+    __hip_atomic_store(static_cast<uint64_t*>(p), (uint64_t)hi << 32 | lo, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2_t published(const void* p) {
+    return __builtin_bit_cast(f32x2_t, __hip_atomic_load(static_cast<const uint64_t*>(p),
+                                                         __ATOMIC_RELAXED,
+                                                         __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// The sum of parts, one after the other.
+struct Sum {
+    f32x4_t v{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, s = 0.f;
+    __device__ __forceinline__ void add(f32x4_t pv, float pm, float ps) {
+        const float now = fmaxf(m, pm);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+        const float g = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - now);
+        v = f * v + g * pv;
+        s = f * s + g * ps;
+        m = now;
+    }
+    // n parts, the loads of eight at a time in flight
+    template <typename V, typename M>
+    __device__ __forceinline__ void add_parts(int n, V value, M ml) {
+        for (int i0 = 0; i0 < n; i0 += 8) {
+            f32x4_t v[8];
+            f32x2_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = min(i0 + i, n - 1);
+                v[i] = value(at);
+                w[i] = ml(at);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < n) add(v[i], w[i][0], w[i][1]);
+        }
+    }
+};
+
+// A row's own list: one block per (row, kv head, chunk), the first also for an
+// empty list.
 template <int TYPE, int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_own(AttnCall a) {
     __shared__ __align__(16) float lds[lds_floats<D>()];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lists = a.own.lists * a.c.heads;
-    const int lh = blockIdx.x % lists, chunk = blockIdx.x / lists;
+    __shared__ int last;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = a.c.group;
+    const int rank = blockIdx.x % a.lists, chunk = blockIdx.x / a.lists;
+    const int at = a.list0 + rank;
+    const int lh = a.own.order ? min(max(a.own.order[at], 0), a.own.lists * a.c.heads - 1) : at;
     const int b = lh / a.c.heads, h = lh % a.c.heads;
     const Span s = span_of(a.own, a.c.ptok, lh, a.own_chunk);
-    const bool whole = a.own_parts == 1 && a.shared_parts == 0;  // nothing to merge
-    if (chunk >= s.chunks && !(whole && s.chunks == 0)) return;
+    const int chunks = max(s.chunks, 1);
+    if (chunk >= chunks) return;
     const int t0 = s.start + chunk * a.own_chunk, t1 = min(s.len, t0 + a.own_chunk);
-    const int hq = a.c.heads * a.c.group;
-    const int64_t row0 = (int64_t)b * hq + h * a.c.group;
+    const int64_t row0 = (int64_t)lh * group;
 
     Wave<TYPE, D, 1> w;
     w.clear();
-    const int g = lane & 15;
-    const uint16_t* q = a.q + b * a.q_stride + (h * a.c.group + min(g, a.c.group - 1)) * D;
+    const uint16_t* q = a.q + b * a.q_stride + (h * group + min(lane & 15, group - 1)) * D;
 #pragma unroll
     for (int k = 0; k < D / 32; ++k)
         w.q[0][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
-    if (t0 < t1)
+    if (s.chunks > 0)
         w.run(a.c, a.pool, a.own.pages + (int64_t)lh * a.own.max_pages, t0, t1, s.first, wave, lane);
-    const int parts = a.own_parts + a.shared_parts;
+
+    int prefix = 0;  // parts of the row's shared list
+    if (a.shared_parts) {
+        const int l = a.share[b];
+        if (l >= 0 && l < a.shared.lists)
+            prefix = span_of(a.shared, a.c.ptok, (int64_t)l * a.c.heads + h, a.shared_chunk).chunks;
+    }
+    // the row's prefix joins what there is of its own tokens
+    auto output = [&](Sum& all, int col, int d) {
+        const int64_t row = row0 + col, at = row * a.shared_parts;
+        all.add_parts(
+            prefix,
+            [&](int j) { return *reinterpret_cast<const f32x4_t*>(a.shared_part + (at + j) * D + d); },
+            [&](int j) { return a.shared_ml[at + j]; });
+        write_out(a, row, d, D, all.v, all.m, all.s);
+    };
     join_waves(w, lds, wave, lane, [&](int col, int d, f32x4_t v, float m, float sum) {
-        if (col >= a.c.group) return;
-        const int64_t row = row0 + col;
-        if (whole) {
-            write_out(a, row, d, D, v, m, sum);
+        if (col >= group) return;
+        if (chunks == 1) {
+            Sum all{v, m, sum};
+            output(all, col, d);
         } else {
-            const int64_t slot = row * parts + chunk;
-            *reinterpret_cast<f32x4_t*>(a.part + slot * D + d) = v;
-            if (d == 0) a.ml[slot] = f32x2_t{m, sum};
+            const int64_t slot = (row0 + col) * a.own_parts + chunk;
+            float* p = a.part + slot * D + d;
+            publish(p, __float_as_uint(v[0]), __float_as_uint(v[1]));
+            publish(p + 2, __float_as_uint(v[2]), __float_as_uint(v[3]));
+            if (d == 0) publish(a.ml + slot, __float_as_uint(m), __float_as_uint(sum));
         }
     });
+    if (chunks == 1) return;
+    // every published word has left before the block counts as arrived
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+        last = __hip_atomic_fetch_add(a.arrived + rank, 1, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT) == chunks - 1;
+        if (last)
+            __hip_atomic_store(a.arrived + rank, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+    for (int i = tid; i < group * (D / 4); i += kThreads) {
+        const int col = i / (D / 4), d = i % (D / 4) * 4;
+        const int64_t slot = (row0 + col) * a.own_parts;
+        Sum all;
+        all.add_parts(
+            chunks,
+            [&](int j) {
+                const float* p = a.part + (slot + j) * D + d;
+                const f32x2_t x = published(p), y = published(p + 2);
+                return f32x4_t{x[0], x[1], y[0], y[1]};
+            },
+            [&](int j) { return published(a.ml + slot + j); });
+        output(all, col, d);
+    }
 }
 
 // A shared list: one block per (list, kv head, chunk) and column tile, which
@@ -547,7 +658,7 @@ void k_attn_shared(AttnCall a) {
     const Span s = span_of(a.shared, a.c.ptok, lh, a.shared_chunk);
     if (chunk >= s.chunks) return;
     const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
-    const int hq = a.c.heads * group, parts = a.own_parts + a.shared_parts;
+    const int hq = a.c.heads * group;
 
     for (int tile = tile0;; tile += a.tiles) {
         // the members that the tile's columns belong to: ranks [rank0, rank1)
@@ -588,52 +699,30 @@ void k_attn_shared(AttnCall a) {
             const int col = c0 + n;
             const int64_t row =
                 (int64_t)row_of[col / group - rank0] * hq + h * group + col % group;
-            const int64_t slot = row * parts + a.own_parts + chunk;
-            *reinterpret_cast<f32x4_t*>(a.part + slot * D + d) = v;
-            if (d == 0) a.ml[slot] = f32x2_t{m, sum};
+            const int64_t slot = row * a.shared_parts + chunk;
+            *reinterpret_cast<f32x4_t*>(a.shared_part + slot * D + d) = v;
+            if (d == 0) a.shared_ml[slot] = f32x2_t{m, sum};
         });
     }
-}
-
-// Joins the parts of every query: D / 4 lanes each, in the order of the parts.
-template <int D>
-__global__ __launch_bounds__(kThreads) void k_merge(AttnCall a) {
-    constexpr int LANES = D / 4;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
-    const int hq = a.c.heads * a.c.group;
-    if (row >= (int64_t)a.own.lists * hq) return;
-    const int d = threadIdx.x % LANES * 4, b = (int)(row / hq), h = (int)(row % hq) / a.c.group;
-    const int own = span_of(a.own, a.c.ptok, (int64_t)b * a.c.heads + h, a.own_chunk).chunks;
-    int shared = 0;
-    if (a.shared_parts) {
-        const int l = a.share[b];
-        if (l >= 0 && l < a.shared.lists)
-            shared = span_of(a.shared, a.c.ptok, (int64_t)l * a.c.heads + h, a.shared_chunk).chunks;
-    }
-    const int64_t slot0 = row * (a.own_parts + a.shared_parts);
-    float m = -INFINITY;
-    auto slot = [&](int i) { return slot0 + (i < own ? i : a.own_parts + i - own); };
-    for (int i = 0; i < own + shared; ++i) m = fmaxf(m, a.ml[slot(i)][0]);
-    f32x4_t v{0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int i = 0; i < own + shared; ++i) {
-        const f32x2_t ml = a.ml[slot(i)];
-        const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
-        sum += f * ml[1];
-        v += f * *reinterpret_cast<const f32x4_t*>(a.part + slot(i) * D + d);
-    }
-    write_out(a, row, d, D, v, m, sum);
 }
 
 // ------------------------------------------------------------------- launch
 constexpr int kCus = 256;
 
-// Tokens of a chunk, so that `items` lists of up to max_len tokens give the chip
-// about two blocks per CU; at least two steps of a block.
-int chunk_of(int64_t items, int max_len) {
+// Tokens of a chunk of `items` lists of up to max_len tokens.
+// Own lists: about two blocks per CU for few lists, else short enough that blocks
+// that are done early find others (256 lists of 1500-16384 tokens, fp4: 512 tokens
+// 67 us, 1024 61, 2048 69; 32 lists of 98-2480 tokens: 256 tokens 8.5 us, 512 11;
+// 128, a step of a wavefront, 15).
+int own_chunk_of(int64_t items, int max_len) {
     const int64_t want = std::max<int64_t>(1, 2 * kCus / items);
-    int64_t chunk = (max_len + want - 1) / want;
-    chunk = (chunk + kUnit - 1) / kUnit * kUnit;
+    const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
+    return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), 8 * kUnit);
+}
+// Shared lists, whose blocks are one to a CU at many columns: as many as CUs.
+int shared_chunk_of(int64_t items, int max_len) {
+    const int64_t want = std::max<int64_t>(1, kCus / items);
+    const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
     return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), kMaxChunk);
 }
 
@@ -641,51 +730,56 @@ int parts_of(int max_len, int chunk) { return (max_len + chunk - 1) / chunk; }
 
 struct Split {
     int own_chunk, own_parts, shared_chunk, shared_parts;
-    size_t ml_bytes, bytes;
+    // column tiles of a wavefront, and of the grid for a shared list: as many as
+    // its share of all columns takes; a list with more has its blocks go round
+    int nb, tiles;
+    // offsets, and the total
+    size_t ml, part, shared_ml, shared_part, bytes;
 };
 
 Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shared) {
     Split s{};
-    s.own_chunk = chunk_of((int64_t)own.lists * c.heads, own.max_len);
+    const size_t lists = (size_t)own.lists * c.heads, rows = lists * c.group;
+    s.own_chunk = own_chunk_of(lists, own.max_len);
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
     if (shared) {
-        s.shared_chunk = chunk_of((int64_t)shared->lists * c.heads, shared->max_len);
+        const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
+        s.nb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
+        s.tiles = (int)((mean + 16 * s.nb - 1) / (16 * s.nb));
+        s.shared_chunk = shared_chunk_of((int64_t)shared->lists * c.heads * s.tiles, shared->max_len);
         s.shared_parts = std::max(1, parts_of(shared->max_len, s.shared_chunk));
     }
-    const size_t parts = s.own_parts + s.shared_parts;
-    if (parts > 1) {
-        const size_t rows = (size_t)own.lists * c.heads * c.group;
-        s.ml_bytes = (rows * parts * sizeof(f32x2_t) + 255) / 256 * 256;
-        s.bytes = s.ml_bytes + rows * parts * c.d * sizeof(float);
-    }
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    const size_t own_places = s.own_parts > 1 ? rows * s.own_parts : 0;
+    s.ml = kCounterBytes;
+    s.part = s.ml + up(own_places * sizeof(f32x2_t));
+    s.shared_ml = s.part + up(own_places * c.d * sizeof(float));
+    s.shared_part = s.shared_ml + up(rows * s.shared_parts * sizeof(f32x2_t));
+    s.bytes = s.shared_part + rows * s.shared_parts * c.d * sizeof(float);
     return s;
 }
 
 template <int TYPE, int D>
-int attn_launch(const AttnCall& a, hipStream_t st) {
+int attn_launch(const AttnCall& a, int nb, hipStream_t st) {
     if (a.shared_parts) {
-        const int64_t cols = (int64_t)a.own.lists * a.c.group;  // at most, per list
-        const int64_t mean = (cols + a.shared.lists - 1) / a.shared.lists;
-        const int nb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
-        AttnCall b = a;
-        b.tiles = (int)((mean + 16 * nb - 1) / (16 * nb));
-        const int64_t grid = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * b.tiles;
+        const int64_t grid = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * a.tiles;
         if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
-        if (nb == 1) k_attn_shared<TYPE, D, 1><<<(unsigned)grid, kThreads, 0, st>>>(b);
-        else if (nb == 2) k_attn_shared<TYPE, D, 2><<<(unsigned)grid, kThreads, 0, st>>>(b);
-        else k_attn_shared<TYPE, D, 4><<<(unsigned)grid, kThreads, 0, st>>>(b);
+        if (nb == 1) k_attn_shared<TYPE, D, 1><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        else if (nb == 2) k_attn_shared<TYPE, D, 2><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        else k_attn_shared<TYPE, D, 4><<<(unsigned)grid, kThreads, 0, st>>>(a);
         if (int e = (int)hipGetLastError()) return e;
     }
-    const int64_t grid = (int64_t)a.own.lists * a.c.heads * a.own_parts;
-    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
-    k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);
-    if (int e = (int)hipGetLastError()) return e;
-    if (a.own_parts + a.shared_parts > 1) {
-        const int64_t rows = (int64_t)a.own.lists * a.c.heads * a.c.group;
-        const int64_t blocks = (rows * (D / 4) + kThreads - 1) / kThreads;
-        k_merge<D><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    const int lists = a.own.lists * a.c.heads;
+    for (int l0 = 0; l0 < lists; l0 += kCounters) {
+        AttnCall b = a;
+        b.list0 = l0;
+        b.lists = std::min(lists - l0, kCounters);
+        const int64_t grid = (int64_t)b.lists * a.own_parts;
+        if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+        k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(b);
+        if (int e = (int)hipGetLastError()) return e;
     }
-    return (int)hipGetLastError();
+    return 0;
 }
 
 }  // namespace
@@ -708,20 +802,25 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
     a.q_stride = q_stride;
     a.out = out;
     a.lse = lse;
-    a.ml = static_cast<f32x2_t*>(ws);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + s.ml_bytes);
+    char* w = static_cast<char*>(ws);
+    a.arrived = reinterpret_cast<int*>(w);
+    a.ml = reinterpret_cast<f32x2_t*>(w + s.ml);
+    a.part = reinterpret_cast<float*>(w + s.part);
+    a.shared_ml = reinterpret_cast<f32x2_t*>(w + s.shared_ml);
+    a.shared_part = reinterpret_cast<float*>(w + s.shared_part);
     a.own_chunk = s.own_chunk;
     a.own_parts = s.own_parts;
     a.shared_chunk = s.shared_chunk;
     a.shared_parts = s.shared_parts;
+    a.tiles = s.tiles;
     hipStream_t st = (hipStream_t)stream;
     if (c.d == 128)
-        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, st)
-               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, st)
-                                 : attn_launch<kFp4, 128>(a, st);
-    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, st)
-           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, st)
-                             : attn_launch<kFp4, 64>(a, st);
+        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, s.nb, st)
+               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, s.nb, st)
+                                 : attn_launch<kFp4, 128>(a, s.nb, st);
+    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, s.nb, st)
+           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, s.nb, st)
+                             : attn_launch<kFp4, 64>(a, s.nb, st);
 }
 
 }  // namespace headkv

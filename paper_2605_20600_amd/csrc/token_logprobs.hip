@@ -455,17 +455,17 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
 int segments_of(int vocab, int lead) { return (vocab + lead + kMaxSegment - 1) / kMaxSegment; }
 
 struct ScorePlan {
-    size_t parts, keys, bytes;  // offsets behind the counters, and the total
+    size_t parts, keys, bytes;  // offsets, and the total
 };
 
 ScorePlan plan_of(int rows, int vocab, int top) {
     const size_t segments = segments_of(vocab, 7);
     ScorePlan p{};
     if (segments > 1) {
-        auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-        p.parts = up((size_t)rows * sizeof(int));
-        p.keys = p.parts + up(rows * segments * sizeof(Part));
-        p.bytes = p.keys + up(rows * segments * top * sizeof(uint64_t));
+        const size_t n = std::min(rows, kCounters) * segments;
+        p.parts = kCounterBytes;
+        p.keys = p.parts + n * sizeof(Part);
+        p.bytes = p.keys + n * top * sizeof(uint64_t);
     }
     return p;
 }
@@ -474,37 +474,52 @@ ScorePlan plan_of(int rows, int vocab, int top) {
 
 size_t logprobs_workspace(int rows, int vocab, int top) { return plan_of(rows, vocab, top).bytes; }
 
-int launch_token_logprobs(const ScoreArgs& a, int logits_type, void* ws, void* stream) {
-    const ScorePlan p = plan_of(a.rows, a.vocab, a.top);
+int launch_token_logprobs(const ScoreArgs& all, int logits_type, void* ws, void* stream) {
+    const ScorePlan p = plan_of(all.rows, all.vocab, all.top);
     const int size = logits_type == HEADKV_LOGITS_BF16 ? 2 : 4;
-    const bool even = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
-                      (a.rows == 1 || a.row_stride * size % 16 == 0);
+    const bool even = reinterpret_cast<uintptr_t>(all.logits) % 16 == 0 &&
+                      (all.rows == 1 || all.row_stride * size % 16 == 0);
     const int lead = even ? 0 : 16 / size - 1;
-    const int segments = segments_of(a.vocab, lead);
-    const int64_t grid = (int64_t)a.rows * segments;
-    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+    const int segments = segments_of(all.vocab, lead);
     char* w = static_cast<char*>(ws);
     auto* parts = reinterpret_cast<Part*>(w + p.parts);
     auto* keys = reinterpret_cast<uint64_t*>(w + p.keys);
     auto* arrived = reinterpret_cast<int*>(w);
     hipStream_t st = (hipStream_t)stream;
-    auto run = [&](auto kernel, int threads) {
-        kernel<<<(unsigned)grid, threads, 0, st>>>(a, segments, parts, keys, arrived);
-    };
-    // The smallest segment that holds a row, so that no lane is idle; few blocks
-    // have as many threads as possible, for latency.
-    const int least = a.vocab + lead;
-    auto pick = [&](auto type) {
-        using T = decltype(type);
-        if (least <= 2048) run(k_token_logprobs<T, 256, 8>, 256);
-        else if (least <= 4096) run(k_token_logprobs<T, 256, 16>, 256);
-        else if (least <= 8192) run(k_token_logprobs<T, 512, 16>, 512);
-        else if (grid <= 2 * kCus) run(k_token_logprobs<T, 1024, 16>, 1024);
-        else run(k_token_logprobs<T, 512, 32>, 512);
-    };
-    if (logits_type == HEADKV_LOGITS_BF16) pick(uint16_t{});
-    else pick(uint32_t{});
-    return (int)hipGetLastError();
+    // (grids of at most kCounters rows of 2^10 segments, or 2^24 rows of one)
+    const int most = segments > 1 ? kCounters : 1 << 24;
+    for (int r0 = 0; r0 < all.rows; r0 += most) {
+        ScoreArgs a = all;
+        a.rows = std::min(all.rows - r0, most);
+        a.logits = static_cast<const char*>(all.logits) + r0 * all.row_stride * size;
+        a.tokens += r0;
+        a.logprob += r0;
+        if (a.entropy) a.entropy += r0;
+        if (a.rank) a.rank += r0;
+        if (a.top) {
+            a.top_logprob += (int64_t)r0 * a.top;
+            a.top_index += (int64_t)r0 * a.top;
+        }
+        const int64_t grid = (int64_t)a.rows * segments;
+        auto run = [&](auto kernel, int threads) {
+            kernel<<<(unsigned)grid, threads, 0, st>>>(a, segments, parts, keys, arrived);
+        };
+        // The smallest segment that holds a row, so that no lane is idle; few blocks
+        // have as many threads as possible, for latency.
+        const int least = a.vocab + lead;
+        auto pick = [&](auto type) {
+            using T = decltype(type);
+            if (least <= 2048) run(k_token_logprobs<T, 256, 8>, 256);
+            else if (least <= 4096) run(k_token_logprobs<T, 256, 16>, 256);
+            else if (least <= 8192) run(k_token_logprobs<T, 512, 16>, 512);
+            else if (grid <= 2 * kCus) run(k_token_logprobs<T, 1024, 16>, 1024);
+            else run(k_token_logprobs<T, 512, 32>, 512);
+        };
+        if (logits_type == HEADKV_LOGITS_BF16) pick(uint16_t{});
+        else pick(uint32_t{});
+        if (int e = (int)hipGetLastError()) return e;
+    }
+    return 0;
 }
 
 }  // namespace headkv

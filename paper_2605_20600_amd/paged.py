@@ -37,7 +37,14 @@ class Lists:
         self.pages = _device_int32(pages, (n, heads, per), "pages")
         self.length = None if length is None else _device_int32(length, (n, heads), "length")
         self.first = None if first is None else _device_int32(first, (n, heads), "first")
-        self.arg = B.PagedListsArg(_ptr(pages), _ptr(length), _ptr(first), n, per, extra, max_len)
+        # longest first: a list that starts late makes the others wait for it (64 x 32
+        # lists of 64 to 1024 tokens: 50 us in the order of their numbers, 38 so)
+        self.order = None
+        if length is not None and n * heads > 1:
+            tokens = length if first is None else length - first
+            self.order = torch.argsort(tokens.view(-1), descending=True).to(torch.int32)
+        self.arg = B.PagedListsArg(_ptr(pages), _ptr(length), _ptr(first), _ptr(self.order), n, per,
+                                   extra, max_len)
         self.kv_heads = heads
 
     @property
@@ -120,7 +127,7 @@ class PagedKV:
             for l in (own, shared):
                 a = None
                 if l is not None:
-                    a = B.PagedListsArg(None, None, None, l.arg.lists, l.arg.max_pages, 0,
+                    a = B.PagedListsArg(None, None, None, None, l.arg.lists, l.arg.max_pages, 0,
                                         l.arg.max_pages * self.cfg.page_tokens)
                 most.append(a)
             need = B.headkv_paged_attn_plan(self.cfg, *most)
@@ -156,6 +163,7 @@ class PagedKV:
         return out
 
 
+_LOGITS = {torch.bfloat16: B.HEADKV_LOGITS_BF16, torch.float32: B.HEADKV_LOGITS_F32}
 _score_ws: Dict[Tuple[int, int], torch.Tensor] = {}  # per device and stream
 
 
@@ -165,17 +173,22 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
     logits [rows][vocab] bf16 or float32 with rows of any stride: "logprob",
     "entropy" and "rank" per row, and with top > 0 "top_logprob" and "top_index"
     [rows][top]."""
-    types = {torch.bfloat16: B.HEADKV_LOGITS_BF16, torch.float32: B.HEADKV_LOGITS_F32}
-    if logits.dim() != 2 or logits.dtype not in types or logits.stride(1) != 1:
+    if top < 0:
+        raise ValueError("top must be >= 0")
+    if logits.dim() != 2 or logits.dtype not in _LOGITS or logits.stride(1) != 1:
         raise ValueError("logits must be bf16 or float32 [rows][vocab] with contiguous rows")
     rows, vocab = logits.shape
     _device_int32(tokens, (rows,), "tokens")
     dev = logits.device
-    f32 = lambda *s: torch.empty(s, dtype=torch.float32, device=dev)
-    i32 = lambda *s: torch.empty(s, dtype=torch.int32, device=dev)
-    res = {"logprob": f32(rows), "entropy": f32(rows), "rank": i32(rows)}
+    # one allocation for all results: an empty tensor costs 1.6 us of the 4 that the
+    # call itself takes, a view of one 0.4 to 1.3
+    many = rows * top
+    buf = torch.empty(3 * rows + 2 * many, dtype=torch.int32, device=dev)
+    rank, index, floats = buf.split_with_sizes((rows, many, 2 * rows + many))
+    logprob, entropy, best = floats.view(torch.float32).split_with_sizes((rows, rows, many))
+    res = {"logprob": logprob, "entropy": entropy, "rank": rank}
     if top > 0:
-        res["top_logprob"], res["top_index"] = f32(rows, top), i32(rows, top)
+        res["top_logprob"], res["top_index"] = best.view(rows, top), index.view(rows, top)
     stream = Session.stream()
     need = B.headkv_logprobs_plan(rows, vocab, top)
     ws = None
@@ -184,11 +197,10 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
         ws = _score_ws.get(key)
         if ws is None or ws.numel() < need:
             ws = _score_ws[key] = torch.zeros(need, dtype=torch.uint8, device=dev)
-    B.headkv_token_logprobs(logits.data_ptr(), types[logits.dtype], rows, vocab,
+    B.headkv_token_logprobs(logits.data_ptr(), _LOGITS[logits.dtype], rows, vocab,
                             logits.stride(0) if rows > 1 else vocab, tokens.data_ptr(),
-                            temperature, top,
-                            res["logprob"].data_ptr(), res["entropy"].data_ptr(),
-                            res["rank"].data_ptr(), _ptr(res.get("top_logprob")),
-                            _ptr(res.get("top_index")), _ptr(ws), 0 if ws is None else ws.numel(),
-                            stream)
+                            temperature, top, logprob.data_ptr(), entropy.data_ptr(),
+                            rank.data_ptr(), best.data_ptr() if top > 0 else None,
+                            index.data_ptr() if top > 0 else None, _ptr(ws),
+                            0 if ws is None else ws.numel(), stream)
     return res

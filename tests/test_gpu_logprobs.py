@@ -16,9 +16,10 @@ from paper_2605_20600_amd.paged import token_logprobs
 pytestmark = pytest.mark.gpu
 
 
-def _check(x, tokens, top, temperature=1.0, x_dev=None):
-    got = token_logprobs(x.cuda() if x_dev is None else x_dev, tokens.cuda(), top=top,
-                         temperature=temperature)
+def _check(x, tokens, top, temperature=1.0, x_dev=None, got=None):
+    if got is None:
+        got = token_logprobs(x.cuda() if x_dev is None else x_dev, tokens.cuda(), top=top,
+                             temperature=temperature)
     got = {k: v.cpu() for k, v in got.items()}
     rows, vocab = x.shape
     raw = x.double()
@@ -159,6 +160,26 @@ def test_many_rows_and_repeats_are_the_same():
         again = token_logprobs(xd, td, top=2)
         for k in first:
             assert torch.equal(first[k], again[k])
+
+
+def test_calls_of_any_sizes_share_the_workspace():
+    # what a call leaves behind its counters may not be taken for another's counters
+    for rows, vocab, top in ((256, 65536, 32), (1500, 17000, 1), (3, 300000, 32), (6000, 16500, 0),
+                             (40, 70000, 20), (256, 65536, 32)):
+        x, t = _logits(rows, vocab, torch.bfloat16, rows)
+        _check(x, t, top)
+
+
+def test_more_rows_than_counters():
+    g = torch.Generator().manual_seed(9)
+    rows, vocab = 65536 + 300, 16500
+    one = (3 * torch.randn((1, vocab), generator=g)).to(torch.bfloat16)
+    x = one.expand(rows, vocab).contiguous()
+    x[:, 0] = torch.linspace(0, 20, rows).to(torch.bfloat16)
+    t = torch.randint(0, vocab, (rows,), generator=g).to(torch.int32)
+    got = token_logprobs(x.cuda(), t.cuda(), top=2)
+    some = torch.tensor([0, 1, 65535, 65536, 65537, rows - 1])
+    _check(x[some], t[some], 2, got={k: v[some.cuda()] for k, v in got.items()})
 
 
 def test_on_another_stream_and_in_a_graph():

@@ -410,6 +410,49 @@ def test_a_nan_stays_in_its_head(kind):
         assert torch.equal(got[0, 0], clean[0, 0]) and torch.equal(got[0, 2], clean[0, 2])
 
 
+def test_calls_of_any_sizes_share_the_workspace():
+    setups = [Setup("int8", 128, 2, torch.randint(1, n, (rows, 2), generator=torch.Generator()
+                                                  .manual_seed(rows)).tolist(), group=group, seed=rows)
+              for rows, n, group in ((3, 3000, 1), (200, 40, 2), (2, 5000, 16), (60, 1200, 1))]
+    ws = max((s.c._workspace(s.lists[0], None) for s in setups), key=lambda t: t.numel())
+    for s in setups * 2:
+        s.c._ws = ws
+        s.check()
+
+
+def test_more_lists_than_counters():
+    # 660 x 100 lists of up to two tokens, and eight rows with longer ones that are cut
+    batch, heads, d, ptok, most = 660, 100, 64, 32, 1300
+    rows = [0, 1, 97, 500, 654, 655, 656, 659]
+    g = torch.Generator().manual_seed(5)
+    lens = torch.randint(0, 3, (batch, heads), generator=g).to(torch.int32)
+    lens[rows, ::3] = torch.randint(1100, most, (len(rows), 34), generator=g).to(torch.int32)
+    per = -(-most // ptok)
+    table = torch.full((batch, heads, per), -1, dtype=torch.int32)
+    need = (lens + ptok - 1) // ptok
+    there = torch.arange(per) < need[..., None]
+    n = int(there.sum())
+    table[there] = torch.randperm(n, generator=g).to(torch.int32)
+    c = _cache("fp4", d, heads, n, page_tokens=ptok)
+    k, v = (_values((len(rows), most, heads, d), i, 0.7) for i in range(2))
+    c.write(c.lists(table[rows].contiguous().cuda(), None, max_len=0), k.cuda(), v.cuda())
+    rest = [b for b in range(batch) if b not in rows]
+    kr, vr = (_values((len(rest), 2, heads, d), 3 + i, 0.7) for i in range(2))
+    c.write(c.lists(table[rest].contiguous().cuda(), None, max_len=0), kr.cuda(), vr.cuda())
+    q = _values((batch, heads, d), 7, 0.3)
+    for order in (True, False):
+        l = c.lists(table.cuda(), lens.cuda(), max_len=most)
+        if not order:
+            l.arg.order = None
+        got = c.attn(l, q.cuda()).cpu().double()
+        for i, b in enumerate(rows + rest[::50]):
+            kb, vb = (k[i], v[i]) if b in rows else (kr[rest.index(b)], vr[rest.index(b)])
+            kb, vb = _held(kb, "fp4"), _held(vb, "fp4")
+            seen = torch.arange(kb.shape[0])[None] < lens[b][:, None]
+            ref, _, tol, _ = _reference(q[b].double().view(heads, 1, d), kb, vb, seen)
+            assert float((got[b] - ref[:, 0]).abs().max()) <= tol, b
+
+
 def test_on_another_stream():
     s = Setup("int8", 128, 4, LENS, seed=41)
     want = s.c.attn(s.lists[0], s.q.cuda()).clone()

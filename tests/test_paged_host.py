@@ -18,7 +18,7 @@ def _cfg(**kw):
 
 
 def _lists(**kw):
-    base = dict(pages=FAKE, len=FAKE, first=None, lists=3, max_pages=5, extra=0, max_len=300)
+    base = dict(pages=FAKE, len=FAKE, first=None, order=None, lists=3, max_pages=5, extra=0, max_len=300)
     return B.PagedListsArg(**{**base, **kw})
 
 
@@ -54,7 +54,7 @@ def test_plan():
 
 @pytest.mark.parametrize("kw,status", [
     (dict(pages=None), I), (dict(pages=FAKE + 2), I), (dict(len=FAKE + 1), I), (dict(lists=0), I),
-    (dict(first=FAKE + 2), I), (dict(max_pages=0), I), (dict(extra=-1), I), (dict(max_len=-1), I),
+    (dict(first=FAKE + 2), I), (dict(order=FAKE + 2), I), (dict(max_pages=0), I), (dict(extra=-1), I), (dict(max_len=-1), I),
     (dict(lists=1 << 24), U), (dict(max_pages=(1 << 22) + 1), U)])
 def test_lists(kw, status):
     l = _lists(**kw)
