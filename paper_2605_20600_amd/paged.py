@@ -45,7 +45,7 @@ class Lists:
             self.order = torch.argsort(tokens.view(-1), descending=True).to(torch.int32)
         self.arg = B.PagedListsArg(_ptr(pages), _ptr(length), _ptr(first), _ptr(self.order), n, per,
                                    extra, max_len)
-        self.kv_heads = heads
+        self.n, self.kv_heads = n, heads
 
     @property
     def extra(self) -> int:
@@ -65,6 +65,7 @@ class PagedKV:
         """kv_type: "bf16", "int8" or "fp4"; group: query heads per kv head."""
         self.cfg = B.PagedConfig(B.KV_TYPES[kv_type], head_dim, kv_heads, group, page_tokens,
                                  num_pages)
+        self.kv_heads, self.head_dim, self.heads = kv_heads, head_dim, kv_heads * group
         self.page_bytes, pool_bytes = B.headkv_paged_plan(self.cfg)
         self.device = device
         self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=device)
@@ -80,17 +81,30 @@ class PagedKV:
         return got
 
     def _rows(self, k, v, lists: Lists) -> Tuple[int, Tuple[int, int, int]]:
-        shape = (lists.arg.lists, k.shape[1], self.cfg.kv_heads, self.cfg.head_dim)
+        shape, ks = k.shape, k.stride()
+        if v.stride() != ks or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 \
+                or v.shape != shape or len(shape) != 4 or ks[3] != 1:
+            ks = self._check_rows(k, v)
+        n, tokens, heads, d = shape
+        if n != lists.n or heads != self.kv_heads or d != self.head_dim:
+            raise ValueError(f"k and v must be [{lists.n}][tokens][{self.kv_heads}]"
+                             f"[{self.head_dim}], got {tuple(shape)}")
+        if n == 1 or tokens == 1 or heads == 1:
+            # the stride of a dimension of one is never used, and may be anything
+            return tokens, (ks[0] if n > 1 else 0, ks[1] if tokens > 1 else 0,
+                            ks[2] if heads > 1 else 0)
+        return tokens, ks[:3]
+
+    @staticmethod
+    def _check_rows(k, v):
         for t in (k, v):
-            if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or t.stride(3) != 1:
-                raise ValueError(f"k and v must be bf16 [lists][tokens][kv_heads][head_dim] = "
-                                 f"{shape} with contiguous rows, got {t.dtype} {tuple(t.shape)}")
-        # the stride of a dimension of one is never used, and may be anything
-        ks, vs = (tuple(st if n > 1 else 0 for st, n in zip(t.stride(), shape[:3]))
-                  for t in (k, v))
-        if ks != vs:
-            raise ValueError("k and v must have the same strides")
-        return shape[1], ks
+            if t.dim() != 4 or t.dtype != torch.bfloat16 or t.shape != k.shape or t.stride(3) != 1:
+                raise ValueError("k and v must be bf16 [lists][tokens][kv_heads][head_dim] with "
+                                 f"contiguous rows, got {t.dtype} {tuple(t.shape)}")
+        for i in range(3):
+            if k.shape[i] > 1 and k.stride(i) != v.stride(i):
+                raise ValueError("k and v must have the same strides")
+        return k.stride()
 
     def write(self, lists: Lists, k: torch.Tensor, v: torch.Tensor,
               counts: Optional[torch.Tensor] = None) -> None:
@@ -98,7 +112,7 @@ class PagedKV:
         behind the lists' tokens; counts: int32 [lists], tokens of each list."""
         tokens, strides = self._rows(k, v, lists)
         if counts is not None:
-            _device_int32(counts, (lists.arg.lists,), "counts")
+            _device_int32(counts, (lists.n,), "counts")
         B.headkv_paged_write(self.cfg, self.pool.data_ptr(), lists.arg, k.data_ptr(),
                              v.data_ptr(), strides, tokens, _ptr(counts), Session.stream())
 
@@ -107,7 +121,7 @@ class PagedKV:
         """Tokens begin .. begin + tokens of every list (begin < 0: counted from
         its end) as bf16 [lists][tokens][kv_heads][head_dim], zeros past the end."""
         if k is None:
-            k = torch.empty((lists.arg.lists, tokens, self.cfg.kv_heads, self.cfg.head_dim),
+            k = torch.empty((lists.n, tokens, self.kv_heads, self.head_dim),
                             dtype=torch.bfloat16, device=self.device)
         if v is None:
             v = torch.empty_like(k)
@@ -120,8 +134,7 @@ class PagedKV:
 
     def _workspace(self, own: Lists, shared: Optional[Lists]) -> torch.Tensor:
         """Planned once for the lists' tables, for any length that they can hold."""
-        key = (own.arg.lists, own.arg.max_pages,
-               *(() if shared is None else (shared.arg.lists, shared.arg.max_pages)))
+        key = (own.pages.shape, None if shared is None else shared.pages.shape)
         if key != self._planned:
             most = []
             for l in (own, shared):
@@ -142,24 +155,26 @@ class PagedKV:
         """Attention of q (bf16 [batch][kv_heads * group][head_dim], rows of any
         stride) over the rows' own lists and the shared ones that `share` (int32
         [batch], list number or -1) names; fp32 out, and lse if given."""
-        c = self.cfg
-        batch, heads = own.arg.lists, c.kv_heads * c.group
-        if (q.dtype != torch.bfloat16 or tuple(q.shape) != (batch, heads, c.head_dim)
-                or q.stride(2) != 1 or (heads > 1 and q.stride(1) != c.head_dim)):
-            raise ValueError(f"q must be bf16 {(batch, heads, c.head_dim)} with contiguous rows")
+        batch, heads, d = own.n, self.heads, self.head_dim
+        row, step, one = q.stride()
+        if (q.dtype != torch.bfloat16 or q.shape != (batch, heads, d) or one != 1
+                or (step != d and heads > 1)):
+            raise ValueError(f"q must be bf16 {(batch, heads, d)} with contiguous rows")
         if out is None:
-            out = torch.empty((batch, heads, c.head_dim), dtype=torch.float32, device=self.device)
-        for t, shape in ((out, (batch, heads, c.head_dim)), (lse, (batch, heads))):
-            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape
-                                  or not t.is_contiguous()):
-                raise ValueError(f"out / lse must be contiguous float32 of shape {shape}")
+            out = torch.empty((batch, heads, d), dtype=torch.float32, device=self.device)
+        elif out.dtype != torch.float32 or out.shape != (batch, heads, d) \
+                or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous float32 of shape {(batch, heads, d)}")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads)
+                                or not lse.is_contiguous()):
+            raise ValueError(f"lse must be contiguous float32 of shape {(batch, heads)}")
         if share is not None:
             _device_int32(share, (batch,), "share")
         ws = self._workspace(own, shared)
-        B.headkv_paged_attn(c, self.pool.data_ptr(), own.arg,
+        B.headkv_paged_attn(self.cfg, self.pool.data_ptr(), own.arg,
                             None if shared is None else shared.arg, _ptr(share), q.data_ptr(),
-                            q.stride(0) if batch > 1 else 0, out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(),
-                            Session.stream())
+                            row if batch > 1 else 0, out.data_ptr(), _ptr(lse), ws.data_ptr(),
+                            ws.numel(), Session.stream())
         return out
 
 

@@ -141,6 +141,29 @@ def test_rounding_edges(kind):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("tokens", (1, 4))
+def test_rounding_of_few_tokens(kind, d, tokens):
+    # any bits, infinities and NaN among them, and rows of small numbers only
+    lists, heads = 300, 3
+    g = torch.Generator().manual_seed(d + tokens)
+    for scale in (0, 2.0 ** -130):
+        x = torch.randint(0, 65536, (2, lists, tokens, heads, d), generator=g).to(torch.int32)
+        x = x.to(torch.int16).view(torch.bfloat16)
+        if scale:
+            x = (torch.randn(x.shape, generator=g) * scale).to(torch.bfloat16)
+        else:  # every other row without infinities and NaN
+            x[:, ::2] = torch.where(x[:, ::2].isfinite(), x[:, ::2], torch.ones_like(x[:, ::2]))
+        c = _cache(kind, d, heads, lists * heads)
+        l = c.lists(_table(lists, heads, 1, lists * heads, 2), None, max_len=0)
+        c.write(l, x[0].cuda(), x[1].cuda())
+        l.advance(tokens)
+        k, v = c.read(l, tokens)
+        _same(k, _held(x[0], kind))
+        _same(v, _held(x[1], kind))
+
+
+@pytest.mark.parametrize("kind", TYPES)
 def test_strides_counts_dropped_pages_and_bounds(kind):
     lists, heads, d, tokens = 4, 3, 128, 90
     c = _cache(kind, d, heads, 64, page_tokens=32)
