@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
     // segment make s NaN.
     float mk = product(m, k);
     float s = 0.f, t = 0.f;
-    int above = 0;
+    int above = 0;  // of the wavefront
     auto sums = [&](auto far) {
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -224,15 +224,13 @@ __global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int se
                 const float p = __builtin_amdgcn_exp2f(y);
                 s += p;
                 t = fmaf(p, fmaxf(y, -1e30f), t);
-                above += xv > xt;
+                above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(xv > xt));
             }
     };
     if (__builtin_amdgcn_readfirstlane(fabsf(mk) < INFINITY)) sums(std::false_type{});
     else sums(std::true_type{});
     s = wave_reduce(s, add);
     t = wave_reduce(t, add);
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) above += __shfl_xor(above, o);
     if (lane == 0) {
         red[1][wave] = s;
         red[2][wave] = t;
