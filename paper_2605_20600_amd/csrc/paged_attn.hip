@@ -47,7 +47,8 @@ typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kStep = 32;                          // tokens of a wavefront's step
 constexpr int kUnit = kStep * kWaves;              // and of a block's
-constexpr int kMaxChunk = 64 * kUnit;              // a lane per step holds its page number
+constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
+constexpr int kWideCols = 2 * 16 * kWideWaves;  // columns of a block of k_attn_shared_wide
 
 // One attention call as the kernels see it.
 struct AttnCall {
@@ -85,77 +86,81 @@ struct Tile {
     uint32_t ke[2];     // FP4: exponents of the lane's key rows
     u32x2_t ve[D / 64]; // and of its eight tokens of each V load
 
-    __device__ __forceinline__ void load(const PagedDims& c, const char* page, int tp, int lane) {
+    // Load j of key block u: 16 bytes (FP4, d = 64: 8) of one token's row.
+    static __device__ __forceinline__ u32x4_t key(const char* page, int tp, int lane, int u, int j) {
+        const int i = lane & 15, quarter = lane >> 4, row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
+        if constexpr (TYPE == kBf16) return nt16(page + row * (2 * D) + (4 * j + quarter) * 16);
+        if constexpr (TYPE == kInt8) return nt16(page + row * D + (4 * j + quarter) * 16);
+        if constexpr (D == 128) return nt16(page + row * (D / 2) + quarter * 16);
+        const u32x2_t w = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x2_t*>(page + row * (D / 2) + quarter * 8));
+        return u32x4_t{w[0], w[1], 0, 0};
+    }
+    static __device__ __forceinline__ uint32_t key_exponent(const PagedDims& c, const char* page, int tp,
+                                                            int lane, int u) {
+        const int i = lane & 15, quarter = lane >> 4, row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
+        return (uint8_t)page[c.ks_off + row * (D / 32) + (D == 128 ? quarter : quarter >> 1)];
+    }
+    // Load j of the values: the quarter's eight tokens of 1, 2 or 4 dims.
+    static __device__ __forceinline__ u32x4_t value(const PagedDims& c, const char* page, int tp,
+                                                    int lane, int j) {
+        constexpr int kCell = TYPE == kBf16 ? 16 : 8, kCells = TYPE == kFp4 ? D / 2 : D;
         const int i = lane & 15, quarter = lane >> 4;
-        const char* vp = page + c.v_off;
-        if constexpr (TYPE == kBf16) {
+        return nt16(page + c.v_off + ((tp >> 3) + quarter) * (kCells * kCell) + (16 * j + i) * 16);
+    }
+    static __device__ __forceinline__ u32x2_t value_exponents(const PagedDims& c, const char* page,
+                                                              int tp, int lane, int j) {
+        return *reinterpret_cast<const u32x2_t*>(page + c.vs_off +
+                                                 (2 * j + ((lane & 15) >> 3)) * c.ptok + tp +
+                                                 8 * (lane >> 4));
+    }
+    // INT8: scales of the quarter's eight tokens
+    static __device__ __forceinline__ u32x4_t scales(const char* page, int off, int tp, int lane) {
+        return *reinterpret_cast<const u32x4_t*>(page + off + 2 * (tp + 8 * (lane >> 4)));
+    }
+
+    __device__ __forceinline__ void load(const PagedDims& c, const char* page, int tp, int lane) {
+        if constexpr (TYPE == kInt8) {
+            ks = scales(page, c.ks_off, tp, lane);
+            vs = scales(page, c.vs_off, tp, lane);
+        }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (TYPE == kFp4) ke[u] = key_exponent(c, page, tp, lane, u);
 #pragma unroll
-                for (int j = 0; j < KN; ++j) k[u][j] = nt16(page + row * (2 * D) + (4 * j + quarter) * 16);
-            }
+            for (int j = 0; j < KN; ++j) k[u][j] = key(page, tp, lane, u, j);
+        }
 #pragma unroll
-            for (int j = 0; j < VN; ++j)
-                v[j] = nt16(vp + ((tp >> 3) + quarter) * (D * 16) + (16 * j + i) * 16);
-        } else if constexpr (TYPE == kInt8) {
-            ks = *reinterpret_cast<const u32x4_t*>(page + c.ks_off + 2 * (tp + 8 * quarter));
-            vs = *reinterpret_cast<const u32x4_t*>(page + c.vs_off + 2 * (tp + 8 * quarter));
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
-#pragma unroll
-                for (int j = 0; j < KN; ++j) k[u][j] = nt16(page + row * D + (4 * j + quarter) * 16);
-            }
-#pragma unroll
-            for (int j = 0; j < VN; ++j)
-                v[j] = nt16(vp + ((tp >> 3) + quarter) * (D * 8) + (32 * j + 2 * i) * 8);
-        } else {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
-                ke[u] = (uint8_t)page[c.ks_off + row * (D / 32) + (D == 128 ? quarter : quarter >> 1)];
-                if constexpr (D == 128) {
-                    k[u][0] = nt16(page + row * (D / 2) + quarter * 16);
-                } else {
-                    const u32x2_t w = __builtin_nontemporal_load(
-                        reinterpret_cast<const u32x2_t*>(page + row * (D / 2) + quarter * 8));
-                    k[u][0] = u32x4_t{w[0], w[1], 0, 0};
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < VN; ++j) {
-                ve[j] = *reinterpret_cast<const u32x2_t*>(
-                    page + c.vs_off + (2 * j + (i >> 3)) * c.ptok + tp + 8 * quarter);
-                v[j] = nt16(vp + ((tp >> 3) + quarter) * (D * 4) + (32 * j + 2 * i) * 8);
-            }
+        for (int j = 0; j < VN; ++j) {
+            if constexpr (TYPE == kFp4) ve[j] = value_exponents(c, page, tp, lane, j);
+            v[j] = value(c, page, tp, lane, j);
         }
     }
 
     // Nothing that times a zero weight is not zero, for the lane's tokens n whose
-    // bit n of `seen` is 0 (never written, perhaps).
+    // bit n of `seen` is 0 (never written, perhaps): pairs of 16 bits, or bytes.
+    static __device__ __forceinline__ u32x4_t blank16(u32x4_t w, uint32_t seen) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] &= (seen >> (2 * e) & 1 ? 0xffffu : 0u) | (seen >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+        return w;
+    }
+    static __device__ __forceinline__ u32x2_t blank8(u32x2_t w, uint32_t seen) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m |= seen >> (4 * h + e) & 1 ? 0xffu << (8 * e) : 0u;
+            w[h] &= m;
+        }
+        return w;
+    }
     __device__ __forceinline__ void blank(uint32_t seen) {
-        if constexpr (TYPE == kFp4) {
+        if constexpr (TYPE == kInt8) vs = blank16(vs, seen);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) m |= seen >> (4 * h + e) & 1 ? 0xffu << (8 * e) : 0u;
-#pragma unroll
-                for (int j = 0; j < D / 64; ++j) ve[j][h] &= m;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t m = (seen >> (2 * e) & 1 ? 0xffffu : 0u) |
-                                   (seen >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
-                if constexpr (TYPE == kInt8) {
-                    vs[e] &= m;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < VN; ++j) v[j][e] &= m;
-                }
-            }
+        for (int j = 0; j < VN; ++j) {
+            if constexpr (TYPE == kFp4) ve[j] = blank8(ve[j], seen);
+            if constexpr (TYPE == kBf16) v[j] = blank16(v[j], seen);
         }
     }
 };
@@ -199,16 +204,17 @@ __device__ __forceinline__ bf16x8_t operand(const uint32_t* w) {
     return __builtin_bit_cast(bf16x8_t, u32x4_t{w[0], w[1], w[2], w[3]});
 }
 
-template <int TYPE, int D>
-__device__ __forceinline__ bf16x8_t key_operand(const Tile<TYPE, D>& t, int u, int s) {
-    if constexpr (TYPE == kBf16) return __builtin_bit_cast(bf16x8_t, t.k[u][s]);
+// K operand n of a load of keys (it has 1, 2 or d / 32 of them).
+template <int TYPE>
+__device__ __forceinline__ bf16x8_t key_operand(const u32x4_t& k, uint32_t ke, int n) {
+    if constexpr (TYPE == kBf16) return __builtin_bit_cast(bf16x8_t, k);
     uint32_t o[4];
     if constexpr (TYPE == kInt8) {
-        int8_pack(t.k[u][s >> 1][2 * (s & 1)], o);
-        int8_pack(t.k[u][s >> 1][2 * (s & 1) + 1], o + 2);
+        int8_pack(k[2 * n], o);
+        int8_pack(k[2 * n + 1], o + 2);
     } else {
-        const float e = fp4_exponent(t.ke[u]);
-        const uint32_t w = t.k[u][0][s];
+        const float e = fp4_exponent(ke);
+        const uint32_t w = k[n];
         o[0] = fp4_pack<0>(w, e);
         o[1] = fp4_pack<1>(w, e);
         o[2] = fp4_pack<2>(w, e);
@@ -217,24 +223,24 @@ __device__ __forceinline__ bf16x8_t key_operand(const Tile<TYPE, D>& t, int u, i
     return operand(o);
 }
 
-// V^T operands of load j: one for each of the dims it holds (1, 2 or 4).
-template <int TYPE, int D>
-__device__ __forceinline__ void value_operands(const Tile<TYPE, D>& t, int j, bf16x8_t* a) {
+// V^T operands of a load of values: one for each of the dims it holds (1, 2 or 4).
+template <int TYPE>
+__device__ __forceinline__ void value_operands(const u32x4_t& v, const u32x2_t& ve, bf16x8_t* a) {
     if constexpr (TYPE == kBf16) {
-        a[0] = __builtin_bit_cast(bf16x8_t, t.v[j]);
+        a[0] = __builtin_bit_cast(bf16x8_t, v);
     } else if constexpr (TYPE == kInt8) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             uint32_t o[4];
-            int8_pack(t.v[j][2 * x], o);
-            int8_pack(t.v[j][2 * x + 1], o + 2);
+            int8_pack(v[2 * x], o);
+            int8_pack(v[2 * x + 1], o + 2);
             a[x] = operand(o);
         }
     } else {
         float e[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t w = whole(t.ve[j][h]);
+            const uint32_t w = whole(ve[h]);
 #pragma unroll
             for (int n = 0; n < 4; ++n) e[4 * h + n] = fp4_exponent(w >> (8 * n) & 0xffu);
         }
@@ -243,7 +249,7 @@ __device__ __forceinline__ void value_operands(const Tile<TYPE, D>& t, int j, bf
             uint32_t w[8], lo[4], hi[4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t b = t.v[j][2 * x + h];
+                const uint32_t b = v[2 * x + h];
                 w[4 * h] = fp4_pack<0>(b, e[4 * h]);
                 w[4 * h + 1] = fp4_pack<1>(b, e[4 * h + 1]);
                 w[4 * h + 2] = fp4_pack<2>(b, e[4 * h + 2]);
@@ -260,6 +266,13 @@ __device__ __forceinline__ void value_operands(const Tile<TYPE, D>& t, int j, bf
     }
 }
 
+// Bit n: token n of the lane's eight, of the step at `at`, lies in [first, end).
+__device__ __forceinline__ uint32_t seen_of(int at, int first, int end, int lane) {
+    const int tk = at + 8 * (lane >> 4);
+    const int lo = min(max(first - tk, 0), 8), hi = min(max(end - tk, 0), 8);
+    return 0xffu >> (8 - hi) & 0xffu << lo;
+}
+
 // f over the four lanes of a column (lanes i, i + 16, i + 32, i + 48).
 template <typename F>
 __device__ __forceinline__ float over_quarters(float v, F f) {
@@ -269,6 +282,23 @@ __device__ __forceinline__ float over_quarters(float v, F f) {
     return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
+__device__ __forceinline__ float rounded(float a, float b) {  // the product, not fused
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// Without the instructions that fmaxf adds where an argument might be a signalling
+// NaN.  (Not for what a matrix instruction has just written: the compiler keeps no
+// distance from it for an asm.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// The reference before any score: below all, and finite, so that nothing is NaN.
+constexpr float kLow = -3.402823466e38f;
+
 // State of a wavefront: column i = lane % 16 of each of its NB tiles.
 template <int TYPE, int D, int NB>
 struct Wave {
@@ -277,28 +307,34 @@ struct Wave {
     static constexpr int VX = DB / Tile<TYPE, D>::VN;  // dims of a V load
     bf16x8_t q[NB][KS];
     f32x4_t acc[NB][DB];  // block VX j + x: rows 16 of load j, dim x of each
-    float m[NB], sum[NB];
+    float m[NB], sum[NB];  // reference (log2) and sum of 2^(score - reference)
+    // A reference is a rounded product; from 2^31 on, scores less it, computed with
+    // one rounding, could pass exp2's range, so the scores are rounded like it too.
+    bool far;
 
     __device__ __forceinline__ void clear() {
+        far = false;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            m[b] = -INFINITY;
+            m[b] = kLow;
             sum[b] = 0.f;
 #pragma unroll
             for (int j = 0; j < DB; ++j) acc[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
     }
 
-    // partial: not all tokens are attended, bit n of `seen` is set if token n of
-    // the lane's eight is
-    __device__ __forceinline__ void step(const Tile<TYPE, D>& t, bool partial, uint32_t seen) {
+    // One step: operands from key(u, s) and value(j, a), INT8 scales.  partial: not
+    // all tokens are attended, bit n of `seen` is set if token n of the lane's eight is.
+    template <typename Key, typename Value>
+    __device__ __forceinline__ void step(Key key, Value value, const u32x4_t& key_scales,
+                                         const u32x4_t& value_scales, bool partial, uint32_t seen) {
         constexpr float kScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0));
         f32x4_t st[NB][2];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const bf16x8_t a = key_operand<TYPE, D>(t, u, s);
+                const bf16x8_t a = key(u, s);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
                     st[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
@@ -311,7 +347,7 @@ struct Wave {
         if constexpr (TYPE == kInt8) {
 #pragma unroll
             for (int n = 0; n < 8; n += 2) {
-                const uint32_t k = whole(t.ks[n / 2]), v = whole(t.vs[n / 2]);
+                const uint32_t k = whole(key_scales[n / 2]), v = whole(value_scales[n / 2]);
                 ks[n] *= __uint_as_float(k << 16);
                 ks[n + 1] *= __uint_as_float(k & 0xffff0000u);
                 vs[n] = __uint_as_float(v << 16);
@@ -322,36 +358,50 @@ struct Wave {
         bf16x8_t p[NB][3];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            float s[8];
+            // scores less the reference, log2
+            float x[8];
+            auto less = [&](bool twice) {
 #pragma unroll
-            for (int n = 0; n < 8; ++n) s[n] = st[b][n / 4][n % 4] * ks[n];
-            if (partial) {
+                for (int n = 0; n < 8; ++n) {
+                    const float s = st[b][n / 4][n % 4];
+                    if (twice) x[n] = rounded(s, ks[n]) - m[b];
+                    else x[n] = fmaf(s, ks[n], -m[b]);
+                }
+                if (partial) {
 #pragma unroll
-                for (int n = 0; n < 8; ++n) s[n] = seen >> n & 1 ? s[n] : -INFINITY;
-            }
-            float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])),
-                             fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-            mx = over_quarters(mx, [](float x, float y) { return fmaxf(x, y); });
-            if (__builtin_amdgcn_ballot_w64(mx > m[b]) != 0) {
-                const float now = fmaxf(mx, m[b]);
-                const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[b] - now);
+                    for (int n = 0; n < 8; ++n) x[n] = seen >> n & 1 ? x[n] : -INFINITY;
+                }
+            };
+            if (__builtin_expect(far, 0)) less(true);
+            else less(false);
+            // A reference up to 2^8 below the largest score does as well, and has to
+            // follow it far less often.
+            const float most = max3(max3(max3(x[0], x[1], x[2]), x[3], x[4]), max3(x[5], x[6], x[7]), 0.f);
+            if (__builtin_amdgcn_ballot_w64(most > 8.f) != 0) {
+                float mx = kLow;
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    if (!partial || (seen >> n & 1)) mx = fmaxf(mx, rounded(st[b][n / 4][n % 4], ks[n]));
+                mx = over_quarters(mx, [](float x, float y) { return fmaxf(x, y); });
+                const float now = fmaxf(mx, m[b]), f = __builtin_amdgcn_exp2f(m[b] - now);
                 m[b] = now;
+                far = far || __builtin_amdgcn_ballot_w64(now > kLow && !(fabsf(now) < 0x1p24f)) != 0;
                 sum[b] *= f;
 #pragma unroll
                 for (int j = 0; j < DB; ++j) acc[b][j] *= f;
+                less(far);
             }
-            const float less = m[b] == -INFINITY ? 0.f : m[b];
             uint32_t w[3][4];
 #pragma unroll
             for (int n = 0; n < 8; n += 2) {
                 uint32_t hi[2], mid[2], lo[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float x = __builtin_amdgcn_exp2f(s[n + e] - less);
-                    sum[b] += x;
-                    if constexpr (TYPE == kInt8) x *= vs[n + e];
-                    hi[e] = __float_as_uint(x);
-                    const float r = x - __uint_as_float(hi[e] & 0xffff0000u);
+                    float y = __builtin_amdgcn_exp2f(x[n + e]);
+                    sum[b] += y;
+                    if constexpr (TYPE == kInt8) y *= vs[n + e];
+                    hi[e] = __float_as_uint(y);
+                    const float r = y - __uint_as_float(hi[e] & 0xffff0000u);
                     mid[e] = __float_as_uint(r);
                     lo[e] = __float_as_uint(r - __uint_as_float(mid[e] & 0xffff0000u));
                 }
@@ -368,7 +418,7 @@ struct Wave {
         for (int j0 = 0; j0 < Tile<TYPE, D>::VN; j0 += J) {
             bf16x8_t a[J][VX];
 #pragma unroll
-            for (int j = 0; j < J; ++j) value_operands<TYPE, D>(t, j0 + j, a[j]);
+            for (int j = 0; j < J; ++j) value(j0 + j, a[j]);
 #pragma unroll
             for (int e = 0; e < 3; ++e)
 #pragma unroll
@@ -407,13 +457,13 @@ struct Wave {
         const bool partial = at < first || at + kStep > end;
         uint32_t seen = 0xffu;
         if (partial) {
-            // of the lane's eight tokens
-            const int tk = at + 8 * (lane >> 4);
-            const int lo = min(max(first - tk, 0), 8), hi = min(max(end - tk, 0), 8);
-            seen = 0xffu >> (8 - hi) & 0xffu << lo;
+            seen = seen_of(at, first, end, lane);
             t.blank(seen);
         }
-        step(t, partial, seen);
+        constexpr int kPer = KS / Tile<TYPE, D>::KN;  // operands of a load of keys
+        step([&](int u, int s) { return key_operand<TYPE>(t.k[u][s / kPer], t.ke[u], s % kPer); },
+             [&](int j, bf16x8_t* a) { value_operands<TYPE>(t.v[j], t.ve[TYPE == kFp4 ? j : 0], a); },
+             t.ks, t.vs, partial, seen);
     }
 
     // Tokens [t0, t1) of a list, t0 a multiple of 32, those before `first` not
@@ -468,7 +518,7 @@ __device__ __forceinline__ void join_waves(Wave<TYPE, D, NB>& w, float* lds, int
 #pragma unroll
         for (int k0 = 0; k0 < 16 * D / 4; k0 += kThreads) {
             const int k = k0 + tid, col = k / (D / 4), d = k % (D / 4) * 4;
-            float m = -INFINITY;
+            float m = kLow;
 #pragma unroll
             for (int x = 0; x < kWaves; ++x) m = fmaxf(m, ms[x * 16 + col]);
             f32x4_t v{0.f, 0.f, 0.f, 0.f};
@@ -476,7 +526,7 @@ __device__ __forceinline__ void join_waves(Wave<TYPE, D, NB>& w, float* lds, int
 #pragma unroll
             for (int x = 0; x < kWaves; ++x) {
                 const float mx = ms[x * 16 + col];
-                const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m);
+                const float f = __builtin_amdgcn_exp2f(mx - m);
                 s += f * ms[(kWaves + x) * 16 + col];
                 v += f * *reinterpret_cast<const f32x4_t*>(o + (x * 16 + col) * ROW + d);
             }
@@ -527,11 +577,10 @@ __device__ __forceinline__ f32x2_t published(const void* p) {
 // The sum of parts, one after the other.
 struct Sum {
     f32x4_t v{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, s = 0.f;
+    float m = kLow, s = 0.f;
     __device__ __forceinline__ void add(f32x4_t pv, float pm, float ps) {
         const float now = fmaxf(m, pm);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
-        const float g = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - now);
+        const float f = __builtin_amdgcn_exp2f(m - now), g = __builtin_amdgcn_exp2f(pm - now);
         v = f * v + g * pv;
         s = f * s + g * ps;
         m = now;
@@ -554,6 +603,57 @@ struct Sum {
         }
     }
 };
+
+// The rows whose columns a block of a shared list has: `members` of its rows, counted
+// up to rank1, those of ranks [rank0, rank1) in row_of.  W wavefronts.
+template <int W>
+__device__ __forceinline__ int find_members(const AttnCall& a, int list, int rank0, int rank1,
+                                            int* row_of, int* found, int tid) {
+    const int lane = tid & 63, wave = tid >> 6;
+    int members = 0;
+    for (int b0 = 0; b0 < a.own.lists && members < rank1; b0 += 64 * W) {
+        const int b = b0 + tid;
+        const bool is = b < a.own.lists && a.share[b] == list;
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(is);
+        if (lane == 0) found[wave] = __builtin_popcountll(mask);
+        __syncthreads();
+        int rank = members + __builtin_popcountll(mask & ((1ull << lane) - 1));
+        for (int x = 0; x < W; ++x) {
+            if (x < wave) rank += found[x];
+            members += found[x];
+        }
+        if (is && rank >= rank0 && rank < rank1) row_of[rank - rank0] = b;
+        __syncthreads();
+    }
+    return members;
+}
+
+// Column `col` of a shared list is a query head of the member of rank col / group.
+template <int TYPE, int D>
+__device__ __forceinline__ void load_queries(const AttnCall& a, int h, int col, int rank0,
+                                             const int* row_of, int lane, bf16x8_t* q) {
+    const int group = a.c.group;
+    const uint16_t* from = a.q + row_of[col / group - rank0] * a.q_stride +
+                           (h * group + col % group) * D;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)
+        q[k] = *reinterpret_cast<const bf16x8_t*>(from + key_dim<TYPE, D>(k, lane >> 4));
+}
+// Where its part of a chunk lies.
+__device__ __forceinline__ int64_t shared_slot(const AttnCall& a, int h, int col, int rank0,
+                                               const int* row_of, int chunk) {
+    const int group = a.c.group;
+    const int64_t row = ((int64_t)row_of[col / group - rank0] * a.c.heads + h) * group + col % group;
+    return row * a.shared_parts + chunk;
+}
+
+// Parts of the prefix that row b shares, for kv head h.
+__device__ __forceinline__ int prefix_parts(const AttnCall& a, int b, int h) {
+    if (!a.shared_parts) return 0;
+    const int l = a.share[b];
+    if (l < 0 || l >= a.shared.lists) return 0;
+    return span_of(a.shared, a.c.ptok, (int64_t)l * a.c.heads + h, a.shared_chunk).chunks;
+}
 
 // A row's own list: one block per (row, kv head, chunk), the first also for an
 // empty list.
@@ -583,12 +683,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (s.chunks > 0)
         w.run(a.c, a.pool, a.own.pages + (int64_t)lh * a.own.max_pages, t0, t1, s.first, wave, lane);
 
-    int prefix = 0;  // parts of the row's shared list
-    if (a.shared_parts) {
-        const int l = a.share[b];
-        if (l >= 0 && l < a.shared.lists)
-            prefix = span_of(a.shared, a.c.ptok, (int64_t)l * a.c.heads + h, a.shared_chunk).chunks;
-    }
+    const int prefix = prefix_parts(a, b, h);
     // the row's prefix joins what there is of its own tokens
     auto output = [&](Sum& all, int col, int d) {
         const int64_t row = row0 + col, at = row * a.shared_parts;
@@ -639,15 +734,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
 }
 
-// A shared list: one block per (list, kv head, chunk) and column tile, which
-// takes every `tiles`-th tile of the NB * 16 columns (members * group of them).
-template <int TYPE, int D, int NB>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(NB == 4 ? 1 : 2)))
-void k_attn_shared(AttnCall a) {
-    constexpr int COLS = 16 * NB;
+// A shared list of few columns (members * group of them): one block per (list, kv
+// head, chunk) and tile of 16 columns; a block goes on to every `tiles`-th tile.
+template <int TYPE, int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_shared(AttnCall a) {
     __shared__ __align__(16) float lds[lds_floats<D>()];
-    __shared__ int row_of[COLS + 1];
-    __shared__ int found[kWaves];
+    __shared__ int row_of[17], found[kWaves];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lists = a.shared.lists * a.c.heads;
@@ -658,51 +750,178 @@ void k_attn_shared(AttnCall a) {
     const Span s = span_of(a.shared, a.c.ptok, lh, a.shared_chunk);
     if (chunk >= s.chunks) return;
     const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
-    const int hq = a.c.heads * group;
 
     for (int tile = tile0;; tile += a.tiles) {
-        // the members that the tile's columns belong to: ranks [rank0, rank1)
-        const int c0 = tile * COLS, rank0 = c0 / group, rank1 = (c0 + COLS - 1) / group + 1;
-        int members = 0;
-        for (int b0 = 0; b0 < a.own.lists && members < rank1; b0 += kThreads) {
-            const int b = b0 + tid;
-            const bool is = b < a.own.lists && a.share[b] == list;
-            const uint64_t mask = __builtin_amdgcn_ballot_w64(is);
-            if (lane == 0) found[wave] = __builtin_popcountll(mask);
-            __syncthreads();
-            int rank = members + __builtin_popcountll(mask & ((1ull << lane) - 1));
-            for (int x = 0; x < kWaves; ++x) {
-                if (x < wave) rank += found[x];
-                members += found[x];
-            }
-            if (is && rank >= rank0 && rank < rank1) row_of[rank - rank0] = b;
-            __syncthreads();
-        }
-        const int cols = min(COLS, members * group - c0);  // of this tile
+        const int c0 = tile * 16, rank0 = c0 / group, rank1 = (c0 + 15) / group + 1;
+        const int members = find_members<kWaves>(a, list, rank0, rank1, row_of, found, tid);
+        const int cols = min(16, members * group - c0);
         if (cols <= 0) return;
-
-        Wave<TYPE, D, NB> w;
+        Wave<TYPE, D, 1> w;
         w.clear();
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            const int col = c0 + min(16 * n + (lane & 15), cols - 1);
-            const uint16_t* q = a.q + row_of[col / group - rank0] * a.q_stride +
-                                (h * group + col % group) * D;
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-                w.q[n][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
-        }
+        load_queries<TYPE, D>(a, h, c0 + min(lane & 15, cols - 1), rank0, row_of, lane, w.q[0]);
         w.run(a.c, a.pool, a.shared.pages + (int64_t)lh * a.shared.max_pages, t0, t1, s.first, wave,
               lane);
         join_waves(w, lds, wave, lane, [&](int n, int d, f32x4_t v, float m, float sum) {
             if (n >= cols) return;
-            const int col = c0 + n;
-            const int64_t row =
-                (int64_t)row_of[col / group - rank0] * hq + h * group + col % group;
-            const int64_t slot = row * a.shared_parts + chunk;
+            const int64_t slot = shared_slot(a, h, c0 + n, rank0, row_of, chunk);
             *reinterpret_cast<f32x4_t*>(a.shared_part + slot * D + d) = v;
             if (d == 0) a.shared_ml[slot] = f32x2_t{m, sum};
         });
+    }
+}
+
+// A shared list of many columns: the W wavefronts of a block take NB * 16 columns
+// each and the same tokens, whose operands they convert once for all, a share each,
+// into LDS in the order in which the lanes read them.  While a step is computed, the
+// next one's operands are converted and those of the one after it are loaded.
+template <int TYPE, int D>
+__global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
+    using T = Tile<TYPE, D>;
+    constexpr int W = kWideWaves, COLS = kWideCols, NB = COLS / (16 * W);
+    constexpr int KS = D / 32, DB = D / 16, VX = DB / T::VN;
+    constexpr int kKeys = 2 * T::KN, kLoads = kKeys + T::VN + (TYPE == kInt8 ? 2 : 0);
+    constexpr int kEach = (kLoads + W - 1) / W;
+    constexpr int kScales = 2 * KS + DB;  // INT8: scales lie behind the operands
+    constexpr int kSlots = kScales + (TYPE == kInt8 ? 2 : 0);
+    constexpr int kPer = KS / T::KN;  // operands of a load of keys
+    __shared__ u32x4_t operands[2][kSlots][64];
+    __shared__ int row_of[COLS + 1];
+    __shared__ int found[W];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lists = a.shared.lists * a.c.heads;
+    const int per_tile = lists * a.shared_parts;
+    const int tile0 = blockIdx.x / per_tile, item = blockIdx.x % per_tile;
+    const int lh = item % lists, chunk = item / lists;
+    const int list = lh / a.c.heads, h = lh % a.c.heads, group = a.c.group;
+    const Span s = span_of(a.shared, a.c.ptok, lh, a.shared_chunk);
+    if (chunk >= s.chunks) return;
+    const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
+    // lane n: page of step n of the chunk, which has 64 at most
+    int page = -1;
+    if (t0 + lane * kStep < t1)
+        page = a.shared.pages[(int64_t)lh * a.shared.max_pages + ((t0 + lane * kStep) >> a.c.pshift)];
+    const uint64_t steps = __builtin_amdgcn_ballot_w64(page >= 0 && page < a.c.num_pages);
+
+    for (int tile = tile0;; tile += a.tiles) {
+        // the members that the tile's columns belong to: ranks [rank0, rank1)
+        const int c0 = tile * COLS, rank0 = c0 / group, rank1 = (c0 + COLS - 1) / group + 1;
+        const int members = find_members<W>(a, list, rank0, rank1, row_of, found, tid);
+        const int cols = min(COLS, members * group - c0);  // of this tile
+        if (cols <= 0) return;
+        const int w0 = wave * 16 * NB;  // the wavefront's first column
+        Wave<TYPE, D, NB> w;
+        w.clear();
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+            load_queries<TYPE, D>(a, h, c0 + min(w0 + 16 * n + (lane & 15), cols - 1), rank0, row_of,
+                                  lane, w.q[n]);
+
+        // this wavefront's loads of a step
+        u32x4_t raw[kEach];
+        u32x2_t exponents[kEach];
+        auto fetch = [&](int n) {
+            const char* p = a.pool + __builtin_amdgcn_readlane(page, n) * a.c.page_bytes;
+            const int tp = (t0 + n * kStep) & (a.c.ptok - 1);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int id = wave + W * i;
+                if (id < kKeys) {
+                    raw[i] = T::key(p, tp, lane, id / T::KN, id % T::KN);
+                    if constexpr (TYPE == kFp4)
+                        exponents[i][0] = T::key_exponent(a.c, p, tp, lane, id / T::KN);
+                } else if (id < kKeys + T::VN) {
+                    raw[i] = T::value(a.c, p, tp, lane, id - kKeys);
+                    if constexpr (TYPE == kFp4)
+                        exponents[i] = T::value_exponents(a.c, p, tp, lane, id - kKeys);
+                } else if (id < kLoads) {
+                    raw[i] = T::scales(p, id == kLoads - 2 ? a.c.ks_off : a.c.vs_off, tp, lane);
+                }
+            }
+        };
+        auto convert = [&](int n, int buf) {
+            const int at = t0 + n * kStep;
+            const bool partial = at < s.first || at + kStep > t1;
+            const uint32_t seen = partial ? seen_of(at, s.first, t1, lane) : 0xffu;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int id = wave + W * i;
+                if (id < kKeys) {
+#pragma unroll
+                    for (int x = 0; x < kPer; ++x)
+                        operands[buf][id / T::KN * KS + id % T::KN * kPer + x][lane] =
+                            __builtin_bit_cast(u32x4_t, key_operand<TYPE>(raw[i], exponents[i][0], x));
+                } else if (id < kKeys + T::VN) {
+                    if (partial) {
+                        if constexpr (TYPE == kBf16) raw[i] = T::blank16(raw[i], seen);
+                        if constexpr (TYPE == kFp4) exponents[i] = T::blank8(exponents[i], seen);
+                    }
+                    bf16x8_t o[VX];
+                    value_operands<TYPE>(raw[i], exponents[i], o);
+#pragma unroll
+                    for (int x = 0; x < VX; ++x)
+                        operands[buf][2 * KS + (id - kKeys) * VX + x][lane] =
+                            __builtin_bit_cast(u32x4_t, o[x]);
+                } else if (id < kLoads) {
+                    if (partial && id == kLoads - 1) raw[i] = T::blank16(raw[i], seen);
+                    operands[buf][kScales + id - (kLoads - 2)][lane] = raw[i];
+                }
+            }
+        };
+        uint64_t todo = steps;
+        auto take = [&] {
+            const int n = todo ? __builtin_ctzll(todo) : -1;
+            todo &= todo - 1;
+            return n;
+        };
+        int n0 = take(), n1 = take(), buf = 0;
+        if (n0 >= 0) {
+            fetch(n0);
+            convert(n0, 0);
+            if (n1 >= 0) fetch(n1);
+        }
+        __syncthreads();
+        while (n0 >= 0) {
+            if (n1 >= 0) convert(n1, buf ^ 1);
+            const int n2 = take();
+            if (n2 >= 0) fetch(n2);
+            if (w0 < cols) {
+                const int at = t0 + n0 * kStep;
+                const bool partial = at < s.first || at + kStep > t1;
+                const uint32_t seen = partial ? seen_of(at, s.first, t1, lane) : 0xffu;
+                u32x4_t ks{}, vs{};
+                if constexpr (TYPE == kInt8) {
+                    ks = operands[buf][kScales][lane];
+                    vs = operands[buf][kScales + 1][lane];
+                }
+                w.step([&](int u, int k) {
+                           return __builtin_bit_cast(bf16x8_t, operands[buf][u * KS + k][lane]);
+                       },
+                       [&](int j, bf16x8_t* v) {
+#pragma unroll
+                           for (int x = 0; x < VX; ++x)
+                               v[x] = __builtin_bit_cast(bf16x8_t, operands[buf][2 * KS + j * VX + x][lane]);
+                       },
+                       ks, vs, partial, seen);
+            }
+            __syncthreads();
+            n0 = n1;
+            n1 = n2;
+            buf ^= 1;
+        }
+
+        // the columns' parts, from where they are
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const int at = w0 + 16 * n + (lane & 15);
+            const float sum = over_quarters(w.sum[n], [](float x, float y) { return x + y; });
+            if (at < cols) {
+                const int64_t slot = shared_slot(a, h, c0 + at, rank0, row_of, chunk);
+                w.to_row(n, lane >> 4, a.shared_part + slot * D);
+                if (lane < 16) a.shared_ml[slot] = f32x2_t{w.m[n], sum};
+            }
+        }
+        __syncthreads();  // row_of is written again
     }
 }
 
@@ -719,20 +938,26 @@ int own_chunk_of(int64_t items, int max_len) {
     const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
     return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), 8 * kUnit);
 }
-// Shared lists, whose blocks are one to a CU at many columns: as many as CUs.
-int shared_chunk_of(int64_t items, int max_len) {
-    const int64_t want = std::max<int64_t>(1, kCus / items);
+// Shared lists: as many blocks as fit on the CUs (the wide kernel's, one to a CU).
+int shared_chunk_of(int64_t items, int blocks, int max_len) {
+    const int64_t want = std::max<int64_t>(1, blocks / items);
     const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
-    return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), kMaxChunk);
+    return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), 64 * kStep);
 }
 
 int parts_of(int max_len, int chunk) { return (max_len + chunk - 1) / chunk; }
 
 struct Split {
     int own_chunk, own_parts, shared_chunk, shared_parts;
-    // column tiles of a wavefront, and of the grid for a shared list: as many as
-    // its share of all columns takes; a list with more has its blocks go round
-    int nb, tiles;
+    // Shared lists: which kernel takes them, and the column tiles of one in the grid:
+    // as many as its share of all columns takes; a list with more has its blocks go
+    // round.  Sharing the converted operands among 256 columns costs a barrier per
+    // step, which many columns repay: 128 columns of 32 heads over 2048 tokens take
+    // 52 us in tiles of 16 and 57 wide (INT8; FP4 45 and 54), 256 columns of 8 heads
+    // over 16384 tokens 84 and 63 (FP4 60 and 62, 512 columns 110 and 95; BF16 130
+    // and 61).
+    bool wide;
+    int tiles;
     // offsets, and the total
     size_t ml, part, shared_ml, shared_part, bytes;
 };
@@ -744,9 +969,11 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
     if (shared) {
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
-        s.nb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
-        s.tiles = (int)((mean + 16 * s.nb - 1) / (16 * s.nb));
-        s.shared_chunk = shared_chunk_of((int64_t)shared->lists * c.heads * s.tiles, shared->max_len);
+        s.wide = mean > 128;
+        const int cols = s.wide ? kWideCols : 16;
+        s.tiles = (int)((mean + cols - 1) / cols);
+        s.shared_chunk = shared_chunk_of((int64_t)shared->lists * c.heads * s.tiles,
+                                         s.wide ? kCus : 2 * kCus, shared->max_len);
         s.shared_parts = std::max(1, parts_of(shared->max_len, s.shared_chunk));
     }
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -760,23 +987,21 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
 }
 
 template <int TYPE, int D>
-int attn_launch(const AttnCall& a, int nb, hipStream_t st) {
+int attn_launch(AttnCall a, bool wide, hipStream_t st) {
     if (a.shared_parts) {
         const int64_t grid = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * a.tiles;
         if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
-        if (nb == 1) k_attn_shared<TYPE, D, 1><<<(unsigned)grid, kThreads, 0, st>>>(a);
-        else if (nb == 2) k_attn_shared<TYPE, D, 2><<<(unsigned)grid, kThreads, 0, st>>>(a);
-        else k_attn_shared<TYPE, D, 4><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        if (wide) k_attn_shared_wide<TYPE, D><<<(unsigned)grid, kWideThreads, 0, st>>>(a);
+        else k_attn_shared<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);
         if (int e = (int)hipGetLastError()) return e;
     }
     const int lists = a.own.lists * a.c.heads;
     for (int l0 = 0; l0 < lists; l0 += kCounters) {
-        AttnCall b = a;
-        b.list0 = l0;
-        b.lists = std::min(lists - l0, kCounters);
-        const int64_t grid = (int64_t)b.lists * a.own_parts;
+        a.list0 = l0;
+        a.lists = std::min(lists - l0, kCounters);
+        const int64_t grid = (int64_t)a.lists * a.own_parts;
         if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
-        k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(b);
+        k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);
         if (int e = (int)hipGetLastError()) return e;
     }
     return 0;
@@ -815,12 +1040,12 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
     a.tiles = s.tiles;
     hipStream_t st = (hipStream_t)stream;
     if (c.d == 128)
-        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, s.nb, st)
-               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, s.nb, st)
-                                 : attn_launch<kFp4, 128>(a, s.nb, st);
-    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, s.nb, st)
-           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, s.nb, st)
-                             : attn_launch<kFp4, 64>(a, s.nb, st);
+        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, s.wide, st)
+               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, s.wide, st)
+                                 : attn_launch<kFp4, 128>(a, s.wide, st);
+    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, s.wide, st)
+           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, s.wide, st)
+                             : attn_launch<kFp4, 64>(a, s.wide, st);
 }
 
 }  // namespace headkv

@@ -257,13 +257,17 @@ class Setup:
         self.q = (1.3 * torch.randn((lens.shape[0], heads * group, d), generator=g2)).to(
             torch.bfloat16)
 
-    def check(self, first=None, share=None, dropped=(), max_len=None, q=None, q_dev=None):
+    def check(self, first=None, share=None, dropped=(), max_len=None, q=None, q_dev=None,
+              shared_first=None, shared_dropped=()):
         own = self.lists[0]
         own.arg.max_len = own.arg.max_len if max_len is None else max_len
         keep = []
         if first is not None:
             keep.append(torch.tensor(first, dtype=torch.int32).cuda())
             own.arg.first = keep[-1].data_ptr()
+        if shared_first is not None:
+            keep.append(torch.tensor(shared_first, dtype=torch.int32).cuda())
+            self.lists[1].arg.first = keep[-1].data_ptr()
         q = self.q if q is None else q
         q_dev = q.cuda() if q_dev is None else q_dev
         bsz, hq, d = q.shape
@@ -294,7 +298,13 @@ class Setup:
             if share is not None and 0 <= share[b] < self.k[1].shape[0]:
                 j = share[b]
                 pk, pv = self.k[1][j], self.v[1][j]
-                ps = torch.arange(pk.shape[0])[None] < self.lens[1][j][:, None]
+                at = torch.arange(pk.shape[0])
+                ps = at[None] < self.lens[1][j][:, None]
+                if shared_first is not None:
+                    ps &= at[None] >= torch.tensor(shared_first)[j][:, None]
+                for (db, dh, dp) in shared_dropped:
+                    if db == j:
+                        ps[dh, dp * self.c.cfg.page_tokens:(dp + 1) * self.c.cfg.page_tokens] = False
                 k, v, seen = torch.cat((pk, k)), torch.cat((pv, v)), torch.cat((ps, seen), 1)
             ref, ref_lse, tol, tol_lse = _reference(
                 q[b].double().view(heads, self.group, d), k, v, seen)
@@ -348,6 +358,32 @@ def test_attention_with_shared_prefixes(kind, group, rows):
     s.check(share=[(0, 2, 0, -1, 1, 0, 3)[i % 7] for i in range(rows)])
     s.check(share=[0] * rows)
     s.check(share=[-1] * rows)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d,ptok,group,rows", ((128, 64, 16, 43), (64, 32, 7, 60), (128, 256, 2, 131)))
+def test_prefixes_of_many_columns(kind, d, ptok, group, rows):
+    # windows that start and pages that are dropped inside a chunk, chunks past the
+    # first, an own list that is empty, one list with nearly all columns
+    g = torch.Generator().manual_seed(rows)
+    lens = torch.randint(0, 60, (rows, 2), generator=g).tolist()
+    s = Setup(kind, d, 2, lens, ptok=ptok, group=group, prefix_lens=[[4400, 97], [290, 0]], seed=d)
+    share = [(0, 0, 1, -1, 0)[i % 5] for i in range(rows)]
+    s.check(share=share)
+    s.check(share=[0] * (rows - 1) + [1])
+    for i, (b, h, p) in enumerate(((0, 0, 0), (0, 0, 3000 // ptok), (1, 0, 1))):
+        s.lists[1].pages[b, h, p] = (-1, s.c.cfg.num_pages, -7)[i]
+    s.check(share=share, shared_first=[[1003, 96], [31, 5]],
+            shared_dropped=[(0, 0, 0), (0, 0, 3000 // ptok), (1, 0, 1)])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_prefix_windows_and_dropped_pages(kind):
+    s = Setup(kind, 128, 2, [[3, 40]] * 9, group=3, prefix_lens=[[700, 97], [290, 0]], seed=6)
+    for i, (b, h, p) in enumerate(((0, 0, 2), (0, 1, 0), (1, 0, 1))):
+        s.lists[1].pages[b, h, p] = (-1, s.c.cfg.num_pages, -7)[i]
+    s.check(share=[0, 1, 0, 0, 1, -1, 0, 0, 0], shared_first=[[130, 96], [2 ** 31 - 1, 5]],
+            shared_dropped=[(0, 0, 2), (0, 1, 0), (1, 0, 1)])
 
 
 @pytest.mark.parametrize("d", (64, 128))
