@@ -80,61 +80,59 @@ template <int TYPE, int D>
 struct Tile {
     static constexpr int KN = TYPE == kBf16 ? D / 32 : TYPE == kInt8 ? D / 64 : 1;
     static constexpr int VN = TYPE == kBf16 ? D / 16 : TYPE == kInt8 ? D / 32 : D / 64;
+    static constexpr int kRow = TYPE == kBf16 ? 2 * D : TYPE == kInt8 ? D : D / 2;  // of a token
     u32x4_t k[2][KN];
     u32x4_t v[VN];
     u32x4_t ks, vs;     // INT8: scales of the quarter's eight tokens
     uint32_t ke[2];     // FP4: exponents of the lane's key rows
     u32x2_t ve[D / 64]; // and of its eight tokens of each V load
 
-    // Load j of key block u: 16 bytes (FP4, d = 64: 8) of one token's row.
-    static __device__ __forceinline__ u32x4_t key(const char* page, int tp, int lane, int u, int j) {
-        const int i = lane & 15, quarter = lane >> 4, row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
-        if constexpr (TYPE == kBf16) return nt16(page + row * (2 * D) + (4 * j + quarter) * 16);
-        if constexpr (TYPE == kInt8) return nt16(page + row * D + (4 * j + quarter) * 16);
-        if constexpr (D == 128) return nt16(page + row * (D / 2) + quarter * 16);
-        const u32x2_t w = __builtin_nontemporal_load(
-            reinterpret_cast<const u32x2_t*>(page + row * (D / 2) + quarter * 8));
-        return u32x4_t{w[0], w[1], 0, 0};
-    }
-    static __device__ __forceinline__ uint32_t key_exponent(const PagedDims& c, const char* page, int tp,
-                                                            int lane, int u) {
-        const int i = lane & 15, quarter = lane >> 4, row = tp + 8 * (i >> 2) + 4 * u + (i & 3);
-        return (uint8_t)page[c.ks_off + row * (D / 32) + (D == 128 ? quarter : quarter >> 1)];
-    }
-    // Load j of the values: the quarter's eight tokens of 1, 2 or 4 dims.
-    static __device__ __forceinline__ u32x4_t value(const PagedDims& c, const char* page, int tp,
-                                                    int lane, int j) {
-        constexpr int kCell = TYPE == kBf16 ? 16 : 8, kCells = TYPE == kFp4 ? D / 2 : D;
-        const int i = lane & 15, quarter = lane >> 4;
-        return nt16(page + c.v_off + ((tp >> 3) + quarter) * (kCells * kCell) + (16 * j + i) * 16);
-    }
-    static __device__ __forceinline__ u32x2_t value_exponents(const PagedDims& c, const char* page,
-                                                              int tp, int lane, int j) {
-        return *reinterpret_cast<const u32x2_t*>(page + c.vs_off +
-                                                 (2 * j + ((lane & 15) >> 3)) * c.ptok + tp +
-                                                 8 * (lane >> 4));
-    }
-    // INT8: scales of the quarter's eight tokens
-    static __device__ __forceinline__ u32x4_t scales(const char* page, int off, int tp, int lane) {
-        return *reinterpret_cast<const u32x4_t*>(page + off + 2 * (tp + 8 * (lane >> 4)));
-    }
-
-    __device__ __forceinline__ void load(const PagedDims& c, const char* page, int tp, int lane) {
-        if constexpr (TYPE == kInt8) {
-            ks = scales(page, c.ks_off, tp, lane);
-            vs = scales(page, c.vs_off, tp, lane);
+    // Where a lane's loads are, from the step's place in the page: 32 bits beside an
+    // address that the wavefront has in scalar registers.
+    struct Place {
+        uint32_t key, value, scales, key_powers, value_powers;
+        __device__ __forceinline__ Place(const PagedDims& c, int lane) {
+            const uint32_t i = lane & 15, quarter = lane >> 4, row = 8 * (i >> 2) + (i & 3);
+            key = row * kRow + quarter * (TYPE == kFp4 && D == 64 ? 8 : 16);
+            value = quarter * (8 * kRow) + i * 16;
+            scales = 16 * quarter;
+            key_powers = row * (D / 32) + (D == 128 ? quarter : quarter >> 1);
+            value_powers = (i >> 3) * c.ptok + 8 * quarter;
         }
+    };
+
+    __device__ __forceinline__ void load(const PagedDims& c, const char* page, int tp, const Place& o) {
+        const char* at = page + tp * kRow;
+        if constexpr (TYPE == kInt8) {
+            ks = *reinterpret_cast<const u32x4_t*>(page + c.ks_off + 2 * tp + o.scales);
+            vs = *reinterpret_cast<const u32x4_t*>(page + c.vs_off + 2 * tp + o.scales);
+        }
+        // 16 bytes (FP4, d = 64: 8) of the rows of the two key blocks
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if constexpr (TYPE == kFp4) ke[u] = key_exponent(c, page, tp, lane, u);
+            if constexpr (TYPE == kFp4)
+                ke[u] = (uint8_t)(page + c.ks_off + tp * (D / 32) + o.key_powers)[4 * u * (D / 32)];
 #pragma unroll
-            for (int j = 0; j < KN; ++j) k[u][j] = key(page, tp, lane, u, j);
+            for (int j = 0; j < KN; ++j) {
+                const char* from = at + o.key + (4 * u * kRow + 64 * j);
+                if constexpr (TYPE == kFp4 && D == 64) {
+                    const u32x2_t w =
+                        __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(from));
+                    k[u][j][0] = w[0], k[u][j][1] = w[1];
+                } else {
+                    k[u][j] = nt16(from);
+                }
+            }
+        }
+        // the quarter's eight tokens of 1, 2 or 4 dims
+        if constexpr (TYPE == kFp4) {
+#pragma unroll
+            for (int j = 0; j < VN; ++j)
+                ve[j] = *reinterpret_cast<const u32x2_t*>(page + c.vs_off + 2 * j * c.ptok + tp +
+                                                          o.value_powers);
         }
 #pragma unroll
-        for (int j = 0; j < VN; ++j) {
-            if constexpr (TYPE == kFp4) ve[j] = value_exponents(c, page, tp, lane, j);
-            v[j] = value(c, page, tp, lane, j);
-        }
+        for (int j = 0; j < VN; ++j) v[j] = nt16(at + c.v_off + o.value + 256 * j);
     }
 
     // Nothing that times a zero weight is not zero, for the lane's tokens n whose
@@ -223,6 +221,25 @@ __device__ __forceinline__ bf16x8_t key_operand(const u32x4_t& k, uint32_t ke, i
     return operand(o);
 }
 
+// The two V^T operands of eight FP4 bytes: two dims of the lane's eight tokens.
+__device__ __forceinline__ void fp4_pair(uint32_t v0, uint32_t v1, const u32x2_t& ve, bf16x8_t* a) {
+    uint32_t w[8], lo[4], hi[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t b = h ? v1 : v0, x = whole(ve[h]);
+        w[4 * h] = fp4_pack<0>(b, fp4_exponent(x & 0xffu));
+        w[4 * h + 1] = fp4_pack<1>(b, fp4_exponent(x >> 8 & 0xffu));
+        w[4 * h + 2] = fp4_pack<2>(b, fp4_exponent(x >> 16 & 0xffu));
+        w[4 * h + 3] = fp4_pack<3>(b, fp4_exponent(x >> 24));
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        lo[n] = pack_low(w[2 * n], w[2 * n + 1]);
+        hi[n] = pack_high(w[2 * n], w[2 * n + 1]);
+    }
+    a[0] = operand(lo);
+    a[1] = operand(hi);
+}
 // V^T operands of a load of values: one for each of the dims it holds (1, 2 or 4).
 template <int TYPE>
 __device__ __forceinline__ void value_operands(const u32x4_t& v, const u32x2_t& ve, bf16x8_t* a) {
@@ -237,32 +254,9 @@ __device__ __forceinline__ void value_operands(const u32x4_t& v, const u32x2_t& 
             a[x] = operand(o);
         }
     } else {
-        float e[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t w = whole(ve[h]);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) e[4 * h + n] = fp4_exponent(w >> (8 * n) & 0xffu);
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            uint32_t w[8], lo[4], hi[4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t b = v[2 * x + h];
-                w[4 * h] = fp4_pack<0>(b, e[4 * h]);
-                w[4 * h + 1] = fp4_pack<1>(b, e[4 * h + 1]);
-                w[4 * h + 2] = fp4_pack<2>(b, e[4 * h + 2]);
-                w[4 * h + 3] = fp4_pack<3>(b, e[4 * h + 3]);
-            }
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                lo[n] = pack_low(w[2 * n], w[2 * n + 1]);
-                hi[n] = pack_high(w[2 * n], w[2 * n + 1]);
-            }
-            a[2 * x] = operand(lo);
-            a[2 * x + 1] = operand(hi);
-        }
+        const u32x2_t e{whole(ve[0]), whole(ve[1])};
+        fp4_pair(v[0], v[1], e, a);
+        fp4_pair(v[2], v[3], e, a + 2);
     }
 }
 
@@ -367,7 +361,8 @@ struct Wave {
                     if (twice) x[n] = rounded(s, ks[n]) - m[b];
                     else x[n] = fmaf(s, ks[n], -m[b]);
                 }
-                if (partial) {
+                if (__builtin_expect(partial, 0)) {
+                    asm volatile("");  // a branch: its selects cost as much as the products
 #pragma unroll
                     for (int n = 0; n < 8; ++n) x[n] = seen >> n & 1 ? x[n] : -INFINITY;
                 }
@@ -476,10 +471,10 @@ struct Wave {
         if (mine < t1) page = pages[mine >> c.pshift];
         uint64_t todo = __builtin_amdgcn_ballot_w64(page >= 0 && page < c.num_pages);
         if (!todo) return;
+        const typename Tile<TYPE, D>::Place place(c, lane);
         auto fetch = [&](Tile<TYPE, D>& t, int n) {
-            const int pg = __builtin_amdgcn_readlane(page, n);
             const int at = t0 + (wave + kWaves * n) * kStep;
-            t.load(c, pool + pg * c.page_bytes, at & (c.ptok - 1), lane);
+            t.load(c, pool + __builtin_amdgcn_readlane(page, n) * c.page_bytes, at & (c.ptok - 1), place);
         };
         Tile<TYPE, D> now, next;
         int n = __builtin_ctzll(todo);
@@ -490,6 +485,8 @@ struct Wave {
             if (after >= 0) fetch(next, after);
             step_at(now, t0 + (wave + kWaves * n) * kStep, first, t1, lane);
             if (after < 0) break;
+            // Two tiles in turn, without the copy, take 12 to 30 more registers: 64 x 32
+            // lists of 1000 INT8 tokens 42 us instead of 39.
             now = next;
             n = after;
         }
@@ -770,21 +767,134 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
 }
 
+// What a wavefront of k_attn_shared_wide does of a step's operands: the first four
+// wavefronts convert those of the keys, the others those of the values, D / 64 each
+// (FP4 values: two), which lie together in the page.  One load for all of them, at
+// an address that follows from the token and a number per lane, so that it needs no
+// branch: a load that only some wavefronts do is waited for where the branch ends.
+template <int TYPE, int D>
+struct Share {
+    using T = Tile<TYPE, D>;
+    static constexpr int KS = D / 32, N = D / 64, kRow = T::kRow;
+    static constexpr int kWords = TYPE == kBf16 ? 4 * N : TYPE == kInt8 ? 2 * N : 2;
+    u32x4_t raw[(kWords + 3) / 4];
+    u32x4_t scales;  // INT8: of the lane's eight tokens
+    u32x2_t powers;  // FP4: exponents
+    int off, more, scale_off, scale_step;
+    int slot;     // of its first operand
+    bool values;
+
+    __device__ __forceinline__ Share(const PagedDims& c, int wave, int lane) {
+        const int i = lane & 15, quarter = lane >> 4, w = wave & 3;
+        values = wave >= 4;
+        more = 0;
+        scale_step = 2;
+        if (!values) {
+            const int row = 8 * (i >> 2) + 4 * (w >> 1) + (i & 3), part = w & 1;
+            slot = (w >> 1) * KS + part * N;
+            off = row * kRow;
+            if constexpr (TYPE == kBf16) {
+                off += (4 * N * part + quarter) * 16;
+                more = 64;
+            }
+            if constexpr (TYPE == kInt8) {
+                off += N == 2 ? (4 * part + quarter) * 16 : quarter * 16 + part * 8;
+                scale_off = c.ks_off + 16 * quarter;
+            }
+            if constexpr (TYPE == kFp4) {  // eight bytes that hold the row's exponents
+                off += N == 2 ? quarter * 16 + part * 8 : quarter * 8;
+                scale_step = D / 32;
+                scale_off = c.ks_off + (row * scale_step & ~7);
+                more = (row * scale_step & 7) + (N == 2 ? quarter : quarter >> 1);
+            }
+        } else {
+            const int pair = N == 2 ? w : w & 1;
+            slot = 2 * KS + (TYPE == kFp4 ? 2 * pair : w * N);
+            off = c.v_off + quarter * (8 * kRow);
+            if constexpr (TYPE == kBf16) {
+                off += (16 * N * w + i) * 16;
+                more = 256;
+            }
+            if constexpr (TYPE == kInt8) {
+                off += N == 2 ? (16 * w + i) * 16 : (16 * (w >> 1) + i) * 16 + (w & 1) * 8;
+                scale_off = c.vs_off + 16 * quarter;
+            }
+            if constexpr (TYPE == kFp4) {
+                const int load = pair >> 1;
+                off += (16 * load + i) * 16 + (pair & 1) * 8;
+                scale_step = 1;
+                scale_off = c.vs_off + (2 * load + (i >> 3)) * c.ptok + 8 * quarter;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void fetch(const char* page, int tp) {
+        const char* from = page + tp * kRow + off;
+        if constexpr (kWords == 2) {
+            const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(from));
+            raw[0][0] = w[0], raw[0][1] = w[1];
+        } else {
+            raw[0] = nt16(from);
+            if constexpr (kWords == 8) raw[1] = nt16(from + more);
+        }
+        const char* s = page + tp * scale_step + scale_off;
+        if constexpr (TYPE == kInt8) scales = *reinterpret_cast<const u32x4_t*>(s);
+        if constexpr (TYPE == kFp4) powers = *reinterpret_cast<const u32x2_t*>(s);
+    }
+
+    // Its operands, into the lane's places of the slots; values that are not seen as
+    // zeros (INT8: with scales of zero, which go to slot `at_scales` and the next).
+    __device__ __forceinline__ void convert(u32x4_t (*to)[64], int at_scales, bool partial,
+                                            uint32_t seen, int wave, int lane) {
+        if (values && partial) {
+            if constexpr (TYPE == kBf16) {
+#pragma unroll
+                for (u32x4_t& w : raw) w = T::blank16(w, seen);
+            }
+            if constexpr (TYPE == kInt8) scales = T::blank16(scales, seen);
+            if constexpr (TYPE == kFp4) powers = T::blank8(powers, seen);
+        }
+        if constexpr (TYPE == kBf16) {
+#pragma unroll
+            for (int x = 0; x < N; ++x) to[slot + x][lane] = raw[x];
+        } else if constexpr (TYPE == kInt8) {
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                uint32_t o[4];
+                int8_pack(raw[0][2 * x], o);
+                int8_pack(raw[0][2 * x + 1], o + 2);
+                to[slot + x][lane] = u32x4_t{o[0], o[1], o[2], o[3]};
+            }
+            if ((wave & 3) == 0) to[at_scales + values][lane] = scales;
+        } else if (values) {
+            bf16x8_t o[2];
+            fp4_pair(raw[0][0], raw[0][1], powers, o);
+            to[slot][lane] = __builtin_bit_cast(u32x4_t, o[0]);
+            to[slot + 1][lane] = __builtin_bit_cast(u32x4_t, o[1]);
+        } else {
+            const uint64_t all = (uint64_t)whole(powers[1]) << 32 | whole(powers[0]);
+            const uint32_t e = (uint32_t)(all >> (8 * more)) & 0xffu;
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                const uint32_t w = N == 2 ? raw[0][x] : (wave & 1) ? raw[0][1] : raw[0][0];
+                to[slot + x][lane] = __builtin_bit_cast(u32x4_t, key_operand<kFp4>(u32x4_t{w, 0, 0, 0}, e, 0));
+            }
+        }
+    }
+};
+
 // A shared list of many columns: the W wavefronts of a block take NB * 16 columns
 // each and the same tokens, whose operands they convert once for all, a share each,
-// into LDS in the order in which the lanes read them.  While a step is computed, the
-// next one's operands are converted and those of the one after it are loaded.
+// into LDS in the order in which the lanes read them: those of the next step while
+// one is computed, from loads of the step before it.
 template <int TYPE, int D>
 __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     using T = Tile<TYPE, D>;
     constexpr int W = kWideWaves, COLS = kWideCols, NB = COLS / (16 * W);
     constexpr int KS = D / 32, DB = D / 16, VX = DB / T::VN;
-    constexpr int kKeys = 2 * T::KN, kLoads = kKeys + T::VN + (TYPE == kInt8 ? 2 : 0);
-    constexpr int kEach = (kLoads + W - 1) / W;
     constexpr int kScales = 2 * KS + DB;  // INT8: scales lie behind the operands
     constexpr int kSlots = kScales + (TYPE == kInt8 ? 2 : 0);
-    constexpr int kPer = KS / T::KN;  // operands of a load of keys
-    __shared__ u32x4_t operands[2][kSlots][64];
+    __shared__ u32x4_t operands[2][kSlots][64];  // of two steps in turn
     __shared__ int row_of[COLS + 1];
     __shared__ int found[W];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -802,6 +912,7 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     if (t0 + lane * kStep < t1)
         page = a.shared.pages[(int64_t)lh * a.shared.max_pages + ((t0 + lane * kStep) >> a.c.pshift)];
     const uint64_t steps = __builtin_amdgcn_ballot_w64(page >= 0 && page < a.c.num_pages);
+    Share<TYPE, D> share(a.c, wave, lane);
 
     for (int tile = tile0;; tile += a.tiles) {
         // the members that the tile's columns belong to: ranks [rank0, rank1)
@@ -816,98 +927,54 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
         for (int n = 0; n < NB; ++n)
             load_queries<TYPE, D>(a, h, c0 + min(w0 + 16 * n + (lane & 15), cols - 1), rank0, row_of,
                                   lane, w.q[n]);
-
-        // this wavefront's loads of a step
-        u32x4_t raw[kEach];
-        u32x2_t exponents[kEach];
-        auto fetch = [&](int n) {
-            const char* p = a.pool + __builtin_amdgcn_readlane(page, n) * a.c.page_bytes;
-            const int tp = (t0 + n * kStep) & (a.c.ptok - 1);
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int id = wave + W * i;
-                if (id < kKeys) {
-                    raw[i] = T::key(p, tp, lane, id / T::KN, id % T::KN);
-                    if constexpr (TYPE == kFp4)
-                        exponents[i][0] = T::key_exponent(a.c, p, tp, lane, id / T::KN);
-                } else if (id < kKeys + T::VN) {
-                    raw[i] = T::value(a.c, p, tp, lane, id - kKeys);
-                    if constexpr (TYPE == kFp4)
-                        exponents[i] = T::value_exponents(a.c, p, tp, lane, id - kKeys);
-                } else if (id < kLoads) {
-                    raw[i] = T::scales(p, id == kLoads - 2 ? a.c.ks_off : a.c.vs_off, tp, lane);
-                }
-            }
-        };
-        auto convert = [&](int n, int buf) {
+        auto part_of = [&](int n, uint32_t* seen) {  // step n: is it attended in part
             const int at = t0 + n * kStep;
             const bool partial = at < s.first || at + kStep > t1;
-            const uint32_t seen = partial ? seen_of(at, s.first, t1, lane) : 0xffu;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int id = wave + W * i;
-                if (id < kKeys) {
-#pragma unroll
-                    for (int x = 0; x < kPer; ++x)
-                        operands[buf][id / T::KN * KS + id % T::KN * kPer + x][lane] =
-                            __builtin_bit_cast(u32x4_t, key_operand<TYPE>(raw[i], exponents[i][0], x));
-                } else if (id < kKeys + T::VN) {
-                    if (partial) {
-                        if constexpr (TYPE == kBf16) raw[i] = T::blank16(raw[i], seen);
-                        if constexpr (TYPE == kFp4) exponents[i] = T::blank8(exponents[i], seen);
-                    }
-                    bf16x8_t o[VX];
-                    value_operands<TYPE>(raw[i], exponents[i], o);
-#pragma unroll
-                    for (int x = 0; x < VX; ++x)
-                        operands[buf][2 * KS + (id - kKeys) * VX + x][lane] =
-                            __builtin_bit_cast(u32x4_t, o[x]);
-                } else if (id < kLoads) {
-                    if (partial && id == kLoads - 1) raw[i] = T::blank16(raw[i], seen);
-                    operands[buf][kScales + id - (kLoads - 2)][lane] = raw[i];
-                }
-            }
+            *seen = partial ? seen_of(at, s.first, t1, lane) : 0xffu;
+            return partial;
         };
-        uint64_t todo = steps;
-        auto take = [&] {
-            const int n = todo ? __builtin_ctzll(todo) : -1;
-            todo &= todo - 1;
-            return n;
-        };
-        int n0 = take(), n1 = take(), buf = 0;
-        if (n0 >= 0) {
-            fetch(n0);
-            convert(n0, 0);
-            if (n1 >= 0) fetch(n1);
-        }
-        __syncthreads();
-        while (n0 >= 0) {
-            if (n1 >= 0) convert(n1, buf ^ 1);
-            const int n2 = take();
-            if (n2 >= 0) fetch(n2);
-            if (w0 < cols) {
-                const int at = t0 + n0 * kStep;
-                const bool partial = at < s.first || at + kStep > t1;
-                const uint32_t seen = partial ? seen_of(at, s.first, t1, lane) : 0xffu;
-                u32x4_t ks{}, vs{};
-                if constexpr (TYPE == kInt8) {
-                    ks = operands[buf][kScales][lane];
-                    vs = operands[buf][kScales + 1][lane];
-                }
-                w.step([&](int u, int k) {
-                           return __builtin_bit_cast(bf16x8_t, operands[buf][u * KS + k][lane]);
-                       },
-                       [&](int j, bf16x8_t* v) {
-#pragma unroll
-                           for (int x = 0; x < VX; ++x)
-                               v[x] = __builtin_bit_cast(bf16x8_t, operands[buf][2 * KS + j * VX + x][lane]);
-                       },
-                       ks, vs, partial, seen);
-            }
+        if (steps) {
+            uint64_t to_fetch = steps;
+            int held = 0;  // the step whose loads are held
+            auto fetch = [&] {  // past the last step, that one again
+                if (to_fetch) held = __builtin_ctzll(to_fetch);
+                to_fetch &= to_fetch - 1;
+                share.fetch(a.pool + __builtin_amdgcn_readlane(page, held) * a.c.page_bytes,
+                            (t0 + held * kStep) & (a.c.ptok - 1));
+            };
+            auto produce = [&](int into) {
+                uint32_t seen;
+                const bool partial = part_of(held, &seen);
+                share.convert(operands[into], kScales, partial, seen, wave, lane);
+                fetch();
+            };
+            fetch();
+            produce(0);
             __syncthreads();
-            n0 = n1;
-            n1 = n2;
-            buf ^= 1;
+            int buf = 0;
+            for (uint64_t todo = steps; todo; todo &= todo - 1, buf ^= 1) {
+                produce(buf ^ 1);
+                if (w0 < cols) {
+                    uint32_t seen;
+                    const bool partial = part_of(__builtin_ctzll(todo), &seen);
+                    u32x4_t ks{}, vs{};
+                    if constexpr (TYPE == kInt8) {
+                        ks = operands[buf][kScales][lane];
+                        vs = operands[buf][kScales + 1][lane];
+                    }
+                    w.step([&](int u, int k) {
+                               return __builtin_bit_cast(bf16x8_t, operands[buf][u * KS + k][lane]);
+                           },
+                           [&](int j, bf16x8_t* v) {
+#pragma unroll
+                               for (int x = 0; x < VX; ++x)
+                                   v[x] = __builtin_bit_cast(
+                                       bf16x8_t, operands[buf][2 * KS + j * VX + x][lane]);
+                           },
+                           ks, vs, partial, seen);
+                }
+                __syncthreads();
+            }
         }
 
         // the columns' parts, from where they are
@@ -951,11 +1018,11 @@ struct Split {
     int own_chunk, own_parts, shared_chunk, shared_parts;
     // Shared lists: which kernel takes them, and the column tiles of one in the grid:
     // as many as its share of all columns takes; a list with more has its blocks go
-    // round.  Sharing the converted operands among 256 columns costs a barrier per
-    // step, which many columns repay: 128 columns of 32 heads over 2048 tokens take
-    // 52 us in tiles of 16 and 57 wide (INT8; FP4 45 and 54), 256 columns of 8 heads
-    // over 16384 tokens 84 and 63 (FP4 60 and 62, 512 columns 110 and 95; BF16 130
-    // and 61).
+    // round.  Tiles of 16 columns read and convert the tokens for each tile, the wide
+    // kernel does for 256 columns, with a barrier per step.  With tiles of 16 and wide,
+    // us: BF16 64 columns of 32 heads over 2048 tokens 41 and 39, 96 columns 61 and 50,
+    // 256 columns of 8 heads over 16384 tokens 130 and 52; INT8 33 and 38, 46 and 45,
+    // 85 and 60; FP4 24 and 32, 34 and 39, 58 and 59, 512 columns 103 and 85.
     bool wide;
     int tiles;
     // offsets, and the total
@@ -969,7 +1036,7 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
     if (shared) {
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
-        s.wide = mean > 128;
+        s.wide = mean >= (c.type == kBf16 ? 64 : c.type == kInt8 ? 96 : 256);
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
         s.shared_chunk = shared_chunk_of((int64_t)shared->lists * c.heads * s.tiles,

@@ -361,7 +361,8 @@ def test_attention_with_shared_prefixes(kind, group, rows):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("d,ptok,group,rows", ((128, 64, 16, 43), (64, 32, 7, 60), (128, 256, 2, 131)))
+@pytest.mark.parametrize("d,ptok,group,rows", ((128, 64, 16, 43), (64, 32, 7, 60), (128, 256, 2, 131),
+                                              (64, 64, 13, 41)))
 def test_prefixes_of_many_columns(kind, d, ptok, group, rows):
     # windows that start and pages that are dropped inside a chunk, chunks past the
     # first, an own list that is empty, one list with nearly all columns
