@@ -995,24 +995,27 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
 // ------------------------------------------------------------------- launch
 constexpr int kCus = 256;
 
-// Tokens of a chunk of `items` lists of up to max_len tokens.
+// Tokens of a chunk of lists of up to max_len tokens, of which `want` chunks are wanted.
 // Own lists: about two blocks per CU for few lists, else short enough that blocks
 // that are done early find others (256 lists of 1500-16384 tokens, fp4: 512 tokens
 // 67 us, 1024 61, 2048 69; 32 lists of 98-2480 tokens: 256 tokens 8.5 us, 512 11;
 // 128, a step of a wavefront, 15).
-int own_chunk_of(int64_t items, int max_len) {
-    const int64_t want = std::max<int64_t>(1, 2 * kCus / items);
-    const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
-    return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), 8 * kUnit);
-}
 // Shared lists: as many blocks as fit on the CUs (the wide kernel's, one to a CU).
-int shared_chunk_of(int64_t items, int blocks, int max_len) {
-    const int64_t want = std::max<int64_t>(1, blocks / items);
+constexpr int kLeastChunk = 2 * kUnit, kOwnMost = 8 * kUnit, kSharedMost = 64 * kStep;
+int chunk_of(int max_len, int64_t want, int most) {
     const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
-    return (int)std::min<int64_t>(std::max<int64_t>(chunk, 2 * kUnit), 64 * kStep);
+    return (int)std::min<int64_t>(std::max<int64_t>(chunk, kLeastChunk), most);
 }
 
 int parts_of(int max_len, int chunk) { return (max_len + chunk - 1) / chunk; }
+
+// Parts that no smaller max_len has more of, if chunks of `least` tokens are made
+// longer only once there are `want` of them, up to `most` tokens: a workspace that is
+// large enough for a length is so for all shorter ones.
+int64_t most_parts(int max_len, int64_t want, int least, int most) {
+    return std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(parts_of(max_len, least), want),
+                                                  parts_of(max_len, most)));
+}
 
 struct Split {
     int own_chunk, own_parts, shared_chunk, shared_parts;
@@ -1032,24 +1035,29 @@ struct Split {
 Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shared) {
     Split s{};
     const size_t lists = (size_t)own.lists * c.heads, rows = lists * c.group;
-    s.own_chunk = own_chunk_of(lists, own.max_len);
+    auto wanted = [](int64_t blocks, int64_t items) { return std::max<int64_t>(1, blocks / items); };
+    const int64_t own_want = wanted(2 * kCus, lists);
+    s.own_chunk = chunk_of(own.max_len, own_want, kOwnMost);
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
+    const size_t own_most = most_parts(own.max_len, own_want, kLeastChunk, kOwnMost);
+    size_t shared_most = 0;
     if (shared) {
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
         s.wide = mean >= (c.type == kBf16 ? 64 : c.type == kInt8 ? 96 : 256);
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
-        s.shared_chunk = shared_chunk_of((int64_t)shared->lists * c.heads * s.tiles,
-                                         s.wide ? kCus : 2 * kCus, shared->max_len);
+        const int64_t want = wanted(s.wide ? kCus : 2 * kCus, (int64_t)shared->lists * c.heads * s.tiles);
+        s.shared_chunk = chunk_of(shared->max_len, want, kSharedMost);
         s.shared_parts = std::max(1, parts_of(shared->max_len, s.shared_chunk));
+        shared_most = most_parts(shared->max_len, want, kLeastChunk, kSharedMost);
     }
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-    const size_t own_places = s.own_parts > 1 ? rows * s.own_parts : 0;
+    const size_t own_places = own_most > 1 ? rows * own_most : 0;
     s.ml = kCounterBytes;
     s.part = s.ml + up(own_places * sizeof(f32x2_t));
     s.shared_ml = s.part + up(own_places * c.d * sizeof(float));
-    s.shared_part = s.shared_ml + up(rows * s.shared_parts * sizeof(f32x2_t));
-    s.bytes = s.shared_part + rows * s.shared_parts * c.d * sizeof(float);
+    s.shared_part = s.shared_ml + up(rows * shared_most * sizeof(f32x2_t));
+    s.bytes = s.shared_part + rows * shared_most * c.d * sizeof(float);
     return s;
 }
 
@@ -1063,9 +1071,11 @@ int attn_launch(AttnCall a, bool wide, hipStream_t st) {
         if (int e = (int)hipGetLastError()) return e;
     }
     const int lists = a.own.lists * a.c.heads;
-    for (int l0 = 0; l0 < lists; l0 += kCounters) {
+    // (fewer than 2^32 threads in a launch)
+    const int most = std::max(1, std::min(kCounters, (1 << 23) / a.own_parts));
+    for (int l0 = 0; l0 < lists; l0 += most) {
         a.list0 = l0;
-        a.lists = std::min(lists - l0, kCounters);
+        a.lists = std::min(lists - l0, most);
         const int64_t grid = (int64_t)a.lists * a.own_parts;
         if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
         k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);

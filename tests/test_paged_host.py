@@ -126,6 +126,22 @@ def test_attention_workspace_does_not_shrink():
             last = need
 
 
+@pytest.mark.parametrize("lists,heads", ((20, 5), (1, 1), (3, 4), (8, 8), (64, 32)))
+@pytest.mark.parametrize("kind", (B.HEADKV_KV_BF16, B.HEADKV_KV_INT8, B.HEADKV_KV_FP4))
+def test_attention_workspace_holds_every_shorter_length(lists, heads, kind):
+    cfg, lists2 = _cfg(kv_heads=heads, kv_type=kind), max(1, lists // 8)
+    own = shared = 0
+    for n in range(0, 40000, 32):
+        a = _lists(lists=lists, max_pages=1000, max_len=n)
+        b = _lists(lists=lists2, max_pages=1000, max_len=n)
+        need = B.headkv_paged_attn_plan(cfg, a, None)
+        assert need >= own, n
+        own = need
+        need = B.headkv_paged_attn_plan(cfg, _lists(lists=lists, max_pages=1, max_len=1), b)
+        assert need >= shared, n
+        shared = need
+
+
 def test_scores():
     def status(logits=FAKE, kind=B.HEADKV_LOGITS_BF16, rows=4, vocab=100, stride=100, tokens=FAKE,
                temperature=1.0, top=5, logprob=FAKE, entropy=None, rank=None, tv=FAKE, ti=FAKE,
