@@ -243,12 +243,12 @@ __global__ __launch_bounds__(kThreads) void k_paged_write_few(PagedDims c, char*
     int i;  // the token
     const Task<D> task(ls.lists, c.heads, tokens, &i);
     if (!task.any) return;
+    if (counts && i >= counts[task.l]) return;
     const int lane = task.lane;
     const int64_t row = task.l * r.list + task.h * r.head + i * r.token + 2 * lane;
     const uint32_t wk = *reinterpret_cast<const uint32_t*>(k + row);
     const uint32_t wv = *reinterpret_cast<const uint32_t*>(v + row);
     const int64_t at = (int64_t)(ls.len ? max(ls.len[task.lh], 0) : 0) + ls.extra + i;
-    if (counts && i >= counts[task.l]) return;
     char* page = const_cast<char*>(list_page(c, ls, pool, task.lh, at));
     const int tp = (int)(at & (c.ptok - 1));
     // the largest bits of the key (low half) and the value

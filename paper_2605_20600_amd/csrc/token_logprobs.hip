@@ -484,8 +484,8 @@ int launch_token_logprobs(const ScoreArgs& all, int logits_type, void* ws, void*
     auto* keys = reinterpret_cast<uint64_t*>(w + p.keys);
     auto* arrived = reinterpret_cast<int*>(w);
     hipStream_t st = (hipStream_t)stream;
-    // (grids of at most kCounters rows of 2^10 segments, or 2^24 rows of one)
-    const int most = segments > 1 ? kCounters : 1 << 24;
+    // (fewer than 2^32 threads in a launch)
+    const int most = std::min(segments > 1 ? kCounters : 1 << 22, (1 << 22) / segments);
     for (int r0 = 0; r0 < all.rows; r0 += most) {
         ScoreArgs a = all;
         a.rows = std::min(all.rows - r0, most);

@@ -7,7 +7,7 @@ computation is a call into libheadkv.so through the binding.
 from __future__ import annotations
 
 from functools import lru_cache
-from typing import Dict, Optional, Tuple
+from typing import Dict, List, Optional, Tuple
 
 import torch
 
@@ -16,10 +16,20 @@ from .session import Session, _ptr
 
 
 def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape}, got "
-                         f"{t.dtype} {tuple(t.shape)}")
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on the GPU, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
+
+
+def _new_workspace(need: int, device) -> torch.Tensor:
+    """Its counters zero; what lies behind them is written before it is read."""
+    ws = torch.empty(max(need, _COUNTERS), dtype=torch.uint8, device=device)
+    ws[:_COUNTERS].zero_()
+    return ws
+
+
+_COUNTERS = 1 << 18  # bytes that hold every workspace's counters
 
 
 class Lists:
@@ -59,7 +69,8 @@ class Lists:
 
 
 class PagedKV:
-    """A pool of pages and the workspace of its attention.  Use one per stream."""
+    """A pool of pages and the workspace of its attention.  Use one per stream; a
+    graph that has captured its calls counts as work of the stream it is replayed on."""
 
     def __init__(self, kv_type: str, head_dim: int, kv_heads: int, num_pages: int,
                  page_tokens: int = 64, group: int = 1, device: str = "cuda"):
@@ -70,26 +81,32 @@ class PagedKV:
         self.page_bytes, pool_bytes = B.headkv_paged_plan(self.cfg)
         self.device = device
         self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=device)
-        self._ws = torch.zeros(256, dtype=torch.uint8, device=device)
+        self._ws: Optional[torch.Tensor] = None
+        self._replaced: List[torch.Tensor] = []  # graphs may hold calls that use them
         self._planned = None
 
     def lists(self, pages: torch.Tensor, length: Optional[torch.Tensor], max_len: int,
               first: Optional[torch.Tensor] = None, extra: int = 0) -> Lists:
         got = Lists(pages, length, max_len, first, extra)
-        if got.kv_heads != self.cfg.kv_heads:
-            raise ValueError(f"lists of {got.kv_heads} kv heads for a cache of "
-                             f"{self.cfg.kv_heads}")
+        self._check_heads(got)
         return got
+
+    def _check_heads(self, lists: Lists) -> None:
+        if lists.kv_heads != self.kv_heads:
+            raise ValueError(f"lists of {lists.kv_heads} kv heads for a cache of {self.kv_heads}")
 
     def _rows(self, k, v, lists: Lists) -> Tuple[int, Tuple[int, int, int]]:
         shape, ks = k.shape, k.stride()
         if v.stride() != ks or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 \
-                or v.shape != shape or len(shape) != 4 or ks[3] != 1:
+                or v.shape != shape or len(shape) != 4 or ks[3] != 1 \
+                or not (k.is_cuda and v.is_cuda):
             ks = self._check_rows(k, v)
         n, tokens, heads, d = shape
         if n != lists.n or heads != self.kv_heads or d != self.head_dim:
             raise ValueError(f"k and v must be [{lists.n}][tokens][{self.kv_heads}]"
                              f"[{self.head_dim}], got {tuple(shape)}")
+        if lists.kv_heads != heads:
+            self._check_heads(lists)
         if n == 1 or tokens == 1 or heads == 1:
             # the stride of a dimension of one is never used, and may be anything
             return tokens, (ks[0] if n > 1 else 0, ks[1] if tokens > 1 else 0,
@@ -99,9 +116,11 @@ class PagedKV:
     @staticmethod
     def _check_rows(k, v):
         for t in (k, v):
-            if t.dim() != 4 or t.dtype != torch.bfloat16 or t.shape != k.shape or t.stride(3) != 1:
+            if t.dim() != 4 or t.dtype != torch.bfloat16 or t.shape != k.shape \
+                    or t.stride(3) != 1 or not t.is_cuda:
                 raise ValueError("k and v must be bf16 [lists][tokens][kv_heads][head_dim] with "
-                                 f"contiguous rows, got {t.dtype} {tuple(t.shape)}")
+                                 "contiguous rows on the GPU, got "
+                                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
         for i in range(3):
             if k.shape[i] > 1 and k.stride(i) != v.stride(i):
                 raise ValueError("k and v must have the same strides")
@@ -136,18 +155,24 @@ class PagedKV:
     def _workspace(self, own: Lists, shared: Optional[Lists]) -> torch.Tensor:
         """Planned once for the lists' tables, for any length that they can hold."""
         key = (own.pages.shape, None if shared is None else shared.pages.shape)
-        if key != self._planned:
-            most = []
-            for l in (own, shared):
-                a = None
-                if l is not None:
-                    a = B.PagedListsArg(None, None, None, None, l.arg.lists, l.arg.max_pages, 0,
-                                        l.arg.max_pages * self.cfg.page_tokens)
-                most.append(a)
-            need = B.headkv_paged_attn_plan(self.cfg, *most)
-            if need > self._ws.numel():
-                self._ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
-            self._planned = key
+        if key == self._planned:
+            return self._ws
+        most = []
+        for l in (own, shared):
+            a = None
+            if l is not None:
+                a = B.PagedListsArg(None, None, None, None, l.arg.lists, l.arg.max_pages, 0,
+                                    l.arg.max_pages * self.cfg.page_tokens)
+            most.append(a)
+        need = B.headkv_paged_attn_plan(self.cfg, *most)
+        if self._ws is None or need > self._ws.numel():
+            ws = _new_workspace(need, self.device)
+            if torch.cuda.is_current_stream_capturing():
+                return ws  # the graph's memory, zeroed by it: for this call only
+            if self._ws is not None:
+                self._replaced.append(self._ws)
+            self._ws = ws
+        self._planned = key
         return self._ws
 
     def attn(self, own: Lists, q: torch.Tensor, shared: Optional[Lists] = None,
@@ -157,18 +182,21 @@ class PagedKV:
         stride) over the rows' own lists and the shared ones that `share` (int32
         [batch], list number or -1) names; fp32 out, and lse if given."""
         batch, heads, d = own.n, self.heads, self.head_dim
+        if q.dtype != torch.bfloat16 or q.shape != (batch, heads, d) or not q.is_cuda:
+            raise ValueError(f"q must be bf16 {(batch, heads, d)} on the GPU")
         row, step, one = q.stride()
-        if (q.dtype != torch.bfloat16 or q.shape != (batch, heads, d) or one != 1
-                or (step != d and heads > 1)):
-            raise ValueError(f"q must be bf16 {(batch, heads, d)} with contiguous rows")
+        if one != 1 or (step != d and heads > 1):
+            raise ValueError("q must have contiguous rows")
         if out is None:
             out = torch.empty((batch, heads, d), dtype=torch.float32, device=self.device)
-        elif out.dtype != torch.float32 or out.shape != (batch, heads, d) \
+        elif out.dtype != torch.float32 or out.shape != (batch, heads, d) or not out.is_cuda \
                 or not out.is_contiguous():
-            raise ValueError(f"out must be contiguous float32 of shape {(batch, heads, d)}")
+            raise ValueError(f"out must be contiguous float32 {(batch, heads, d)} on the GPU")
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads)
-                                or not lse.is_contiguous()):
-            raise ValueError(f"lse must be contiguous float32 of shape {(batch, heads)}")
+                                or not lse.is_cuda or not lse.is_contiguous()):
+            raise ValueError(f"lse must be contiguous float32 {(batch, heads)} on the GPU")
+        if own.kv_heads != self.kv_heads or (shared and shared.kv_heads != self.kv_heads):
+            raise ValueError(f"lists of other than {self.kv_heads} kv heads")
         if share is not None:
             _device_int32(share, (batch,), "share")
         ws = self._workspace(own, shared)
@@ -194,8 +222,10 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
     [rows][top]."""
     if top < 0:
         raise ValueError("top must be >= 0")
-    if logits.dim() != 2 or logits.dtype not in _LOGITS or logits.stride(1) != 1:
-        raise ValueError("logits must be bf16 or float32 [rows][vocab] with contiguous rows")
+    if logits.dim() != 2 or logits.dtype not in _LOGITS or logits.stride(1) != 1 \
+            or not logits.is_cuda:
+        raise ValueError("logits must be bf16 or float32 [rows][vocab] with contiguous rows on "
+                         "the GPU")
     rows, vocab = logits.shape
     _device_int32(tokens, (rows,), "tokens")
     dev = logits.device
@@ -215,10 +245,14 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
     need = _score_need(rows, vocab, top)
     ws = None
     if need:
-        key = (dev.index or 0, stream)
-        ws = _score_ws.get(key)
-        if ws is None or ws.numel() < need:
-            ws = _score_ws[key] = torch.zeros(need, dtype=torch.uint8, device=dev)
+        if torch.cuda.is_current_stream_capturing():
+            # the graph's memory, zeroed by it: graphs may be replayed on other streams
+            ws = _new_workspace(need, dev)
+        else:
+            key = (dev.index or 0, stream)
+            ws = _score_ws.get(key)
+            if ws is None or ws.numel() < need:
+                ws = _score_ws[key] = _new_workspace(need, dev)
     B.headkv_token_logprobs(logits.data_ptr(), _LOGITS[logits.dtype], rows, vocab,
                             logits.stride(0) if rows > 1 else vocab, tokens.data_ptr(),
                             temperature, top, logprob.data_ptr(), entropy.data_ptr(),

@@ -215,3 +215,34 @@ def test_refusals():
     for args in ((x.double(), t), (x[:, ::2], t), (x, t.long()), (x[0], t)):
         with pytest.raises(ValueError):
             token_logprobs(*args)
+
+
+def test_refuses_host_memory():
+    x = torch.zeros((2, 10), device="cuda")
+    t = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for args in ((x.cpu(), t), (x, t.cpu())):
+        with pytest.raises(ValueError):
+            token_logprobs(*args)
+
+
+def test_first_use_in_a_graph():
+    # the workspace that a capture makes belongs to the graph alone
+    x, t = _logits(5, 70000, torch.float32, 8)
+    xd, td = x.cuda(), t.cuda()
+    want = token_logprobs(xd, td, top=7)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        res = token_logprobs(xd, td, top=7)
+    with torch.cuda.stream(st):  # before any replay
+        eager = token_logprobs(xd, td, top=7)
+    st.synchronize()
+    for k in want:
+        assert torch.equal(eager[k], want[k]), k
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in want:
+            assert torch.equal(res[k], want[k]), k
+        token_logprobs(xd, td, top=7)

@@ -576,3 +576,70 @@ def test_python_refusals():
     with pytest.raises(B.HeadKVError) as e:
         c.attn(l, good[:, 0], shared=l)
     assert e.value.status == B.HEADKV_ERR_INVALID_ARG
+
+
+def test_python_refuses_other_heads_and_host_memory():
+    c = PagedKV("int8", 128, 2, 10)
+    pages = torch.zeros((1, 1, 3), dtype=torch.int32, device="cuda")
+    other = PagedKV("int8", 128, 1, 10).lists(pages, None, max_len=0)
+    own = c.lists(pages.expand(1, 2, 3).contiguous(), None, max_len=0)
+    rows = torch.zeros((1, 4, 2, 128), dtype=torch.bfloat16, device="cuda")
+    share = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        c.write(other, rows, rows)
+    with pytest.raises(ValueError):
+        c.read(other, 4)
+    with pytest.raises(ValueError):
+        c.attn(other, rows[:, 0])
+    with pytest.raises(ValueError):
+        c.attn(own, rows[:, 0], shared=other, share=share)
+    with pytest.raises(ValueError):
+        c.lists(own.pages.cpu(), None, max_len=0)
+    with pytest.raises(ValueError):
+        c.write(own, rows.cpu(), rows.cpu())
+    with pytest.raises(ValueError):
+        c.write(own, rows, rows, counts=torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        c.attn(own, rows[:, 0].cpu())
+    with pytest.raises(ValueError):
+        c.attn(own, rows[:, 0], out=torch.zeros((1, 2, 128)))
+    with pytest.raises(ValueError):
+        c.attn(own, rows[:, 0], lse=torch.zeros((1, 2)))
+    with pytest.raises(ValueError):
+        c.attn(own, rows[:, 0], shared=own, share=share.cpu())
+
+
+def test_lists_shorter_than_the_tables():
+    # 20 x 5 lists in tables of 21 pages of 64: 1280 tokens take more chunks than 1344
+    g = torch.Generator().manual_seed(3)
+    table = torch.randperm(2100, generator=g).to(torch.int32).view(20, 5, 21).cuda()
+    c = _cache("int8", 64, 5, 2100)
+    k, v = (torch.randn((20, 1280, 5, 64), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    c.write(c.lists(table, None, max_len=0), k, v)
+    q = torch.randn((20, 5, 64), generator=g).to(torch.bfloat16).cuda()
+    n = torch.full((20, 5), 1280, dtype=torch.int32).cuda()
+    a = c.attn(c.lists(table, n, max_len=1280), q)
+    b = c.attn(c.lists(table, n, max_len=1344), q)
+    # other chunks, the same sums: 1280 weighted values of less than 6, added in another order
+    assert float((a - b).abs().max()) <= 2 * 1280 * U * 6
+
+
+def test_first_use_in_a_graph():
+    # the workspace that a capture makes belongs to the graph alone
+    s = Setup("fp4", 64, 2, [[700, 3], [1, 900], [64, 500]], seed=47)
+    q = s.q.cuda()
+    want = s.c.attn(s.lists[0], q).clone()
+    fresh = PagedKV("fp4", 64, 2, s.c.cfg.num_pages, page_tokens=s.c.cfg.page_tokens)
+    fresh.pool.copy_(s.c.pool)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = fresh.attn(s.lists[0], q)
+    eager = fresh.attn(s.lists[0], q)  # before any replay
+    assert torch.equal(eager, want)
+    for _ in range(3):
+        captured.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(captured, want)
+        assert torch.equal(fresh.attn(s.lists[0], q), want)
