@@ -22,9 +22,9 @@
 // bits are exact in bf16; an INT8 scale multiplies its token's score or weight,
 // an FP4 scale enters with the conversion.
 // The wavefronts of a block split its tokens and meet in LDS; blocks split a list
-// into chunks, whose parts (maximum, sum, unnormalised output) the block of a row's
-// own list that finishes last joins in their order, those of the row's prefix,
-// which ran before, among them.
+// into chunks, whose parts (maximum, sum, unnormalised output) the block that brings
+// the last part of a row's list joins in their order, those of the row's prefix
+// among them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -69,6 +69,7 @@ struct AttnCall {
     int own_chunk, own_parts;        // tokens of a chunk, chunks at most
     int shared_chunk, shared_parts;  // (0: no shared lists)
     int tiles;                       // column tiles in the grid, per shared list
+    int shared_blocks;               // of the launch, before those of own lists
 };
 
 __device__ __forceinline__ u32x4_t nt16(const char* p) {
@@ -101,6 +102,13 @@ struct Tile {
         }
     };
 
+    // ONCE: nobody else reads it.
+    template <bool ONCE, typename T>
+    static __device__ __forceinline__ T get(const char* p) {
+        const T* t = reinterpret_cast<const T*>(p);
+        return ONCE ? __builtin_nontemporal_load(t) : *t;
+    }
+    template <bool ONCE>
     __device__ __forceinline__ void load(const PagedDims& c, const char* page, int tp, const Place& o) {
         const char* at = page + tp * kRow;
         if constexpr (TYPE == kInt8) {
@@ -116,11 +124,10 @@ struct Tile {
             for (int j = 0; j < KN; ++j) {
                 const char* from = at + o.key + (4 * u * kRow + 64 * j);
                 if constexpr (TYPE == kFp4 && D == 64) {
-                    const u32x2_t w =
-                        __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(from));
+                    const u32x2_t w = get<ONCE, u32x2_t>(from);
                     k[u][j][0] = w[0], k[u][j][1] = w[1];
                 } else {
-                    k[u][j] = nt16(from);
+                    k[u][j] = get<ONCE, u32x4_t>(from);
                 }
             }
         }
@@ -132,7 +139,7 @@ struct Tile {
                                                           o.value_powers);
         }
 #pragma unroll
-        for (int j = 0; j < VN; ++j) v[j] = nt16(at + c.v_off + o.value + 256 * j);
+        for (int j = 0; j < VN; ++j) v[j] = get<ONCE, u32x4_t>(at + c.v_off + o.value + 256 * j);
     }
 
     // Nothing that times a zero weight is not zero, for the lane's tokens n whose
@@ -461,20 +468,26 @@ struct Wave {
              t.ks, t.vs, partial, seen);
     }
 
+    // Lane n: the page of the wavefront's n-th step of the tokens [t0, t1).
+    template <int W>
+    static __device__ __forceinline__ int pages_of(const PagedDims& c, const int32_t* pages, int t0,
+                                                   int t1, int wave, int lane) {
+        const int mine = t0 + (wave + W * lane) * kStep;
+        return mine < t1 ? pages[mine >> c.pshift] : -1;
+    }
+
     // Tokens [t0, t1) of a list, t0 a multiple of 32, those before `first` not
-    // attended; this wavefront takes every fourth step.
-    __device__ __forceinline__ void run(const PagedDims& c, const char* pool, const int32_t* pages,
-                                        int t0, int t1, int first, int wave, int lane) {
-        // lane n: the page of the wavefront's n-th step, if it is there
-        const int mine = t0 + (wave + kWaves * lane) * kStep;
-        int page = -1;
-        if (mine < t1) page = pages[mine >> c.pshift];
+    // attended; this wavefront takes every W-th step, on pages_of()'s page.
+    template <bool ONCE, int W>
+    __device__ __forceinline__ void run(const PagedDims& c, const char* pool, int page, int t0, int t1,
+                                        int first, int wave, int lane) {
+        if (t0 + (wave + W * lane) * kStep >= t1) page = -1;
         uint64_t todo = __builtin_amdgcn_ballot_w64(page >= 0 && page < c.num_pages);
         if (!todo) return;
         const typename Tile<TYPE, D>::Place place(c, lane);
         auto fetch = [&](Tile<TYPE, D>& t, int n) {
-            const int at = t0 + (wave + kWaves * n) * kStep;
-            t.load(c, pool + __builtin_amdgcn_readlane(page, n) * c.page_bytes, at & (c.ptok - 1), place);
+            const int at = t0 + (wave + W * n) * kStep;
+            t.template load<ONCE>(c, pool + __builtin_amdgcn_readlane(page, n) * c.page_bytes, at & (c.ptok - 1), place);
         };
         Tile<TYPE, D> now, next;
         int n = __builtin_ctzll(todo);
@@ -483,7 +496,7 @@ struct Wave {
             todo &= todo - 1;
             const int after = todo ? __builtin_ctzll(todo) : -1;
             if (after >= 0) fetch(next, after);
-            step_at(now, t0 + (wave + kWaves * n) * kStep, first, t1, lane);
+            step_at(now, t0 + (wave + W * n) * kStep, first, t1, lane);
             if (after < 0) break;
             // Two tiles in turn, without the copy, take 12 to 30 more registers: 64 x 32
             // lists of 1000 INT8 tokens 42 us instead of 39.
@@ -493,49 +506,56 @@ struct Wave {
     }
 };
 
-// Joins the wavefronts of a block, column tile by column tile, and gives every
-// column's maximum, sum and output to `store(column, d, four outputs, m, sum)`.
-template <int TYPE, int D, int NB, typename Store>
-__device__ __forceinline__ void join_waves(Wave<TYPE, D, NB>& w, float* lds, int wave, int lane,
-                                           Store store) {
-    constexpr int ROW = D + 4;  // floats of a column in LDS: 16-byte writes of 16 columns do not meet
-    float* o = lds;                              // [wave][16][ROW]
-    float* ms = lds + kWaves * 16 * ROW;         // [wave][16] maximum, then sum
-    const int i = lane & 15, quarter = lane >> 4;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const float sum = over_quarters(w.sum[b], [](float x, float y) { return x + y; });
-        if (lane < 16) {
-            ms[wave * 16 + lane] = w.m[b];
-            ms[(kWaves + wave) * 16 + lane] = sum;
-        }
-        w.to_row(b, quarter, o + (wave * 16 + i) * ROW);
+// A barrier of the W wavefronts that work together: all of a block, or one alone.
+template <int W>
+__device__ __forceinline__ void together() {
+    if constexpr (W == kWaves) {
         __syncthreads();
-        const int tid = wave * 64 + lane;
-#pragma unroll
-        for (int k0 = 0; k0 < 16 * D / 4; k0 += kThreads) {
-            const int k = k0 + tid, col = k / (D / 4), d = k % (D / 4) * 4;
-            float m = kLow;
-#pragma unroll
-            for (int x = 0; x < kWaves; ++x) m = fmaxf(m, ms[x * 16 + col]);
-            f32x4_t v{0.f, 0.f, 0.f, 0.f};
-            float s = 0.f;
-#pragma unroll
-            for (int x = 0; x < kWaves; ++x) {
-                const float mx = ms[x * 16 + col];
-                const float f = __builtin_amdgcn_exp2f(mx - m);
-                s += f * ms[(kWaves + x) * 16 + col];
-                v += f * *reinterpret_cast<const f32x4_t*>(o + (x * 16 + col) * ROW + d);
-            }
-            store(16 * b + col, d, v, m, s);
-        }
-        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
 }
 
-template <int D>
-constexpr int lds_floats() {
-    return kWaves * 16 * (D + 4) + 2 * kWaves * 16;
+// Joins W wavefronts and gives the maximum, sum and output of their first `cols`
+// columns to `store(column, d, four outputs, m, sum)`.
+template <int W, int TYPE, int D, typename Store>
+__device__ __forceinline__ void join_waves(Wave<TYPE, D, 1>& w, float* lds, int cols, int wave,
+                                           int lane, Store store) {
+    constexpr int ROW = D + 4;  // floats of a column in LDS: 16-byte writes of 16 columns do not meet
+    float* ms = lds;                     // [wave][16] maximum, then sum
+    float* o = lds + 2 * W * 16;         // [wave][cols][ROW]
+    const int i = lane & 15, quarter = lane >> 4;
+    const float sum = over_quarters(w.sum[0], [](float x, float y) { return x + y; });
+    if (lane < 16) {
+        ms[wave * 16 + lane] = w.m[0];
+        ms[(W + wave) * 16 + lane] = sum;
+    }
+    if (i < cols) w.to_row(0, quarter, o + (wave * cols + i) * ROW);
+    together<W>();
+    for (int k = wave * 64 + lane; k < cols * (D / 4); k += 64 * W) {
+        const int col = k / (D / 4), d = k % (D / 4) * 4;
+        float m = kLow;
+#pragma unroll
+        for (int x = 0; x < W; ++x) m = fmaxf(m, ms[x * 16 + col]);
+        f32x4_t v{0.f, 0.f, 0.f, 0.f};
+        float s = 0.f;
+#pragma unroll
+        for (int x = 0; x < W; ++x) {
+            const float mx = ms[x * 16 + col];
+            const float f = __builtin_amdgcn_exp2f(mx - m);
+            s += f * ms[(W + x) * 16 + col];
+            v += f * *reinterpret_cast<const f32x4_t*>(o + (x * cols + col) * ROW + d);
+        }
+        store(col, d, v, m, s);
+    }
+    together<W>();
+}
+
+// LDS that W wavefronts need for `cols` columns.
+constexpr size_t join_bytes(int d, int cols, int W = kWaves) {
+    return (2 * W * 16 + W * cols * (d + 4)) * sizeof(float);
 }
 
 __device__ __forceinline__ void write_out(const AttnCall& a, int64_t row, int d, int D, f32x4_t v,
@@ -569,6 +589,11 @@ __device__ __forceinline__ f32x2_t published(const void* p) {
     return __builtin_bit_cast(f32x2_t, __hip_atomic_load(static_cast<const uint64_t*>(p),
                                                          __ATOMIC_RELAXED,
                                                          __HIP_MEMORY_SCOPE_AGENT));
+}
+
+__device__ __forceinline__ void publish4(float* p, f32x4_t v) {
+    publish(p, __float_as_uint(v[0]), __float_as_uint(v[1]));
+    publish(p + 2, __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
 // The sum of parts, one after the other.
@@ -652,24 +677,75 @@ __device__ __forceinline__ int prefix_parts(const AttnCall& a, int b, int h) {
     return span_of(a.shared, a.c.ptok, (int64_t)l * a.c.heads + h, a.shared_chunk).chunks;
 }
 
-// A row's own list: one block per (row, kv head, chunk), the first also for an
-// empty list.
-template <int TYPE, int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_own(AttnCall a) {
-    __shared__ __align__(16) float lds[lds_floats<D>()];
-    __shared__ int last;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// Output `col`, dims d .. d + 3 of a list whose `chunks` parts and `prefix` parts are
+// all there.  WITH: the prefix's come from the same launch too.
+template <int D, bool WITH>
+__device__ __forceinline__ void add_prefix(const AttnCall& a, Sum& all, int64_t row, int prefix, int d) {
+    const int64_t at = row * a.shared_parts;
+    all.add_parts(
+        prefix,
+        [&](int j) {
+            const float* p = a.shared_part + (at + j) * D + d;
+            if constexpr (!WITH) return *reinterpret_cast<const f32x4_t*>(p);
+            const f32x2_t x = published(p), y = published(p + 2);
+            return f32x4_t{x[0], x[1], y[0], y[1]};
+        },
+        [&](int j) { return WITH ? published(a.shared_ml + at + j) : a.shared_ml[at + j]; });
+}
+template <int D, bool WITH>
+__device__ __forceinline__ void finish(const AttnCall& a, int lh, int chunks, int prefix, int col, int d) {
+    const int64_t row = (int64_t)lh * a.c.group + col, slot = row * a.own_parts;
+    Sum all;
+    all.add_parts(
+        chunks,
+        [&](int j) {
+            const float* p = a.part + (slot + j) * D + d;
+            const f32x2_t x = published(p), y = published(p + 2);
+            return f32x4_t{x[0], x[1], y[0], y[1]};
+        },
+        [&](int j) { return published(a.ml + slot + j); });
+    add_prefix<D, WITH>(a, all, row, prefix, d);
+    write_out(a, row, d, D, all.v, all.m, all.s);
+}
+
+// `columns` of a list's part have arrived; true for the last of `total`.
+__device__ __forceinline__ bool arrive(int* counter, int columns, int total) {
+    const bool last = __hip_atomic_fetch_add(counter, columns, __ATOMIC_RELAXED,
+                                             __HIP_MEMORY_SCOPE_AGENT) + columns == total;
+    if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return last;
+}
+
+// A row's own list: one block, or with W = 1 one wavefront, per (row, kv head, chunk),
+// the first also for an empty list.
+template <int TYPE, int D, bool WITH, int W>
+__device__ __forceinline__ void own_block(const AttnCall& a, int block, float* lds, int* flags) {
+    const int lane = threadIdx.x & 63;
+    int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int unit = block;
+    if constexpr (W == 1) {
+        unit = block * kWaves + wave;
+        if (unit >= a.lists * a.own_parts) return;
+        lds += wave * (join_bytes(D, a.c.group, 1) / sizeof(float));
+        flags += wave;
+        wave = 0;
+    }
+    const int tid = wave * 64 + lane;
     const int group = a.c.group;
-    const int rank = blockIdx.x % a.lists, chunk = blockIdx.x / a.lists;
+    const int rank = unit % a.lists, chunk = unit / a.lists;
     const int at = a.list0 + rank;
     const int lh = a.own.order ? min(max(a.own.order[at], 0), a.own.lists * a.c.heads - 1) : at;
     const int b = lh / a.c.heads, h = lh % a.c.heads;
+    // the pages as they are without a window, before the length is known
+    const int32_t* pages = a.own.pages + (int64_t)lh * a.own.max_pages;
+    const int g0 = chunk * a.own_chunk, g1 = min(g0 + a.own_chunk, a.own.max_len);
+    int page = Wave<TYPE, D, 1>::template pages_of<W>(a.c, pages, g0, g1, wave, lane);
     const Span s = span_of(a.own, a.c.ptok, lh, a.own_chunk);
     const int chunks = max(s.chunks, 1);
     if (chunk >= chunks) return;
     const int t0 = s.start + chunk * a.own_chunk, t1 = min(s.len, t0 + a.own_chunk);
     const int64_t row0 = (int64_t)lh * group;
+    const int prefix = prefix_parts(a, b, h);
 
     Wave<TYPE, D, 1> w;
     w.clear();
@@ -677,94 +753,137 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
     for (int k = 0; k < D / 32; ++k)
         w.q[0][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
-    if (s.chunks > 0)
-        w.run(a.c, a.pool, a.own.pages + (int64_t)lh * a.own.max_pages, t0, t1, s.first, wave, lane);
+    if (s.chunks > 0) {  // (else t0 may be past what an int holds)
+        if (s.start > 0) page = Wave<TYPE, D, 1>::template pages_of<W>(a.c, pages, t0, t1, wave, lane);
+        w.template run<true, W>(a.c, a.pool, page, t0, t1, s.first, wave, lane);
+    }
 
-    const int prefix = prefix_parts(a, b, h);
-    // the row's prefix joins what there is of its own tokens
-    auto output = [&](Sum& all, int col, int d) {
-        const int64_t row = row0 + col, at = row * a.shared_parts;
-        all.add_parts(
-            prefix,
-            [&](int j) { return *reinterpret_cast<const f32x4_t*>(a.shared_part + (at + j) * D + d); },
-            [&](int j) { return a.shared_ml[at + j]; });
-        write_out(a, row, d, D, all.v, all.m, all.s);
-    };
-    join_waves(w, lds, wave, lane, [&](int col, int d, f32x4_t v, float m, float sum) {
-        if (col >= group) return;
-        if (chunks == 1) {
+    int* counter = a.arrived + (WITH ? lh : rank);
+    // the only part that is still missing, or the only one at all
+    if (WITH && tid == 0)
+        *flags = chunks == 1 && (prefix == 0 || __hip_atomic_load(counter, __ATOMIC_RELAXED,
+                                                                  __HIP_MEMORY_SCOPE_AGENT) ==
+                                                    group * prefix);
+    bool alone = chunks == 1;
+    join_waves<W>(w, lds, group, wave, lane, [&](int col, int d, f32x4_t v, float m, float sum) {
+        if (WITH) alone = *flags;  // (there is a barrier before)
+        if (alone) {
             Sum all{v, m, sum};
-            output(all, col, d);
+            add_prefix<D, WITH>(a, all, row0 + col, prefix, d);
+            write_out(a, row0 + col, d, D, all.v, all.m, all.s);
         } else {
             const int64_t slot = (row0 + col) * a.own_parts + chunk;
-            float* p = a.part + slot * D + d;
-            publish(p, __float_as_uint(v[0]), __float_as_uint(v[1]));
-            publish(p + 2, __float_as_uint(v[2]), __float_as_uint(v[3]));
+            publish4(a.part + slot * D + d, v);
             if (d == 0) publish(a.ml + slot, __float_as_uint(m), __float_as_uint(sum));
         }
     });
-    if (chunks == 1) return;
-    // every published word has left before the block counts as arrived
+    if (WITH) alone = *flags;
+    if (alone) {
+        if (WITH && prefix > 0 && tid == 0)
+            __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return;
+    }
+    // every published word has left before the list's part counts as arrived
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-        last = __hip_atomic_fetch_add(a.arrived + rank, 1, __ATOMIC_RELAXED,
-                                      __HIP_MEMORY_SCOPE_AGENT) == chunks - 1;
-        if (last)
-            __hip_atomic_store(a.arrived + rank, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!last) return;
-    for (int i = tid; i < group * (D / 4); i += kThreads) {
-        const int col = i / (D / 4), d = i % (D / 4) * 4;
-        const int64_t slot = (row0 + col) * a.own_parts;
-        Sum all;
-        all.add_parts(
-            chunks,
-            [&](int j) {
-                const float* p = a.part + (slot + j) * D + d;
-                const f32x2_t x = published(p), y = published(p + 2);
-                return f32x4_t{x[0], x[1], y[0], y[1]};
-            },
-            [&](int j) { return published(a.ml + slot + j); });
-        output(all, col, d);
-    }
+    together<W>();
+    if (tid == 0) *flags = arrive(counter, group, group * (chunks + (WITH ? prefix : 0)));
+    together<W>();
+    if (!*flags) return;
+    for (int i = tid; i < group * (D / 4); i += 64 * W)
+        finish<D, WITH>(a, lh, chunks, prefix, i / (D / 4), i % (D / 4) * 4);
 }
 
 // A shared list of few columns (members * group of them): one block per (list, kv
 // head, chunk) and tile of 16 columns; a block goes on to every `tiles`-th tile.
+struct SharedLds {
+    int row_of[17], found[kWaves];
+    int chunks[16];       // of the members' own lists
+    int done[16], count;  // members (of the tile) whose parts are all there
+};
 template <int TYPE, int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_shared(AttnCall a) {
-    __shared__ __align__(16) float lds[lds_floats<D>()];
-    __shared__ int row_of[17], found[kWaves];
+__device__ __forceinline__ void shared_block(const AttnCall& a, int block, float* lds, SharedLds& ints) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lists = a.shared.lists * a.c.heads;
     const int per_tile = lists * a.shared_parts;
-    const int tile0 = blockIdx.x / per_tile, item = blockIdx.x % per_tile;
+    const int tile0 = block / per_tile, item = block % per_tile;
     const int lh = item % lists, chunk = item / lists;
     const int list = lh / a.c.heads, h = lh % a.c.heads, group = a.c.group;
     const Span s = span_of(a.shared, a.c.ptok, lh, a.shared_chunk);
-    if (chunk >= s.chunks) return;
-    const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
+    const int32_t* pages = a.shared.pages + (int64_t)lh * a.shared.max_pages;
+    int* row_of = ints.row_of;
 
     for (int tile = tile0;; tile += a.tiles) {
         const int c0 = tile * 16, rank0 = c0 / group, rank1 = (c0 + 15) / group + 1;
-        const int members = find_members<kWaves>(a, list, rank0, rank1, row_of, found, tid);
+        const int members = find_members<kWaves>(a, list, rank0, rank1, row_of, ints.found, tid);
         const int cols = min(16, members * group - c0);
-        if (cols <= 0) return;
+        if (cols <= 0 || chunk >= s.chunks) return;  // (the length is not waited for alone)
+        const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
+        // lane i: the member of rank rank0 + i, its columns in the tile
+        auto columns = [&] {
+            return min(c0 + cols, (rank0 + lane + 1) * group) - max(c0, (rank0 + lane) * group);
+        };
         Wave<TYPE, D, 1> w;
         w.clear();
         load_queries<TYPE, D>(a, h, c0 + min(lane & 15, cols - 1), rank0, row_of, lane, w.q[0]);
-        w.run(a.c, a.pool, a.shared.pages + (int64_t)lh * a.shared.max_pages, t0, t1, s.first, wave,
-              lane);
-        join_waves(w, lds, wave, lane, [&](int n, int d, f32x4_t v, float m, float sum) {
-            if (n >= cols) return;
+        if (wave == 0 && columns() > 0)
+            ints.chunks[lane] = max(span_of(a.own, a.c.ptok, (int64_t)row_of[lane] * a.c.heads + h,
+                                            a.own_chunk).chunks, 1);
+        const int page = Wave<TYPE, D, 1>::template pages_of<kWaves>(a.c, pages, t0, t1, wave, lane);
+        w.template run<false, kWaves>(a.c, a.pool, page, t0, t1, s.first, wave, lane);
+        join_waves<kWaves>(w, lds, cols, wave, lane, [&](int n, int d, f32x4_t v, float m, float sum) {
             const int64_t slot = shared_slot(a, h, c0 + n, rank0, row_of, chunk);
-            *reinterpret_cast<f32x4_t*>(a.shared_part + slot * D + d) = v;
-            if (d == 0) a.shared_ml[slot] = f32x2_t{m, sum};
+            publish4(a.shared_part + slot * D + d, v);
+            if (d == 0) publish(a.shared_ml + slot, __float_as_uint(m), __float_as_uint(sum));
         });
+        if (a.lists == 0) continue;  // a later launch joins
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (wave == 0) {
+            const int mine = columns();
+            const bool last = mine > 0 && arrive(a.arrived + row_of[lane] * a.c.heads + h, mine,
+                                                 group * (ints.chunks[lane] + s.chunks));
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(last);
+            if (last) ints.done[__builtin_popcountll(mask & ((1ull << lane) - 1))] = lane;
+            if (lane == 0) ints.count = __builtin_popcountll(mask);
+        }
+        __syncthreads();
+        const int per = group * (D / 4);
+        for (int i = tid; i < ints.count * per; i += kThreads) {
+            const int n = ints.done[i / per], k = i % per;
+            finish<D, true>(a, row_of[n] * a.c.heads + h, ints.chunks[n], s.chunks, k / (D / 4),
+                            k % (D / 4) * 4);
+        }
+        __syncthreads();  // row_of and done are written again
     }
+}
+
+// Wavefronts of a SIMD that the kernels' registers allow; the compiler passes the
+// limits by a few registers if it isn't held to them.
+template <int TYPE, int D>
+constexpr int own_waves() { return D == 64 || TYPE == kFp4 ? 4 : TYPE == kInt8 ? 3 : 2; }
+template <int TYPE, int D>
+constexpr int with_shared_waves() { return D == 64 ? 4 : TYPE == kBf16 ? 2 : 3; }
+
+template <int TYPE, int D, int W>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(own_waves<TYPE, D>())))
+void k_attn_own(AttnCall a) {
+    extern __shared__ __align__(16) float lds[];  // join_bytes(D, group)
+    __shared__ int flags[kWaves];
+    own_block<TYPE, D, false, W>(a, blockIdx.x, lds, flags);
+}
+
+// Shared lists of few columns and the rows' own ones in one launch: the shared ones'
+// blocks, which have more to compute, start first, and the rows' fill the CUs beside
+// them.  Whichever brings the last part of a row's list joins them all.
+template <int TYPE, int D, int W>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(with_shared_waves<TYPE, D>())))
+void k_attn_with_shared(AttnCall a) {
+    extern __shared__ __align__(16) float lds[];  // join_bytes(D, 16)
+    __shared__ SharedLds ints;
+    const int block = blockIdx.x;
+    if (block < a.shared_blocks) shared_block<TYPE, D>(a, block, lds, ints);
+    else own_block<TYPE, D, true, W>(a, block - a.shared_blocks, lds, ints.found);
 }
 
 // What a wavefront of k_attn_shared_wide does of a step's operands: the first four
@@ -1000,7 +1119,9 @@ constexpr int kCus = 256;
 // that are done early find others (256 lists of 1500-16384 tokens, fp4: 512 tokens
 // 67 us, 1024 61, 2048 69; 32 lists of 98-2480 tokens: 256 tokens 8.5 us, 512 11;
 // 128, a step of a wavefront, 15).
-// Shared lists: as many blocks as fit on the CUs (the wide kernel's, one to a CU).
+// Shared lists: as many blocks as there are CUs, beside which own lists find room (64
+// rows on a prefix of 2048 INT8 tokens: 256 blocks 58 us, 384 61, 512 63; the own lists'
+// blocks first 74).
 constexpr int kLeastChunk = 2 * kUnit, kOwnMost = 8 * kUnit, kSharedMost = 64 * kStep;
 int chunk_of(int max_len, int64_t want, int most) {
     const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
@@ -1021,13 +1142,22 @@ struct Split {
     int own_chunk, own_parts, shared_chunk, shared_parts;
     // Shared lists: which kernel takes them, and the column tiles of one in the grid:
     // as many as its share of all columns takes; a list with more has its blocks go
-    // round.  Tiles of 16 columns read and convert the tokens for each tile, the wide
-    // kernel does for 256 columns, with a barrier per step.  With tiles of 16 and wide,
-    // us: BF16 64 columns of 32 heads over 2048 tokens 41 and 39, 96 columns 61 and 50,
-    // 256 columns of 8 heads over 16384 tokens 130 and 52; INT8 33 and 38, 46 and 45,
-    // 85 and 60; FP4 24 and 32, 34 and 39, 58 and 59, 512 columns 103 and 85.
+    // round.  Tiles of 16 columns read and convert the tokens for each tile, but run
+    // beside the own lists; the wide kernel does for 256 columns, with a barrier per
+    // step.  With tiles of 16 and wide, us, own lists of up to 576 tokens: 32 heads over
+    // 2048 tokens BF16 64 columns 52 and 54, 128 89 and 87, 256 174 and 155, INT8 96
+    // columns 51 and 56, 192 93 and 91, 256 122 and 113, FP4 128 columns 54 and 55, 192 78
+    // and 73; 8 heads in groups of 4 over 16384 tokens BF16 64 columns 35 and 43, 96 51
+    // and 46, INT8 128 columns 50 and 51, 256 77 and 64, FP4 192 columns 48 and 59, 256
+    // 61 and 64.
     bool wide;
     int tiles;
+    // Own lists: a wavefront each, not a block, where they are many and short, so that
+    // what a list costs however short it is (four loads that wait for each other) is paid
+    // for four at a time.  A block and a wavefront, INT8, d = 128, us: 1024 lists of up to
+    // 16 tokens 8.9 and 6.4, 128 tokens 9.1 and 10.6; 2048 of 128 14.7 and 11.4, 512 25
+    // and 32; 4096 of 128 25 and 18, 512 44 and 41, 1024 70 and 78; 12288 of 128 73 and 42.
+    bool single;
     // offsets, and the total
     size_t ml, part, shared_ml, shared_part, bytes;
 };
@@ -1039,20 +1169,21 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     const int64_t own_want = wanted(2 * kCus, lists);
     s.own_chunk = chunk_of(own.max_len, own_want, kOwnMost);
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
+    s.single = (int64_t)own.max_len * 8 <= (int64_t)lists;
     const size_t own_most = most_parts(own.max_len, own_want, kLeastChunk, kOwnMost);
     size_t shared_most = 0;
     if (shared) {
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
-        s.wide = mean >= (c.type == kBf16 ? 64 : c.type == kInt8 ? 96 : 256);
+        s.wide = mean >= (c.type == kBf16 ? 96 : c.type == kInt8 ? 160 : 256);
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
-        const int64_t want = wanted(s.wide ? kCus : 2 * kCus, (int64_t)shared->lists * c.heads * s.tiles);
+        const int64_t want = wanted(kCus, (int64_t)shared->lists * c.heads * s.tiles);
         s.shared_chunk = chunk_of(shared->max_len, want, kSharedMost);
         s.shared_parts = std::max(1, parts_of(shared->max_len, s.shared_chunk));
         shared_most = most_parts(shared->max_len, want, kLeastChunk, kSharedMost);
     }
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-    const size_t own_places = own_most > 1 ? rows * own_most : 0;
+    const size_t own_places = own_most > 1 || shared ? rows * own_most : 0;
     s.ml = kCounterBytes;
     s.part = s.ml + up(own_places * sizeof(f32x2_t));
     s.shared_ml = s.part + up(own_places * c.d * sizeof(float));
@@ -1062,23 +1193,39 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
 }
 
 template <int TYPE, int D>
-int attn_launch(AttnCall a, bool wide, hipStream_t st) {
-    if (a.shared_parts) {
-        const int64_t grid = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * a.tiles;
-        if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
-        if (wide) k_attn_shared_wide<TYPE, D><<<(unsigned)grid, kWideThreads, 0, st>>>(a);
-        else k_attn_shared<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);
-        if (int e = (int)hipGetLastError()) return e;
-    }
+int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
     const int lists = a.own.lists * a.c.heads;
     // (fewer than 2^32 threads in a launch)
-    const int most = std::max(1, std::min(kCounters, (1 << 23) / a.own_parts));
+    constexpr int64_t kMost = 1 << 23;
+    const int most = (int)std::max<int64_t>(1, std::min<int64_t>(kCounters, kMost / a.own_parts));
+    auto own_blocks = [&] {
+        const int64_t units = (int64_t)a.lists * a.own_parts;
+        return single ? (units + kWaves - 1) / kWaves : units;
+    };
+    if (a.shared_parts) {
+        const int64_t blocks = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * a.tiles;
+        if (blocks > kMost) return (int)hipErrorInvalidValue;
+        if (wide) {
+            k_attn_shared_wide<TYPE, D><<<(unsigned)blocks, kWideThreads, 0, st>>>(a);
+        } else {
+            // with the own lists, where one launch holds them
+            a.shared_blocks = (int)blocks;
+            a.lists = lists <= most ? lists : 0;
+            const unsigned grid = (unsigned)(blocks + own_blocks());
+            const size_t lds = join_bytes(D, 16);
+            if (single) k_attn_with_shared<TYPE, D, 1><<<grid, kThreads, lds, st>>>(a);
+            else k_attn_with_shared<TYPE, D, kWaves><<<grid, kThreads, lds, st>>>(a);
+        }
+        if (int e = (int)hipGetLastError()) return e;
+        if (a.lists) return 0;
+    }
     for (int l0 = 0; l0 < lists; l0 += most) {
         a.list0 = l0;
         a.lists = std::min(lists - l0, most);
-        const int64_t grid = (int64_t)a.lists * a.own_parts;
-        if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
-        k_attn_own<TYPE, D><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        const unsigned grid = (unsigned)own_blocks();
+        const size_t lds = join_bytes(D, a.c.group);
+        if (single) k_attn_own<TYPE, D, 1><<<grid, kThreads, lds, st>>>(a);
+        else k_attn_own<TYPE, D, kWaves><<<grid, kThreads, lds, st>>>(a);
         if (int e = (int)hipGetLastError()) return e;
     }
     return 0;
@@ -1117,12 +1264,12 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
     a.tiles = s.tiles;
     hipStream_t st = (hipStream_t)stream;
     if (c.d == 128)
-        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, s.wide, st)
-               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, s.wide, st)
-                                 : attn_launch<kFp4, 128>(a, s.wide, st);
-    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, s.wide, st)
-           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, s.wide, st)
-                             : attn_launch<kFp4, 64>(a, s.wide, st);
+        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, s.wide, s.single, st)
+               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, s.wide, s.single, st)
+                                 : attn_launch<kFp4, 128>(a, s.wide, s.single, st);
+    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, s.wide, s.single, st)
+           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, s.wide, s.single, st)
+                             : attn_launch<kFp4, 64>(a, s.wide, s.single, st);
 }
 
 }  // namespace headkv

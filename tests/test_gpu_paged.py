@@ -643,3 +643,82 @@ def test_first_use_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(captured, want)
         assert torch.equal(fresh.attn(s.lists[0], q), want)
+
+
+def _short_lists(rows, heads, most, seed):
+    g = torch.Generator().manual_seed(seed)
+    lens = torch.randint(0, most + 1, (rows, heads), generator=g)
+    lens[0, 0], lens[-1, -1], lens[1] = most, 0, 0  # a row without tokens
+    return lens.tolist()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d,group", ((64, 1), (64, 5), (128, 1), (128, 16)))
+def test_many_short_lists(kind, d, group):
+    # 60 x 16 lists of up to 100 tokens: a wavefront each
+    s = Setup(kind, d, 16, _short_lists(60, 16, 100, d + group), ptok=32, group=group, seed=51)
+    s.check()
+    first = torch.randint(-3, 110, (60, 16), generator=torch.Generator().manual_seed(1))
+    first[2] = 2 ** 31 - 1
+    s.check(first=first.tolist())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("group", (1, 3, 7))
+def test_many_short_lists_with_shared_prefixes(kind, group):
+    # in the order of the launch, rows of two prefixes, of one without tokens and of none
+    g = torch.Generator().manual_seed(group)
+    rows = 16 if group > 1 else 40
+    heads = 50
+    prefix = torch.randint(0, 1400, (3, heads), generator=g)
+    prefix[2] = 0
+    s = Setup(kind, 64, heads, _short_lists(rows, heads, 80, 9), group=group, seed=53,
+              prefix_lens=prefix.tolist())
+    share = torch.randint(-1, 4, (rows,), generator=g).tolist()  # (3 is no list)
+    share[0], share[1] = 0, 0
+    s.check(share=share)
+    first = torch.randint(0, 60, (rows, heads), generator=g).tolist()
+    s.check(share=share, first=first)
+    s.check(share=[1] * rows, first=first,
+            shared_first=torch.randint(0, 900, (3, heads), generator=g).tolist())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("group", (1, 5, 16))
+def test_prefixes_and_long_lists_in_one_launch(kind, group):
+    # both in several parts, rows that end in the middle of a column tile
+    s = Setup(kind, 128, 2, [[1500, 0], [3, 700], [0, 0], [900, 2100], [64, 1]], group=group, seed=57,
+              prefix_lens=[[1700, 1], [30, 2500]])
+    s.check(share=[0, 1, 0, 1, 1])
+    s.check(share=[0, 0, 0, 0, 0], first=[[1400, 0], [0, 650], [0, 0], [899, 3], [64, 0]])
+
+
+def test_shared_prefix_and_more_lists_than_counters():
+    # the shared lists' launch cannot join the rows' own: 66000 of them
+    batch, heads, d, ptok = 660, 100, 64, 32
+    g = torch.Generator().manual_seed(15)
+    lens = torch.randint(0, 60, (batch, heads), generator=g).to(torch.int32)
+    # all rows read the same two pages of a head, each as many tokens as it has
+    table = torch.arange(2 * heads, dtype=torch.int32).view(1, heads, 2)
+    prefix = torch.arange(2 * heads, 5 * heads, dtype=torch.int32).view(1, heads, 3)
+    c = _cache("int8", d, heads, 5 * heads, page_tokens=ptok)
+    k, v = (_values((1, 60, heads, d), 21 + i, 0.7) for i in range(2))
+    pk, pv = (_values((1, 90, heads, d), 23 + i, 0.7) for i in range(2))
+    c.write(c.lists(table.cuda(), None, max_len=0), k.cuda(), v.cuda())
+    c.write(c.lists(prefix.cuda(), None, max_len=0), pk.cuda(), pv.cuda())
+    share = torch.full((batch,), -1, dtype=torch.int32)
+    share[::50] = 0  # 14 columns: tiles of 16
+    q = _values((batch, heads, d), 27, 0.3)
+    own = c.lists(table.expand(batch, heads, 2).contiguous().cuda(), lens.cuda(), max_len=60)
+    p = c.lists(prefix.cuda(), torch.full((1, heads), 90, dtype=torch.int32).cuda(), max_len=90)
+    k, v, pk, pv = (_held(x[0], "int8") for x in (k, v, pk, pv))
+    for _ in range(2):
+        got = c.attn(own, q.cuda(), shared=p, share=share.cuda()).cpu().double()
+        for b in list(range(0, 660, 50)) + [1, 333, 655, 656, 659]:
+            there = torch.arange(60)[None] < lens[b][:, None]
+            kb, vb = k, v
+            if share[b] == 0:
+                kb, vb = torch.cat((pk, k)), torch.cat((pv, v))
+                there = torch.cat((torch.ones((heads, 90), dtype=torch.bool), there), 1)
+            ref, _, tol, _ = _reference(q[b].double().view(heads, 1, d), kb, vb, there)
+            assert float((got[b] - ref[:, 0]).abs().max()) <= tol, b
