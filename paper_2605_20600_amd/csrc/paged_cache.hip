@@ -104,16 +104,10 @@ __global__ __launch_bounds__(kThreads) void k_paged_write(PagedDims c, char* poo
             const uint32_t top = max(m & 0xffffu, m >> 16);
             if constexpr (TYPE == kInt8) {
                 const uint16_t s = int8_scale(top);
+                const Int8Row row(s);
                 uint32_t o[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    o[i] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t x = w[2 * i + e / 2] >> (16 * (e & 1)) & 0xffffu;
-                        o[i] |= (uint32_t)(int8_code(x, s) & 0xff) << (8 * e);
-                    }
-                }
+                for (int i = 0; i < 4; ++i) o[i] = row.codes(w[2 * i], w[2 * i + 1]);
                 if (there) {
                     *reinterpret_cast<uint4*>(page + (tp + t) * D + piece * 16) =
                         make_uint4(o[0], o[1], o[2], o[3]);
@@ -182,15 +176,21 @@ __global__ __launch_bounds__(kThreads) void k_paged_write(PagedDims c, char* poo
         m[t] = lanes_max<TYPE == kInt8 ? D / 2 : 16>(m[t]);
     }
     if constexpr (TYPE == kInt8) {
+        // lane t works out token t's scale and its inverse for all lanes
+        uint32_t top = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            if ((lane & 7) == t) top = t < 4 ? m[t] & 0xffffu : m[t - 4] >> 16;
+        const uint16_t mine = int8_scale(top);
+        const Int8Row own(mine);
         uint32_t o[4] = {};
-        uint16_t mine = 0;
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const uint16_t s = int8_scale(t < 4 ? m[t] & 0xffffu : m[t - 4] >> 16);
-            if (lane == t) mine = s;
-            const uint32_t a = int8_code(w[t] & 0xffffu, s) & 0xff, b = int8_code(w[t] >> 16, s) & 0xff;
-            o[t / 4] |= a << (8 * (t % 4));
-            o[2 + t / 4] |= b << (8 * (t % 4));
+            const Int8Row row(__shfl(own.scale, t, 8), __shfl(own.inverse, t, 8));
+            // both dims of the token, into byte t % 4 of a word each
+            const uint32_t codes = row.codes(w[t], 0);
+            o[t / 4] |= (codes & 0xffu) << (8 * (t % 4));
+            o[2 + t / 4] |= (codes >> 8 & 0xffu) << (8 * (t % 4));
         }
         char* dst = cells + lane * 16;
         if (full) {
@@ -265,11 +265,12 @@ __global__ __launch_bounds__(kThreads) void k_paged_write_few(PagedDims c, char*
         to[8] = (uint16_t)(wv >> 16);
     } else if constexpr (TYPE == kInt8) {
         const uint16_t sk = int8_scale(m & 0xffffu), sv = int8_scale(m >> 16);
-        reinterpret_cast<uint16_t*>(page + tp * D)[lane] =
-            (uint16_t)((int8_code(wk & 0xffffu, sk) & 0xff) | (int8_code(wk >> 16, sk) & 0xff) << 8);
+        const Int8Row key(sk), value(sv);
+        const uint32_t codes = (key.codes(wk, 0) & 0xffffu) | value.codes(wv, 0) << 16;
+        reinterpret_cast<uint16_t*>(page + tp * D)[lane] = (uint16_t)codes;
         char* to = cells + lane * 16 + t;
-        to[0] = (char)int8_code(wv & 0xffffu, sv);
-        to[8] = (char)int8_code(wv >> 16, sv);
+        to[0] = (char)(codes >> 16);
+        to[8] = (char)(codes >> 24);
         if (lane == 0) reinterpret_cast<uint16_t*>(page + c.ks_off)[tp] = sk;
         if (lane == 1) reinterpret_cast<uint16_t*>(page + c.vs_off)[tp] = sv;
     } else {
