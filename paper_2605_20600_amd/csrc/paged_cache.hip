@@ -52,12 +52,15 @@ struct Task {
     int64_t lh;
     bool any;        // a task at all
     __device__ Task(int lists, int heads, int blocks, int* blk) {
-        const int64_t i = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+        // (32 bits: a grid has fewer than 2^24 blocks)
+        uint32_t i = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+        if constexpr (LANES == 64) i = __builtin_amdgcn_readfirstlane(i);
         lane = threadIdx.x % LANES;
-        any = i < (int64_t)lists * heads * blocks;
-        h = (int)(i % heads);  // heads of a token are neighbours in memory
-        *blk = (int)(i / heads % blocks);
-        l = (int)(i / heads / blocks);
+        const uint32_t token = i / (uint32_t)heads;
+        h = (int)(i - token * heads);  // heads of a token are neighbours in memory
+        l = (int)(token / (uint32_t)blocks);
+        *blk = (int)(token - (uint32_t)l * blocks);
+        any = l < lists;
         lh = (int64_t)l * heads + h;
     }
 };
@@ -75,21 +78,41 @@ __global__ __launch_bounds__(kThreads) void k_paged_write(PagedDims c, char* poo
     const int64_t end = base + (counts ? min(max(counts[task.l], 0), tokens) : tokens);
     const int64_t p0 = ((base >> 3) + blk) * 8;
     if (p0 >= end) return;
+    // every load is on its way before the first is waited for
     char* page = const_cast<char*>(list_page(c, ls, pool, task.lh, p0));
-    if (!page) return;
     const int tp = (int)(p0 & (c.ptok - 1)), lane = task.lane;
     const int64_t row0 = task.l * r.list + task.h * r.head + (p0 - base) * r.token;
+    const int key_t = lane / (D / 16), piece = lane % (D / 16);
+    const bool key_there = p0 + key_t >= base && p0 + key_t < end;
+    uint32_t key[8] = {};
+    if (key_there) {
+        const uint4* src = reinterpret_cast<const uint4*>(k + row0 + key_t * r.token + piece * 16);
+        const uint4 a = src[0], b = src[1];
+        key[0] = a.x, key[1] = a.y, key[2] = a.z, key[3] = a.w;
+        key[4] = b.x, key[5] = b.y, key[6] = b.z, key[7] = b.w;
+    }
+    uint32_t w[8];
+    bool there[8], full = true;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        there[t] = p0 + t >= base && p0 + t < end;
+        full = full && there[t];
+    }
+    if (full) {  // (no branch for each)
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            w[t] = *reinterpret_cast<const uint32_t*>(v + row0 + t * r.token + 2 * lane);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            w[t] = there[t] ? *reinterpret_cast<const uint32_t*>(v + row0 + t * r.token + 2 * lane) : 0u;
+    }
+    if (!page) return;
 
     {  // K: 16 dims of one token
-        const int t = lane / (D / 16), piece = lane % (D / 16);
-        const bool there = p0 + t >= base && p0 + t < end;
-        uint32_t w[8] = {};
-        if (there) {
-            const uint4* src = reinterpret_cast<const uint4*>(k + row0 + t * r.token + piece * 16);
-            const uint4 a = src[0], b = src[1];
-            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-            w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-        }
+        const int t = key_t;
+        const bool there = key_there;
+        const uint32_t* w = key;
         if constexpr (TYPE == kBf16) {
             if (there) {
                 uint4* dst = reinterpret_cast<uint4*>(page + (tp + t) * (2 * D) + piece * 32);
@@ -138,14 +161,6 @@ __global__ __launch_bounds__(kThreads) void k_paged_write(PagedDims c, char* poo
     }
 
     // V: two dims of eight tokens
-    uint32_t w[8];
-    bool there[8], full = true;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        there[t] = p0 + t >= base && p0 + t < end;
-        full = full && there[t];
-        w[t] = there[t] ? *reinterpret_cast<const uint32_t*>(v + row0 + t * r.token + 2 * lane) : 0u;
-    }
     char* cells = page + c.v_off + (tp >> 3) * 8 * (c.v_off / c.ptok);
     if constexpr (TYPE == kBf16) {
         char* dst = cells + lane * 32;
@@ -404,7 +419,7 @@ template <int D>
 int grid_of(const PagedLists& l, int heads, int blocks, unsigned* grid) {
     const int64_t n = (int64_t)l.lists * heads * blocks;
     const int64_t g = (n + kThreads / (D / 2) - 1) / (kThreads / (D / 2));
-    if (g > 0x7fffffff) return (int)hipErrorInvalidValue;
+    if (g >= 1 << 24) return (int)hipErrorInvalidValue;  // 2^32 threads: more than a launch has
     *grid = (unsigned)g;
     return 0;
 }
