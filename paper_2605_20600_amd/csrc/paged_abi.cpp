@@ -110,11 +110,11 @@ headkv_status headkv_paged_write(const headkv_paged_config* cfg, void* pool,
     PagedLists l;
     if (headkv_status st = make_dims(cfg, &c)) return st;
     if (headkv_status st = make_lists(c, lists, true, &l)) return st;
+    if (tokens < 0) return bad("tokens must be >= 0");
+    if (tokens == 0) return HEADKV_OK;  // rows of no tokens may have no address
     if (headkv_status st = check_rows(k, v, list_stride, token_stride, head_stride)) return st;
     if (!pool || !aligned(pool, 256)) return bad("pool is NULL or not 256-byte aligned");
-    if (tokens < 0) return bad("tokens must be >= 0");
     if (!aligned(counts, 4)) return bad("counts not aligned");
-    if (tokens == 0) return HEADKV_OK;
     const PagedRows r{list_stride, token_stride, head_stride};
     return hip_status(launch_paged_write(c, static_cast<char*>(pool), l, k, v, r, tokens, counts,
                                          stream),
@@ -129,13 +129,13 @@ headkv_status headkv_paged_read(const headkv_paged_config* cfg, const void* pool
     PagedLists l;
     if (headkv_status st = make_dims(cfg, &c)) return st;
     if (headkv_status st = make_lists(c, lists, true, &l)) return st;
+    if (tokens < 0) return bad("tokens must be >= 0");
+    if (tokens == 0) return HEADKV_OK;
     if (headkv_status st = check_rows(k, v, list_stride, token_stride, head_stride)) return st;
     if (!pool || !aligned(pool, 256)) return bad("pool is NULL or not 256-byte aligned");
-    if (tokens < 0) return bad("tokens must be >= 0");
     if ((l.lists > 1 && list_stride < c.d) || (tokens > 1 && token_stride < c.d) ||
         (c.heads > 1 && head_stride < c.d))
         return bad("output rows overlap: a stride is smaller than head_dim");
-    if (tokens == 0) return HEADKV_OK;
     const PagedRows r{list_stride, token_stride, head_stride};
     return hip_status(launch_paged_read(c, static_cast<const char*>(pool), l, begin, tokens, k, v,
                                         r, stream),

@@ -88,6 +88,13 @@ def test_nothing_to_write_or_read():
                    None) == B.HEADKV_OK
 
 
+def test_rows_of_no_tokens_need_no_address():
+    assert _status("headkv_paged_write", _cfg(), FAKE, _lists(), None, None, 0, 0, 128, 0, None,
+                   None) == B.HEADKV_OK
+    assert _status("headkv_paged_read", _cfg(), FAKE, _lists(), 0, 0, None, None, 0, 0, 128,
+                   None) == B.HEADKV_OK
+
+
 @pytest.mark.parametrize("strides,tokens", [((64, 512, 128), 1), ((512, 64, 128), 2),
                                             ((512, 512, 0), 1)])
 def test_read_refuses_overlapping_rows(strides, tokens):
