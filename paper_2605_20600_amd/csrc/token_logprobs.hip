@@ -16,7 +16,7 @@
 // left, and of the values equal to it the first in index order are taken.
 //
 // One MI355X: 18816 rows of 16384 fp32 logits 181 us, 6.8 TB/s, bound by the bytes; 256
-// rows of 65536 bf16 logits with 20 alternatives 22 us, of which the bytes take 5: the
+// rows of 65536 bf16 logits with 20 alternatives 18 us, of which the bytes take 5: the
 // load, the bisection, ranking the candidates and the join of a row's segments wait for
 // each other; 8 rows of 16384 7 us.
 #include <hip/hip_runtime.h>
@@ -154,10 +154,11 @@ __device__ __forceinline__ void select_top(const uint64_t* keys, int n, int top,
     }
 }
 
+// (32 bf16 logits a thread: in as few registers as four blocks of a CU may have; with
+// three, 256 rows of 65536 took 22 us instead of 18, 1000 of 130000 106 instead of 82.)
 template <typename T, int kThreads, int kEpt>
-__global__ __launch_bounds__(kThreads) void k_token_logprobs(ScoreArgs a, int segments,
-                                                             Part* parts, uint64_t* part_keys,
-                                                             int* arrived) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kEpt == 32 && sizeof(T) == 2 ? 8 : 4)))
+void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_keys, int* arrived) {
     using Values = Logits<T, kThreads, kEpt>;
     constexpr int N = Values::N, NV = Values::NV, kSegment = kThreads * kEpt;
     constexpr int kGroupMost = kMaxTop * (kSegment / kGroups);  // logits of kMaxTop groups
