@@ -1161,7 +1161,10 @@ struct Split {
     // columns 51 and 56, 192 93 and 91, 256 122 and 113, FP4 128 columns 54 and 55, 192 78
     // and 73; 8 heads in groups of 4 over 16384 tokens BF16 64 columns 35 and 43, 96 51
     // and 46, INT8 128 columns 50 and 51, 256 77 and 64, FP4 192 columns 48 and 59, 256
-    // 61 and 64.
+    // 61 and 64.  And it takes 20 us and more however short the prefix is, so tiles of 16
+    // take what does not fill the card several times with blocks: BF16 512 columns of 2 x
+    // 4 heads over 64 tokens 12 and 19, of 8 x 4 over 2048 36 and 40, of 32 x 4 over 1000 70
+    // and 55, FP4 13 (300 tokens) and 29, 28 and 39, 47 and 48, over 2048 63 and 63.
     bool wide;
     int tiles;
     // Own lists: a wavefront each, not a block, where they are many and short, so that
@@ -1186,7 +1189,10 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     size_t shared_most = 0;
     if (shared) {
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
-        s.wide = mean >= (c.type == kBf16 ? 96 : c.type == kInt8 ? 160 : 256);
+        const int64_t blocks = (mean + 15) / 16 * shared->lists * c.heads *
+                               parts_of(shared->max_len, kLeastChunk);  // of 16 columns, 256 tokens
+        s.wide = mean >= (c.type == kBf16 ? 96 : c.type == kInt8 ? 160 : 256) &&
+                 blocks >= (c.type == kBf16 ? 3072 : c.type == kInt8 ? 4096 : 6144);
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
         const int64_t want = wanted(kCus, (int64_t)shared->lists * c.heads * s.tiles);

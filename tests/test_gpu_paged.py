@@ -722,3 +722,25 @@ def test_shared_prefix_and_more_lists_than_counters():
                 there = torch.cat((torch.ones((heads, 90), dtype=torch.bool), there), 1)
             ref, _, tol, _ = _reference(q[b].double().view(heads, 1, d), kb, vb, there)
             assert float((got[b] - ref[:, 0]).abs().max()) <= tol, b
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d,ptok,group,rows", ((128, 64, 16, 43), (64, 32, 7, 60), (128, 256, 2, 180),
+                                              (64, 64, 13, 41), (128, 32, 1, 520)))
+def test_prefixes_of_many_columns_that_may_be_long(kind, d, ptok, group, rows):
+    # what the tables can hold, not the lengths, says that there is work for blocks of
+    # 256 columns
+    g = torch.Generator().manual_seed(rows)
+    lens = torch.randint(0, 60, (rows, 2), generator=g).tolist()
+    s = Setup(kind, d, 2, lens, ptok=ptok, group=group, prefix_lens=[[4400, 97], [290, 0]], seed=d)
+    l = s.lists[1]
+    table = torch.full((2, 2, -(-60000 // ptok)), -1, dtype=torch.int32).cuda()
+    table[:, :, :l.pages.shape[2]] = l.pages
+    s.lists[1] = s.c.lists(table, l.length, max_len=60000)
+    share = [(0, 0, 1, -1, 0)[i % 5] for i in range(rows)]
+    s.check(share=share)
+    s.check(share=[0] * (rows - 1) + [1])
+    for i, (b, h, p) in enumerate(((0, 0, 0), (0, 0, 3000 // ptok), (1, 0, 1))):
+        s.lists[1].pages[b, h, p] = (-1, s.c.cfg.num_pages, -7)[i]
+    s.check(share=share, shared_first=[[1003, 96], [31, 5]],
+            shared_dropped=[(0, 0, 0), (0, 0, 3000 // ptok), (1, 0, 1)])
