@@ -104,11 +104,25 @@ struct Logits {
     }
 };
 
-// m k, 0 for an empty maximum
-__device__ __forceinline__ float product(float m, float k) {
+constexpr float kLog2e = 1.4426950408889634f;
+
+// What exponents y = (x - m) / temperature, in log2 units, are computed from.  Near:
+// y = x k - mk with mk = m k rounded once for all, which shifts every y by what it was
+// rounded, left().  That is up to half a unit in the last place of mk: 1/2 at 2^24, where
+// near ends, 128 and so past exp2's range at 2^31.  Far: (x - m) / temperature, shifted
+// by nothing.  (Far if mk is no number, too.)
+struct Reference {
+    float m, mk;
+    bool far;
+    __device__ __forceinline__ Reference(float most, float k) : m(most) {
 #pragma clang fp contract(off)
-    return m == -INFINITY ? 0.f : m * k;
-}
+        mk = m == -INFINITY ? 0.f : m * k;  // (0 for an empty maximum)
+        far = !(fabsf(mk) < 0x1p24f);
+    }
+    __device__ __forceinline__ float left(float k) const {
+        return far || m == -INFINITY ? 0.f : fmaf(m, k, -mk);
+    }
+};
 
 template <typename F>
 __device__ __forceinline__ float wave_reduce(float v, F f) {
@@ -189,7 +203,7 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
         const T w = row[token];
         xt = sizeof(T) == 4 ? __uint_as_float((uint32_t)w) : __uint_as_float((uint32_t)w << 16);
     }
-    const float k = a.scale * 1.4426950408889634f;  // to log2 units
+    const float k = a.scale * kLog2e;  // to log2 units
 
     float mine = -INFINITY;
 #pragma unroll
@@ -212,10 +226,9 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, red[0][w]);
 
-    // y = x k - mk with mk = m k rounded once for all, which shifts every y, and so
-    // log S, by the same; where m k is not finite, (x - m) k.  NaN and +inf in the
-    // segment make s NaN.
-    float mk = product(m, k);
+    // NaN and +inf in the segment make s NaN.
+    auto scaled = [&](float d) { return d * k; };
+    const Reference own(m, k);
     float s = 0.f, t = 0.f;
     int above = 0;  // of the wavefront
     auto sums = [&](auto far) {
@@ -224,15 +237,15 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float xv = x.at(v, e);
-                const float y = decltype(far)::value ? (xv - m) * k : fmaf(xv, k, -mk);
+                const float y = decltype(far)::value ? scaled(xv - m) : fmaf(xv, k, -own.mk);
                 const float p = __builtin_amdgcn_exp2f(y);
                 s += p;
                 t = fmaf(p, fmaxf(y, -1e30f), t);
                 above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(xv > xt));
             }
     };
-    if (__builtin_amdgcn_readfirstlane(fabsf(mk) < INFINITY)) sums(std::false_type{});
-    else sums(std::true_type{});
+    if (__builtin_amdgcn_readfirstlane(own.far)) sums(std::true_type{});
+    else sums(std::false_type{});
     s = wave_reduce(s, add);
     t = wave_reduce(t, add);
     if (lane == 0) {
@@ -376,7 +389,7 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
         m = -INFINITY;
         for (int i = lane; i < segments; i += 64) m = fmaxf(m, __uint_as_float(first_of(read(p[i].w))));
         m = wave_reduce(m, fmaxf);
-        mk = product(m, k);
+        const Reference all(m, k);
         s = t = 0.f;
         above = 0;
         for (int i = lane; i < segments; i += 64) {
@@ -384,10 +397,11 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
             const float pm = __uint_as_float(first_of(u)), ps = __uint_as_float(second_of(u));
             const float pt = __uint_as_float(first_of(v));
             above += (int)second_of(v);
-            // nothing but -inf: ps is 0, or NaN
-            float shift = product(pm, k) - mk;
-            if (!(fabsf(mk) < INFINITY)) shift = (pm - m) * k;
-            if (pm == -INFINITY) shift = 0.f;
+            // from the segment's reference, which may be the other kind, to the row's
+            const Reference part(pm, k);
+            float shift = part.mk - all.mk;
+            if (part.far || all.far) shift = scaled(pm - m) + (all.left(k) - part.left(k));
+            if (pm == -INFINITY) shift = 0.f;  // nothing but -inf: ps is 0, or NaN
             const float f = __builtin_amdgcn_exp2f(shift);
             s = fmaf(f, ps, s);
             t = fmaf(f, fmaf(fmaxf(shift, -1e30f), ps, pt), t);
@@ -429,8 +443,7 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
     const bool ok = s == s && m < INFINITY;
     constexpr float kLn2 = 0.6931471805599453f;
     const float log_s = __builtin_amdgcn_logf(s);  // log2
-    // without the shift by what m k was rounded
-    const float log_true = fabsf(mk) < INFINITY && m > -INFINITY ? log_s - fmaf(m, k, -mk) : log_s;
+    const float log_true = log_s - Reference(m, k).left(k);
     auto logprob = [&](float v) {
         return v == -INFINITY ? v : (v - m) * a.scale - log_true * kLn2;
     };
