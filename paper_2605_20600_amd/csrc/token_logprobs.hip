@@ -110,7 +110,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // y = x k - mk with mk = m k rounded once for all, which shifts every y by what it was
 // rounded, left().  That is up to half a unit in the last place of mk: 1/2 at 2^24, where
 // near ends, 128 and so past exp2's range at 2^31.  Far: (x - m) / temperature, shifted
-// by nothing.  (Far if mk is no number, too.)
+// by nothing.  (Far if mk or k alone is no number, too.)
 struct Reference {
     float m, mk;
     bool far;
@@ -227,7 +227,7 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, red[0][w]);
 
     // NaN and +inf in the segment make s NaN.
-    auto scaled = [&](float d) { return d * k; };
+    auto scaled = [&](float d) { return d * a.scale * kLog2e; };
     const Reference own(m, k);
     float s = 0.f, t = 0.f;
     int above = 0;  // of the wavefront

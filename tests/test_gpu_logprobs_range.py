@@ -11,6 +11,7 @@ from test_gpu_logprobs import _check, _logits
 
 pytestmark = pytest.mark.gpu
 DTYPES = (torch.bfloat16, torch.float32)
+TINY = float(torch.tensor(3e-39))  # as fp32 holds it
 LARGE = (3e5, 1e9, 9e9, 1e10, 1e20, 1e30)
 
 
@@ -93,3 +94,14 @@ def test_segments_about_the_bound(sign, span):
                                                                  generator=g)
     t = torch.randint(0, vocab, (4,), generator=g).to(torch.int32)
     _check(x, t, 9)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_temperatures_whose_inverse_is_nearly_too_large(dtype):
+    # 1 / 3e-39 is finite, 1 / 3e-39 in log2 units is not; differences of under one, so
+    # that log p is a number of fp32
+    x = torch.rand((3, 20000), generator=torch.Generator().manual_seed(15)).to(dtype)
+    x[1] = 0
+    x[2] = -0.25
+    x[2, 17777] = 0
+    _check(x, torch.tensor([4, 5, 17777], dtype=torch.int32), 3, TINY)
