@@ -445,7 +445,10 @@ void k_token_logprobs(ScoreArgs a, int segments, Part* parts, uint64_t* part_key
     const float log_s = __builtin_amdgcn_logf(s);  // log2
     const float log_true = log_s - Reference(m, k).left(k);
     auto logprob = [&](float v) {
-        return v == -INFINITY ? v : (v - m) * a.scale - log_true * kLn2;
+        if (v == -INFINITY) return v;
+        float y = (v - m) * a.scale;
+        if (v - m == -INFINITY) y = (0.5f * v - 0.5f * m) * a.scale * 2.f;  // its half is a number
+        return y - log_true * kLn2;
     };
     if (tid == 0) {
         a.logprob[r] = !ok ? NAN : has ? logprob(xt) : -INFINITY;

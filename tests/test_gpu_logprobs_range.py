@@ -105,3 +105,14 @@ def test_temperatures_whose_inverse_is_nearly_too_large(dtype):
     x[2] = -0.25
     x[2, 17777] = 0
     _check(x, torch.tensor([4, 5, 17777], dtype=torch.int32), 3, TINY)
+
+
+@pytest.mark.parametrize("vocab", (600, 20000))
+def test_differences_past_the_largest_number(vocab):
+    # x - max is -6e38, and so no number, but log p is: -12 and the like
+    x = 3e38 * (2 * torch.rand((4, vocab), generator=torch.Generator().manual_seed(16)) - 1)
+    x[1, :vocab // 2], x[1, vocab // 2:] = 3e38, -3e38
+    x[2] = torch.finfo(torch.float32).min
+    x[2, 3] = torch.finfo(torch.float32).max
+    t = torch.tensor([7, vocab - 1, 9, 11], dtype=torch.int32)
+    _check(x, t, 5, float(torch.tensor(5e37)))
