@@ -420,7 +420,9 @@ headkv_status headkv_paged_attn_plan(const headkv_paged_config* cfg,
  * lse = -infinity.  fp32 sums, and weights of 24 bits.
  * workspace: device, 256-byte aligned, headkv_paged_attn_plan bytes, zeroed by
  * the caller before its first use; any calls may use it one after the other
- * (every launch leaves its counters zero), calls that overlap need one each. */
+ * (every launch leaves its counters zero), calls that overlap need one each.
+ * HEADKV_ERR_UNSUPPORTED for prefixes of 2^31 pieces (of 256 to 2048 tokens and 16 or 256
+ * queries) and more. */
 headkv_status headkv_paged_attn(const headkv_paged_config* cfg, const void* pool,
                                 const headkv_paged_lists* own, const headkv_paged_lists* shared,
                                 const int32_t* share, const uint16_t* q, int64_t q_stride,

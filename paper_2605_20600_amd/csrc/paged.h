@@ -1,6 +1,7 @@
 // Layout of a paged cache and the launchers of its kernels (paged_cache.hip,
 // paged_attn.hip) and of the token scores (token_logprobs.hip).  Launchers
-// return a hipError_t as an int; paged_abi.cpp has validated what they get.
+// return a hipError_t as an int, or kTooLarge; paged_abi.cpp has validated what they
+// get.
 //
 // A page holds page_tokens tokens of one key/value head:
 //   K rows     [token][d]: a token's key, contiguous (FP4: dim 2 i in the low
@@ -19,6 +20,8 @@
 #include "../../include/headkv.h"
 
 namespace headkv {
+
+constexpr int kTooLarge = -1;  // more blocks than a call may launch
 
 struct PagedDims {
     int type, d, heads, group;

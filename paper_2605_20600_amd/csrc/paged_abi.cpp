@@ -20,6 +20,7 @@ headkv_status unsupported(const char* msg) { return set_error(HEADKV_ERR_UNSUPPO
 
 headkv_status hip_status(int e, const char* what) {
     if (e == 0) return HEADKV_OK;
+    if (e == kTooLarge) return unsupported("more tokens of all lists than one call takes");
     return set_error(HEADKV_ERR_HIP, std::string(what) + ": " + hipGetErrorString((hipError_t)e));
 }
 

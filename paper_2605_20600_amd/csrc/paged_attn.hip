@@ -75,7 +75,7 @@ struct AttnCall {
     int own_chunk, own_parts;        // tokens of a chunk, chunks at most
     int shared_chunk, shared_parts;  // (0: no shared lists)
     int tiles;                       // column tiles in the grid, per shared list
-    int shared_blocks;               // of the launch, before those of own lists
+    int shared_block0, shared_blocks;  // of this launch, before those of own lists
 };
 
 __device__ __forceinline__ u32x4_t nt16(const char* p) {
@@ -890,7 +890,7 @@ void k_attn_with_shared(AttnCall a) {
     extern __shared__ __align__(16) float lds[];  // join_bytes(D, 16)
     __shared__ SharedLds ints;
     const int block = blockIdx.x;
-    if (block < a.shared_blocks) shared_block<TYPE, D>(a, block, lds, ints);
+    if (block < a.shared_blocks) shared_block<TYPE, D>(a, a.shared_block0 + block, lds, ints);
     else own_block<TYPE, D, true, W>(a, block - a.shared_blocks, lds, ints.found);
 }
 
@@ -1031,7 +1031,8 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lists = a.shared.lists * a.c.heads;
     const int per_tile = lists * a.shared_parts;
-    const int tile0 = blockIdx.x / per_tile, item = blockIdx.x % per_tile;
+    const int block = a.shared_block0 + blockIdx.x;
+    const int tile0 = block / per_tile, item = block % per_tile;
     const int lh = item % lists, chunk = item / lists;
     const int list = lh / a.c.heads, h = lh % a.c.heads, group = a.c.group;
     const Span s = span_of(a.shared, a.c.ptok, lh, a.shared_chunk);
@@ -1213,8 +1214,8 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
 template <int TYPE, int D>
 int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
     const int lists = a.own.lists * a.c.heads;
-    // (fewer than 2^32 threads in a launch)
-    constexpr int64_t kMost = 1 << 23;
+    // (a launch has fewer than 2^32 threads)
+    constexpr int64_t kMost = (1ll << 31) / kThreads, kWideMost = (1ll << 31) / kWideThreads;
     const int most = (int)std::max<int64_t>(1, std::min<int64_t>(kCounters, kMost / a.own_parts));
     auto own_blocks = [&] {
         const int64_t units = (int64_t)a.lists * a.own_parts;
@@ -1222,19 +1223,25 @@ int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
     };
     if (a.shared_parts) {
         const int64_t blocks = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * a.tiles;
-        if (blocks > kMost) return (int)hipErrorInvalidValue;
-        if (wide) {
-            k_attn_shared_wide<TYPE, D><<<(unsigned)blocks, kWideThreads, 0, st>>>(a);
-        } else {
-            // with the own lists, where one launch holds them
-            a.shared_blocks = (int)blocks;
+        if (blocks >= 1ll << 31) return kTooLarge;
+        if (!wide) {  // with the own lists, where one launch holds them all
             a.lists = lists <= most ? lists : 0;
-            const unsigned grid = (unsigned)(blocks + own_blocks());
-            const size_t lds = join_bytes(D, 16);
-            if (single) k_attn_with_shared<TYPE, D, 1><<<grid, kThreads, lds, st>>>(a);
-            else k_attn_with_shared<TYPE, D, kWaves><<<grid, kThreads, lds, st>>>(a);
+            if (blocks + own_blocks() > kMost) a.lists = 0;
         }
-        if (int e = (int)hipGetLastError()) return e;
+        const int64_t part = wide ? kWideMost : kMost;
+        for (int64_t b0 = 0; b0 < blocks; b0 += part) {
+            a.shared_block0 = (int)b0;
+            a.shared_blocks = (int)std::min(blocks - b0, part);
+            if (wide) {
+                k_attn_shared_wide<TYPE, D><<<a.shared_blocks, kWideThreads, 0, st>>>(a);
+            } else {
+                const unsigned grid = (unsigned)(a.shared_blocks + own_blocks());
+                const size_t lds = join_bytes(D, 16);
+                if (single) k_attn_with_shared<TYPE, D, 1><<<grid, kThreads, lds, st>>>(a);
+                else k_attn_with_shared<TYPE, D, kWaves><<<grid, kThreads, lds, st>>>(a);
+            }
+            if (int e = (int)hipGetLastError()) return e;
+        }
         if (a.lists) return 0;
     }
     for (int l0 = 0; l0 < lists; l0 += most) {

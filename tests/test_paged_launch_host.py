@@ -1,0 +1,92 @@
+"""Grids of the paged calls at their limits (no GPU): libheadkv.so over
+tests/host/fake_launch.cpp, which notes launches instead of making them."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2605_20600_amd import binding as B
+from paper_2605_20600_amd.build import ROOT
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+U = B.HEADKV_ERR_UNSUPPORTED
+
+RUN = """
+import ctypes, sys
+fake = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
+from paper_2605_20600_amd import binding as B
+FAKE = 0x7F0000000000
+L = B.load_paged()
+
+def cfg(**kw):
+    base = dict(kv_type=B.HEADKV_KV_INT8, head_dim=64, kv_heads=1, group=1, page_tokens=256,
+                num_pages=100)
+    return B.PagedConfig(**{**base, **kw})
+
+def lists(n, max_pages=1, max_len=256):
+    return B.PagedListsArg(FAKE, FAKE, None, None, n, max_pages, 0, max_len)
+
+def attn(c, own, shared):
+    return L.headkv_paged_attn(c, FAKE, own, shared, FAKE, FAKE, 0, FAKE, None, FAKE, 1 << 62, None)
+
+def write(c, n, tokens):
+    return L.headkv_paged_write(c, FAKE, lists(n), FAKE, FAKE, 0, 0, 0, tokens, None, None)
+
+def read(c, tokens, n=1):
+    return L.headkv_paged_read(c, FAKE, lists(n), 0, tokens, FAKE, FAKE, 128, 128, 128, None)
+
+print(eval(sys.argv[2]))
+for i in range(fake.fake_launches()):
+    g, b = ctypes.c_uint(), ctypes.c_uint()
+    fake.fake_launch(i, ctypes.byref(g), ctypes.byref(b))
+    print(g.value, b.value)
+"""
+
+
+@pytest.fixture(scope="module")
+def call(tmp_path_factory):
+    lib = tmp_path_factory.mktemp("fake") / "fake_launch.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-I",
+                    os.path.join(ROCM, "include"), os.path.join(HERE, "host", "fake_launch.cpp"),
+                    "-o", str(lib)], check=True)
+
+    def run(expr):
+        """The call's status, and (blocks, threads of one) of its launches."""
+        out = subprocess.run([sys.executable, "-c", RUN, str(lib), expr], check=True, cwd=ROOT,
+                             stdout=subprocess.PIPE, text=True).stdout.split()
+        n = [int(x) for x in out]
+        return n[0], list(zip(n[1::2], n[2::2]))
+    return run
+
+
+def test_few_and_many(call):
+    # that launches are seen at all: 3 own lists, then with a prefix of two chunks
+    st, got = call("attn(cfg(), lists(3), lists(1, 2, 512))")
+    assert st == B.HEADKV_OK and len(got) == 1 and got[0] == (5, 256)
+    st, got = call("write(cfg(), 3, 9)")
+    assert st == B.HEADKV_OK and got == [(1, 256)]
+
+
+# Blocks of the prefixes, by chunks and tiles of columns, and of own lists (four short
+# ones to a block): 2^24 and 2^23 prefixes of a chunk, the latter also beside own lists
+# that take 2^23 blocks; then blocks of 512 threads for many columns.
+@pytest.mark.parametrize("expr,shared,own", (
+    ("attn(cfg(kv_heads=1024), lists(1), lists(1 << 14))", 1 << 24, 1 << 10),
+    ("attn(cfg(kv_heads=1024), lists(64), lists(1 << 13))", 1 << 23, 1 << 14),
+    ("attn(cfg(kv_heads=1024), lists(64, 512, 1 << 17), lists(1 << 13))", 1 << 23, 1 << 23),
+    ("attn(cfg(kv_heads=4, group=16), lists(1 << 17), lists(1, 1 << 12, 1 << 20))", 1 << 24, 1 << 17),
+    ("attn(cfg(kv_heads=4, group=16), lists(1 << 18), lists(1, 1 << 13, 1 << 21))", 1 << 26, 1 << 18),
+    ("attn(cfg(kv_heads=64, group=16), lists(1 << 17), lists(1, 1 << 8, 1 << 16))", 1 << 24, 1 << 21),
+))
+def test_shared_prefixes_of_any_number(call, expr, shared, own):
+    st, got = call(expr)
+    assert st == B.HEADKV_OK
+    assert all(g * b < 1 << 32 for g, b in got), got
+    assert sum(g for g, _ in got) == shared + own, got
+
+
+def test_shared_prefixes_past_the_limit(call):
+    st, got = call("attn(cfg(kv_heads=64, group=16), lists(1 << 18), lists(1 << 18, 1 << 20, 1 << 28))")
+    assert st == U and not got
