@@ -384,7 +384,9 @@ headkv_status headkv_paged_plan(const headkv_paged_config* cfg, size_t* page_byt
  * head h) starts list_stride l + token_stride i + head_stride h elements on,
  * strides >= 0 and multiples of 8.  Tokens past the table and on dropped pages
  * are not stored.  No length changes: the next calls pass a larger extra, or
- * other lengths.  Lists must not share a page that this call writes. */
+ * other lengths.  Lists must not share a page that this call writes.  lists *
+ * kv_heads * (tokens / 8 + 2) may be 2^25; calls of four times that and more get
+ * HEADKV_ERR_UNSUPPORTED. */
 headkv_status headkv_paged_write(const headkv_paged_config* cfg, void* pool,
                                  const headkv_paged_lists* lists, const uint16_t* k,
                                  const uint16_t* v, int64_t list_stride, int64_t token_stride,
@@ -394,7 +396,7 @@ headkv_status headkv_paged_write(const headkv_paged_config* cfg, void* pool,
 /* Reads back, rounded to bf16 (FP4 and BF16 values are bf16 numbers): row (l, i,
  * h) of k and v, laid out as for headkv_paged_write, receives token begin + i,
  * or with begin < 0 token len + extra + begin + i, of list (l, h); zeros where
- * the list has no such token. */
+ * the list has no such token.  As many tokens as for headkv_paged_write. */
 headkv_status headkv_paged_read(const headkv_paged_config* cfg, const void* pool,
                                 const headkv_paged_lists* lists, int32_t begin, int32_t tokens,
                                 uint16_t* k, uint16_t* v, int64_t list_stride,

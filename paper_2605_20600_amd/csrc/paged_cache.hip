@@ -424,7 +424,7 @@ template <int D>
 int grid_of(const PagedLists& l, int heads, int blocks, unsigned* grid) {
     const int64_t n = (int64_t)l.lists * heads * blocks;
     const int64_t g = (n + kThreads / (D / 2) - 1) / (kThreads / (D / 2));
-    if (g >= 1 << 24) return (int)hipErrorInvalidValue;  // 2^32 threads: more than a launch has
+    if (g >= 1 << 24) return kTooLarge;  // 2^32 threads: more than a launch has
     *grid = (unsigned)g;
     return 0;
 }
@@ -434,8 +434,7 @@ int write_launch(const PagedDims& c, char* pool, const PagedLists& l, const uint
                  const uint16_t* v, const PagedRows& r, int tokens, const int32_t* counts,
                  void* stream) {
     unsigned grid;
-    if (tokens <= kFew) {
-        if (int e = grid_of<D>(l, c.heads, tokens, &grid)) return e;
+    if (tokens <= kFew && grid_of<D>(l, c.heads, tokens, &grid) == 0) {
         k_paged_write_few<TYPE, D><<<grid, kThreads, 0, (hipStream_t)stream>>>(c, pool, l, k, v, r,
                                                                                tokens, counts);
         return (int)hipGetLastError();

@@ -90,3 +90,20 @@ def test_shared_prefixes_of_any_number(call, expr, shared, own):
 def test_shared_prefixes_past_the_limit(call):
     st, got = call("attn(cfg(kv_heads=64, group=16), lists(1 << 18), lists(1 << 18, 1 << 20, 1 << 28))")
     assert st == U and not got
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_tokens_of_as_many_lists_as_there_may_be(call, d):
+    for tokens in (1, 4, 5):
+        st, got = call(f"write(cfg(head_dim={d}, kv_heads=1024), 1 << 14, {tokens})")
+        assert st == B.HEADKV_OK and len(got) == 1 and got[0][0] * got[0][1] < 1 << 32
+    st, got = call(f"write(cfg(head_dim={d}), 1, (1 << 28) - 64)")
+    assert st == B.HEADKV_OK and got[0][0] * got[0][1] < 1 << 32
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_too_many_tokens_for_a_call(call, d):
+    for expr in ("write(cfg(head_dim={d}), 1, (1 << 31) - 1)", "read(cfg(head_dim={d}), (1 << 31) - 1)",
+                 "write(cfg(head_dim={d}, kv_heads=1024), 1 << 14, 64)"):
+        st, got = call(expr.format(d=d))
+        assert st == U and not got
