@@ -114,6 +114,12 @@ def generate(decoder: Decoder, prompt: torch.Tensor, images: int, steps: int, kv
     Returns "tokens" [steps][images] with their "logprob" and "entropy", with top > 0
     the alternatives' "top_logprob" and "top_index" [steps][images][top], and
     "order": the images, the most probable first."""
+    with torch.cuda.device(prompt.device):
+        return _generate(decoder, prompt, images, steps, kv, temperature, top, seed)
+
+
+def _generate(decoder: Decoder, prompt: torch.Tensor, images: int, steps: int, kv: str,
+              temperature: float, top: int, seed: int) -> Dict[str, torch.Tensor]:
     s = decoder.shape
     device = prompt.device
     cache = PagedKV(kv, s.head_dim, s.kv_heads, _pages(s, len(prompt), images, steps),

@@ -2,7 +2,8 @@
 prefixes that rows share, and the scores of sampled tokens.
 
 PyTorch supplies device memory and the stream, as for Session; every
-computation is a call into libheadkv.so through the binding.
+computation is a call into libheadkv.so through the binding.  Calls are made on the
+current device and its current stream; tensors that lie elsewhere are refused.
 """
 from __future__ import annotations
 
@@ -12,12 +13,29 @@ from typing import Dict, List, Optional, Tuple
 import torch
 
 from . import binding as B
-from .session import Session, _ptr
+from .session import _ptr
 
 
-def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on the GPU, "
+# torch's public calls where a torch has no such private ones, which cost less (see
+# Session.stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _stream(index: int) -> int:
+    """The current stream, of device `index`."""
+    if _current_device() != index:
+        raise ValueError(f"tensors on cuda:{index}, but the current device is "
+                         f"cuda:{_current_device()}")
+    return _raw_stream(index)
+
+
+def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str, index: int) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.shape != shape or t.get_device() != index or index < 0 \
+            or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on "
+                         f"{'a GPU' if index < 0 else f'cuda:{index}'}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
 
@@ -44,10 +62,11 @@ class Lists:
         if pages.dim() != 3:
             raise ValueError("pages must be [lists][kv_heads][max_pages]")
         n, heads, per = pages.shape
+        self.index = at = pages.get_device()
         # kept alive with the pointers into them
-        self.pages = _device_int32(pages, (n, heads, per), "pages")
-        self.length = None if length is None else _device_int32(length, (n, heads), "length")
-        self.first = None if first is None else _device_int32(first, (n, heads), "first")
+        self.pages = _device_int32(pages, (n, heads, per), "pages", at)
+        self.length = None if length is None else _device_int32(length, (n, heads), "length", at)
+        self.first = None if first is None else _device_int32(first, (n, heads), "first", at)
         # longest first: a list that starts late makes the others wait for it (64 x 32
         # lists of 64 to 1024 tokens: 50 us in the order of their numbers, 38 so)
         self.order = None
@@ -79,8 +98,8 @@ class PagedKV:
                                  num_pages)
         self.kv_heads, self.head_dim, self.heads = kv_heads, head_dim, kv_heads * group
         self.page_bytes, pool_bytes = B.headkv_paged_plan(self.cfg)
-        self.device = device
         self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=device)
+        self.device, self.index = self.pool.device, self.pool.get_device()
         self._ws: Optional[torch.Tensor] = None
         self._replaced: List[torch.Tensor] = []  # graphs may hold calls that use them
         self._planned = None
@@ -88,38 +107,39 @@ class PagedKV:
     def lists(self, pages: torch.Tensor, length: Optional[torch.Tensor], max_len: int,
               first: Optional[torch.Tensor] = None, extra: int = 0) -> Lists:
         got = Lists(pages, length, max_len, first, extra)
-        self._check_heads(got)
+        self._check_lists(got)
         return got
 
-    def _check_heads(self, lists: Lists) -> None:
+    def _check_lists(self, lists: Lists) -> None:
         if lists.kv_heads != self.kv_heads:
             raise ValueError(f"lists of {lists.kv_heads} kv heads for a cache of {self.kv_heads}")
+        if lists.index != self.index:
+            raise ValueError(f"lists on cuda:{lists.index} for a cache on {self.device}")
 
     def _rows(self, k, v, lists: Lists) -> Tuple[int, Tuple[int, int, int]]:
         shape, ks = k.shape, k.stride()
         if v.stride() != ks or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 \
                 or v.shape != shape or len(shape) != 4 or ks[3] != 1 \
-                or not (k.is_cuda and v.is_cuda):
+                or k.get_device() != self.index or v.get_device() != self.index:
             ks = self._check_rows(k, v)
         n, tokens, heads, d = shape
         if n != lists.n or heads != self.kv_heads or d != self.head_dim:
             raise ValueError(f"k and v must be [{lists.n}][tokens][{self.kv_heads}]"
                              f"[{self.head_dim}], got {tuple(shape)}")
-        if lists.kv_heads != heads:
-            self._check_heads(lists)
+        if lists.kv_heads != heads or lists.index != self.index:
+            self._check_lists(lists)
         if n == 1 or tokens == 1 or heads == 1:
             # the stride of a dimension of one is never used, and may be anything
             return tokens, (ks[0] if n > 1 else 0, ks[1] if tokens > 1 else 0,
                             ks[2] if heads > 1 else 0)
         return tokens, ks[:3]
 
-    @staticmethod
-    def _check_rows(k, v):
+    def _check_rows(self, k, v):
         for t in (k, v):
             if t.dim() != 4 or t.dtype != torch.bfloat16 or t.shape != k.shape \
-                    or t.stride(3) != 1 or not t.is_cuda:
+                    or t.stride(3) != 1 or t.get_device() != self.index:
                 raise ValueError("k and v must be bf16 [lists][tokens][kv_heads][head_dim] with "
-                                 "contiguous rows on the GPU, got "
+                                 f"contiguous rows on {self.device}, got "
                                  f"{t.dtype} {tuple(t.shape)} on {t.device}")
         for i in range(3):
             if k.shape[i] > 1 and k.stride(i) != v.stride(i):
@@ -132,9 +152,9 @@ class PagedKV:
         behind the lists' tokens; counts: int32 [lists], tokens of each list."""
         tokens, strides = self._rows(k, v, lists)
         if counts is not None:
-            _device_int32(counts, (lists.n,), "counts")
+            _device_int32(counts, (lists.n,), "counts", self.index)
         B.headkv_paged_write(self.cfg, self.pool.data_ptr(), lists.arg, k.data_ptr(),
-                             v.data_ptr(), strides, tokens, _ptr(counts), Session.stream())
+                             v.data_ptr(), strides, tokens, _ptr(counts), _stream(self.index))
 
     def read(self, lists: Lists, tokens: int, begin: int = 0, k: Optional[torch.Tensor] = None,
              v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -149,7 +169,7 @@ class PagedKV:
         if got != tokens:
             raise ValueError(f"k and v hold {got} tokens, {tokens} are read")
         B.headkv_paged_read(self.cfg, self.pool.data_ptr(), lists.arg, begin, tokens,
-                            k.data_ptr(), v.data_ptr(), strides, Session.stream())
+                            k.data_ptr(), v.data_ptr(), strides, _stream(self.index))
         return k, v
 
     def _workspace(self, own: Lists, shared: Optional[Lists]) -> torch.Tensor:
@@ -182,28 +202,31 @@ class PagedKV:
         stride) over the rows' own lists and the shared ones that `share` (int32
         [batch], list number or -1) names; fp32 out, and lse if given."""
         batch, heads, d = own.n, self.heads, self.head_dim
-        if q.dtype != torch.bfloat16 or q.shape != (batch, heads, d) or not q.is_cuda:
-            raise ValueError(f"q must be bf16 {(batch, heads, d)} on the GPU")
+        if q.dtype != torch.bfloat16 or q.shape != (batch, heads, d) \
+                or q.get_device() != self.index:
+            raise ValueError(f"q must be bf16 {(batch, heads, d)} on {self.device}")
         row, step, one = q.stride()
         if one != 1 or (step != d and heads > 1):
             raise ValueError("q must have contiguous rows")
         if out is None:
             out = torch.empty((batch, heads, d), dtype=torch.float32, device=self.device)
-        elif out.dtype != torch.float32 or out.shape != (batch, heads, d) or not out.is_cuda \
-                or not out.is_contiguous():
-            raise ValueError(f"out must be contiguous float32 {(batch, heads, d)} on the GPU")
+        elif out.dtype != torch.float32 or out.shape != (batch, heads, d) \
+                or out.get_device() != self.index or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous float32 {(batch, heads, d)} on {self.device}")
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads)
-                                or not lse.is_cuda or not lse.is_contiguous()):
-            raise ValueError(f"lse must be contiguous float32 {(batch, heads)} on the GPU")
-        if own.kv_heads != self.kv_heads or (shared and shared.kv_heads != self.kv_heads):
-            raise ValueError(f"lists of other than {self.kv_heads} kv heads")
+                                or lse.get_device() != self.index or not lse.is_contiguous()):
+            raise ValueError(f"lse must be contiguous float32 {(batch, heads)} on {self.device}")
+        for l in (own,) if shared is None else (own, shared):
+            if l.kv_heads != self.kv_heads or l.index != self.index:
+                self._check_lists(l)
         if share is not None:
-            _device_int32(share, (batch,), "share")
+            _device_int32(share, (batch,), "share", self.index)
+        stream = _stream(self.index)
         ws = self._workspace(own, shared)
         B.headkv_paged_attn(self.cfg, self.pool.data_ptr(), own.arg,
                             None if shared is None else shared.arg, _ptr(share), q.data_ptr(),
                             row if batch > 1 else 0, out.data_ptr(), _ptr(lse), ws.data_ptr(),
-                            ws.numel(), Session.stream())
+                            ws.numel(), stream)
         return out
 
 
@@ -222,26 +245,26 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
     [rows][top]."""
     if top < 0:
         raise ValueError("top must be >= 0")
-    if logits.dim() != 2 or logits.dtype not in _LOGITS or logits.stride(1) != 1 \
-            or not logits.is_cuda:
+    index = logits.get_device()
+    if logits.dim() != 2 or logits.dtype not in _LOGITS or logits.stride(1) != 1 or index < 0:
         raise ValueError("logits must be bf16 or float32 [rows][vocab] with contiguous rows on "
                          "the GPU")
     rows, vocab = logits.shape
-    _device_int32(tokens, (rows,), "tokens")
+    _device_int32(tokens, (rows,), "tokens", index)
+    stream = _stream(index)
     dev = logits.device
     # one allocation for all results: an empty tensor costs 1.3 us of the 4 that the
     # call itself takes, a view of one 0.4
     many = rows * top
     buf = torch.empty(3 * rows + 2 * many, dtype=torch.float32, device=dev)
     if top > 0:
-        logprob, entropy, rank, best, index = buf.split_with_sizes((rows, rows, rows, many, many))
+        logprob, entropy, rank, best, which = buf.split_with_sizes((rows, rows, rows, many, many))
         res = {"logprob": logprob, "entropy": entropy, "rank": rank.view(torch.int32),
                "top_logprob": best.view(rows, top),
-               "top_index": index.view(torch.int32).view(rows, top)}
+               "top_index": which.view(torch.int32).view(rows, top)}
     else:
         logprob, entropy, rank = buf.split_with_sizes((rows, rows, rows))
         res = {"logprob": logprob, "entropy": entropy, "rank": rank.view(torch.int32)}
-    stream = Session.stream()
     need = _score_need(rows, vocab, top)
     ws = None
     if need:
@@ -249,7 +272,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
             # the graph's memory, zeroed by it: graphs may be replayed on other streams
             ws = _new_workspace(need, dev)
         else:
-            key = (dev.index or 0, stream)
+            key = (index, stream)
             ws = _score_ws.get(key)
             if ws is None or ws.numel() < need:
                 ws = _score_ws[key] = _new_workspace(need, dev)
@@ -257,6 +280,6 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0,
                             logits.stride(0) if rows > 1 else vocab, tokens.data_ptr(),
                             temperature, top, logprob.data_ptr(), entropy.data_ptr(),
                             rank.data_ptr(), best.data_ptr() if top > 0 else None,
-                            index.data_ptr() if top > 0 else None, _ptr(ws),
+                            which.data_ptr() if top > 0 else None, _ptr(ws),
                             0 if ws is None else ws.numel(), stream)
     return res
