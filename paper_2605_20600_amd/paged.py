@@ -186,7 +186,10 @@ class PagedKV:
             most.append(a)
         need = B.headkv_paged_attn_plan(self.cfg, *most)
         if self._ws is None or need > self._ws.numel():
-            ws = _new_workspace(need, self.device)
+            # twice the last at least: those that are kept take no more than the one in
+            # use, however often a table grows
+            least = 0 if self._ws is None else 2 * self._ws.numel()
+            ws = _new_workspace(max(need, least), self.device)
             if torch.cuda.is_current_stream_capturing():
                 return ws  # the graph's memory, zeroed by it: for this call only
             if self._ws is not None:
