@@ -1170,9 +1170,13 @@ struct Split {
     int tiles;
     // Own lists: a wavefront each, not a block, where they are many and short, so that
     // what a list costs however short it is (four loads that wait for each other) is paid
-    // for four at a time.  A block and a wavefront, INT8, d = 128, us: 1024 lists of up to
-    // 16 tokens 8.9 and 6.4, 128 tokens 9.1 and 10.6; 2048 of 128 14.7 and 11.4, 512 25
-    // and 32; 4096 of 128 25 and 18, 512 44 and 41, 1024 70 and 78; 12288 of 128 73 and 42.
+    // for four at a time.  A block and a wavefront, tokens from memory, lengths from an
+    // eighth of the longest on, us: INT8, d = 128, 512 lists of up to 32 tokens 5.5 and
+    // 5.5, 64 6.5 and 7.3; 1024 of 64 9.3 and 8.2, 96 9.8 and 9.8, 128 10.6 and 11.5; 2048
+    // of 128 16.5 and 15.1, 256 22.2 and 21.3; 4096 of 512 61.5 and 61.6; 12288 of 128 77
+    // and 55, 1536 481 and 455; FP4, d = 64, 1024 of 64 5.6 and 5.5, 96 6.0 and 6.6; 2048 of
+    // 256 12.4 and 12.9; 4096 of 512 27.8 and 24.8; BF16, d = 128, 512 of 32 5.7 and 6.5, 1024
+    // of 64 11.0 and 9.7; 2048 of 192 28.7 and 28.3, 256 33.4 and 35.2.
     bool single;
     // offsets, and the total
     size_t ml, part, shared_ml, shared_part, bytes;
@@ -1185,7 +1189,7 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     const int64_t own_want = wanted(2 * kCus, lists);
     s.own_chunk = chunk_of(own.max_len, own_want, kOwnMost);
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
-    s.single = (int64_t)own.max_len * 8 <= (int64_t)lists;
+    s.single = (int64_t)own.max_len * 6 + 640 <= (int64_t)lists;
     const size_t own_most = most_parts(own.max_len, own_want, kLeastChunk, kOwnMost);
     size_t shared_most = 0;
     if (shared) {

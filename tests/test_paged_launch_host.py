@@ -107,3 +107,15 @@ def test_too_many_tokens_for_a_call(call, d):
                  "write(cfg(head_dim={d}, kv_heads=1024), 1 << 14, 64)"):
         st, got = call(expr.format(d=d))
         assert st == U and not got
+
+
+# Sizes at which one kind was measured faster than the other, or as fast: a wavefront for
+# a list (blocks of four lists), or a block.
+@pytest.mark.parametrize("lists,most,single", (
+    (1024, 64, True), (1024, 128, False), (512, 32, False), (512, 64, False), (256, 8, False),
+    (2048, 128, True), (2048, 256, False), (4096, 512, True), (12288, 128, True),
+    (4096, 1024, False)))
+def test_many_short_lists(call, lists, most, single):
+    st, got = call(f"L.headkv_paged_attn(cfg(), FAKE, lists({lists}, 16, {most}), None, None, FAKE, 0, "
+                   "FAKE, None, FAKE, 1 << 62, None)")
+    assert st == B.HEADKV_OK and got == [(lists // 4 if single else lists, 256)]
