@@ -1157,15 +1157,25 @@ struct Split {
     // as many as its share of all columns takes; a list with more has its blocks go
     // round.  Tiles of 16 columns read and convert the tokens for each tile, but run
     // beside the own lists; the wide kernel does for 256 columns, with a barrier per
-    // step.  With tiles of 16 and wide, us, own lists of up to 576 tokens: 32 heads over
-    // 2048 tokens BF16 64 columns 52 and 54, 128 89 and 87, 256 174 and 155, INT8 96
-    // columns 51 and 56, 192 93 and 91, 256 122 and 113, FP4 128 columns 54 and 55, 192 78
-    // and 73; 8 heads in groups of 4 over 16384 tokens BF16 64 columns 35 and 43, 96 51
-    // and 46, INT8 128 columns 50 and 51, 256 77 and 64, FP4 192 columns 48 and 59, 256
-    // 61 and 64.  And it takes 20 us and more however short the prefix is, so tiles of 16
-    // take what does not fill the card several times with blocks: BF16 512 columns of 2 x
-    // 4 heads over 64 tokens 12 and 19, of 8 x 4 over 2048 36 and 40, of 32 x 4 over 1000 70
-    // and 55, FP4 13 (300 tokens) and 29, 28 and 39, 47 and 48, over 2048 63 and 63.
+    // step, and takes 20 us and more however short the prefix is.  Which is faster
+    // follows from the work, in blocks of 16 columns and 256 tokens.  Time of the wide
+    // kernel over that of tiles of 16 by columns of a prefix, d = 128, 1 or 2 prefixes of
+    // 512 to 16384 tokens, 2 to 32 heads in groups of 1 to 16, own lists of up to 64 or 576
+    // tokens, all from memory:
+    //         columns  blocks 3072   4096       6144       8192       12288      16384
+    //   BF16     96     .81 - 1.14              .79 -  .96             .42 -  .66
+    //           128                .80 -  .99              .63 -  .90             .33 - .61
+    //           256                .85 - 1.11              .63 -  .83             .47 - .81
+    //           384    1.04 - 1.18              .82 - 1.01             .67 -  .82
+    //   INT8     96     .97 - 1.15             1.12 - 1.24             .89 -  .97
+    //           128                .98 - 1.22              .91 - 1.06             .71 - .85
+    //           256                .98 - 1.38              .83 -  .99             .68 - .87
+    //           384    1.00 - 1.34             1.03 - 1.20             .87 -  .97
+    //   FP4     128               1.21 - 1.36             1.04 - 1.18             .96 - 1.03
+    //           256               1.09 - 1.72             1.06 - 1.12             .85 -  .93
+    //           384    1.17 - 1.62             1.01 - 1.44            1.04 - 1.10
+    // (FP4 of 96 columns 1.2 however many blocks, 192 of 24576 blocks .87 - .93; 256 columns of
+    // FP4 over 2 x 8 lists of 16384: 109 us in tiles and 96 wide, over 8 lists 60 and 68.)
     bool wide;
     int tiles;
     // Own lists: a wavefront each, not a block, where they are many and short, so that
@@ -1196,8 +1206,8 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
         const int64_t blocks = (mean + 15) / 16 * shared->lists * c.heads *
                                parts_of(shared->max_len, kLeastChunk);  // of 16 columns, 256 tokens
-        s.wide = mean >= (c.type == kBf16 ? 96 : c.type == kInt8 ? 160 : 256) &&
-                 blocks >= (c.type == kBf16 ? 3072 : c.type == kInt8 ? 4096 : 6144);
+        s.wide = mean >= (c.type == kFp4 ? 128 : 96) &&
+                 blocks >= (c.type == kBf16 ? 4096 : c.type == kInt8 ? 8192 : 16384);
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
         const int64_t want = wanted(kCus, (int64_t)shared->lists * c.heads * s.tiles);

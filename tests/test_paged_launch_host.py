@@ -119,3 +119,20 @@ def test_many_short_lists(call, lists, most, single):
     st, got = call(f"L.headkv_paged_attn(cfg(), FAKE, lists({lists}, 16, {most}), None, None, FAKE, 0, "
                    "FAKE, None, FAKE, 1 << 62, None)")
     assert st == B.HEADKV_OK and got == [(lists // 4 if single else lists, 256)]
+
+
+# Sizes at which blocks of 512 threads, for 256 columns, were measured faster than tiles of
+# 16 columns, or slower.
+@pytest.mark.parametrize("kind,heads,group,rows,prefixes,tokens,wide", (
+    ("FP4", 8, 4, 64, 1, 16384, False), ("FP4", 8, 4, 96, 1, 16384, False),
+    ("FP4", 8, 4, 128, 2, 16384, True), ("FP4", 8, 4, 128, 1, 16384, True),
+    ("FP4", 32, 1, 96, 1, 16384, False), ("FP4", 32, 1, 256, 1, 8192, True),
+    ("INT8", 8, 4, 32, 1, 16384, False), ("INT8", 8, 4, 48, 1, 16384, False),
+    ("INT8", 32, 4, 128, 1, 2048, True), ("INT8", 32, 1, 96, 1, 16384, True),
+    ("INT8", 8, 4, 64, 1, 2048, False),
+    ("BF16", 8, 4, 24, 1, 16384, False), ("BF16", 8, 4, 32, 1, 16384, True),
+    ("BF16", 32, 1, 96, 1, 2048, False), ("BF16", 32, 1, 96, 1, 8192, True)))
+def test_prefixes_of_many_columns(call, kind, heads, group, rows, prefixes, tokens, wide):
+    st, got = call(f"attn(cfg(kv_type=B.HEADKV_KV_{kind}, head_dim=128, kv_heads={heads}, "
+                   f"group={group}), lists({rows}), lists({prefixes}, 64, {tokens}))")
+    assert st == B.HEADKV_OK and (512 in [b for _, b in got]) == wide, got
