@@ -315,8 +315,9 @@ struct Wave {
     bf16x8_t q[NB][KS];
     f32x4_t acc[NB][DB];  // block VX j + x: rows 16 of load j, dim x of each
     float m[NB], sum[NB];  // reference (log2) and sum of 2^(score - reference)
-    // A reference is a rounded product; from 2^31 on, scores less it, computed with
-    // one rounding, could pass exp2's range, so the scores are rounded like it too.
+    // A reference is a rounded product; scores less it, computed with one rounding, are
+    // off by that, half a unit in its last place: 1/2 at 2^24, 128 and so past exp2's
+    // range at 2^31.  From 2^24 on the scores are rounded like it too.
     bool far;
 
     __device__ __forceinline__ void clear() {
@@ -1175,7 +1176,9 @@ struct Split {
     //           256               1.09 - 1.72             1.06 - 1.12             .85 -  .93
     //           384    1.17 - 1.62             1.01 - 1.44            1.04 - 1.10
     // (FP4 of 96 columns 1.2 however many blocks, 192 of 24576 blocks .87 - .93; 256 columns of
-    // FP4 over 2 x 8 lists of 16384: 109 us in tiles and 96 wide, over 8 lists 60 and 68.)
+    // FP4 over 2 x 8 lists of 16384: 109 us in tiles and 96 wide, over 8 lists 60 and 68.
+    // BF16 of 3072 blocks may go either way: 96 columns of 8 heads over 16384 tokens 55 and
+    // 50, of 16 heads over 8192 57 and 65.)
     bool wide;
     int tiles;
     // Own lists: a wavefront each, not a block, where they are many and short, so that
@@ -1206,8 +1209,8 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
         const int64_t blocks = (mean + 15) / 16 * shared->lists * c.heads *
                                parts_of(shared->max_len, kLeastChunk);  // of 16 columns, 256 tokens
-        s.wide = mean >= (c.type == kFp4 ? 128 : 96) &&
-                 blocks >= (c.type == kBf16 ? 4096 : c.type == kInt8 ? 8192 : 16384);
+        s.wide = mean >= (c.type == kBf16 ? 96 : c.type == kInt8 ? 160 : 192) &&
+                 blocks >= (c.type == kBf16 ? 3072 : c.type == kInt8 ? 8192 : 16384);
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
         const int64_t want = wanted(kCus, (int64_t)shared->lists * c.heads * s.tiles);
