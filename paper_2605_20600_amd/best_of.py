@@ -114,6 +114,9 @@ def generate(decoder: Decoder, prompt: torch.Tensor, images: int, steps: int, kv
     Returns "tokens" [steps][images] with their "logprob" and "entropy", with top > 0
     the alternatives' "top_logprob" and "top_index" [steps][images][top], and
     "order": the images, the most probable first."""
+    if prompt.dim() != 1 or len(prompt) < 1 or images < 1 or steps < 1:
+        raise ValueError("prompt must be [tokens], and tokens, images and steps at least 1, got "
+                         f"{tuple(prompt.shape)}, {images} and {steps}")
     with torch.cuda.device(prompt.device):
         return _generate(decoder, prompt, images, steps, kv, temperature, top, seed)
 
