@@ -8,7 +8,7 @@ current device and its current stream; tensors that lie elsewhere are refused.
 from __future__ import annotations
 
 from functools import lru_cache
-from typing import Dict, List, Optional, Tuple
+from typing import Dict, List, Optional, Tuple, Union
 
 import torch
 
@@ -55,10 +55,15 @@ class Lists:
     lengths, and for sliding windows the first token that is attended."""
 
     def __init__(self, pages: torch.Tensor, length: Optional[torch.Tensor], max_len: int,
-                 first: Optional[torch.Tensor] = None, extra: int = 0):
+                 first: Optional[torch.Tensor] = None, extra: int = 0,
+                 order: Union[None, bool, Lists] = None):
         """pages: int32 [lists][kv_heads][max_pages], -1 for a dropped page;
         length, first: int32 [lists][kv_heads] or None; max_len: no list is
-        longer; extra: added to every length."""
+        longer; extra: added to every length.
+        order: in which attention starts the lists.  None sorts them here, longest first
+        by `length` and `first` as they are now, which costs 30 to 45 us; False leaves
+        them as they are numbered (for lists that are only written and read); another
+        Lists gives its own.  An order by other lengths costs time, not results."""
         if pages.dim() != 3:
             raise ValueError("pages must be [lists][kv_heads][max_pages]")
         n, heads, per = pages.shape
@@ -70,7 +75,14 @@ class Lists:
         # longest first: a list that starts late makes the others wait for it (64 x 32
         # lists of 64 to 1024 tokens: 50 us in the order of their numbers, 38 so)
         self.order = None
-        if length is not None and n * heads > 1:
+        if isinstance(order, Lists):
+            if (order.n, order.kv_heads, order.index) != (n, heads, at):
+                raise ValueError(f"the order of {order.n} x {order.kv_heads} lists on "
+                                 f"cuda:{order.index} for {n} x {heads} on cuda:{at}")
+            self.order = order.order
+        elif order is not None and order is not False:
+            raise ValueError("order must be None, False or Lists")
+        elif order is None and length is not None and n * heads > 1:
             tokens = length if first is None else length - first
             self.order = torch.argsort(tokens.view(-1), descending=True).to(torch.int32)
         self.arg = B.PagedListsArg(_ptr(pages), _ptr(length), _ptr(first), _ptr(self.order), n, per,
@@ -105,8 +117,9 @@ class PagedKV:
         self._planned = None
 
     def lists(self, pages: torch.Tensor, length: Optional[torch.Tensor], max_len: int,
-              first: Optional[torch.Tensor] = None, extra: int = 0) -> Lists:
-        got = Lists(pages, length, max_len, first, extra)
+              first: Optional[torch.Tensor] = None, extra: int = 0,
+              order: Union[None, bool, Lists] = None) -> Lists:
+        got = Lists(pages, length, max_len, first, extra, order)
         self._check_lists(got)
         return got
 
@@ -173,7 +186,9 @@ class PagedKV:
         return k, v
 
     def _workspace(self, own: Lists, shared: Optional[Lists]) -> torch.Tensor:
-        """Planned once for the lists' tables, for any length that they can hold."""
+        """Planned once for the lists' tables, for any length that they can hold (fp32
+        parts of every query head, of 256 to 1024 own and up to 2048 shared tokens:
+        128 rows of 32 query heads of 128 dims with tables of 131072 tokens 270 MB)."""
         key = (own.pages.shape, None if shared is None else shared.pages.shape)
         if key == self._planned:
             return self._ws
