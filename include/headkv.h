@@ -336,7 +336,8 @@ headkv_status headkv_export_retained(headkv_t h, int32_t layer, uint8_t* mask,
  *   HEADKV_KV_FP4   per 32 values a power of two s = 2^e, the smallest e >= -126
  *                   with max|x| <= 6 s, and n = x / s rounded to the nearest of
  *                   0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, ties to the
- *                   one whose last bit is 0; they stand for n s.
+ *                   one whose last bit is 0; they stand for n s.  (From 1.75 * 2^127 on
+ *                   that is 2^128, infinite.)
  * A row (FP4: 32 values) with an infinity or a NaN reads back as NaN. */
 
 #define HEADKV_KV_BF16 0
@@ -412,14 +413,18 @@ headkv_status headkv_paged_attn_plan(const headkv_paged_config* cfg,
 /* Attention of one query per batch row and query head, Eq. (1): o = softmax(q
  * K^T / sqrt(d)) V over the tokens [first, len + extra) of the row's own list
  * (batch = own->lists) and, if share[b] (int32, device) is the number of a list
- * of `shared`, those of that list, whose keys and values are read once for all
- * the rows that share it.  shared and share are both NULL or both given; a
+ * of `shared`, those of that list, whose keys and values are read once for 16 or
+ * 256 queries of the rows that share it.  shared and share are both NULL or both given; a
  * share[b] outside [0, shared->lists) shares nothing.
  * q: bf16, device, 16-byte aligned, row b at q + b q_stride (a multiple of 8, >=
  * 0), there [kv_heads * group][d].  out: [batch][kv_heads * group][d] fp32,
  * 16-byte aligned.  lse: [batch][kv_heads * group] fp32 natural log of the sum
  * of exponentials, or NULL.  A query with nothing to attend gets out = 0 and
- * lse = -infinity.  fp32 sums, and weights of 24 bits.
+ * lse = -infinity.  fp32 sums, and weights of 24 bits.  Weights are relative to a
+ * reference of up to 2^8 below the largest and summed before they are divided by their
+ * sum: values of 2^120 / tokens and more may give infinities or NaN.
+ * Work is laid out for as many rows on each list of `shared` as there are on average;
+ * lists that nobody shares leave less of it to run side by side.
  * workspace: device, 256-byte aligned, headkv_paged_attn_plan bytes, zeroed by
  * the caller before its first use; any calls may use it one after the other
  * (every launch leaves its counters zero), calls that overlap need one each.
