@@ -25,12 +25,13 @@
 // into chunks, whose parts (maximum, sum, unnormalised output) the block that brings
 // the last part of a row's list joins in their order, those of the row's prefix
 // among them.
-// One MI355X, d = 128: 64 x 32 lists of 2000 INT8 tokens 177 us, 6.0 TB/s of codes and
-// scales (a copy reads and writes 5.1), bound by the bytes; of 64 to 1024 tokens 39 us, 4.8
-// TB/s, and 1 x 32 lists of up to 2480 8.8 us, by the four loads that wait for each other
-// before the first tokens are there and the join; 32 x 8 FP4 lists of up to 16384 for 4
-// heads each 56 us, 3.9 TB/s, the vector ALU busy for 45 % and the matrix cores for 18 %
-// of the time, 2.3 of the 4 wavefronts of a SIMD there on average.
+// One MI355X, d = 128: 64 x 32 lists of 2000 INT8 tokens 187 us, 5.7 TB/s of codes and
+// scales (a copy reads and writes 5.1), BF16 334, 6.3 TB/s, bound by the bytes, FP4 116; of
+// 64 to 1024 INT8 tokens 38 us, 4.9 TB/s, and 1 x 32 lists of up to 2480 8.8 us, by the four
+// loads that wait for each other before the first tokens are there and the join; 32 x 8
+// FP4 lists of up to 16384 for 4 heads each 56 us, 3.9 TB/s, the vector ALU busy for 46 % and
+// the matrix cores for 18 % of the time, 2.4 of the 4 wavefronts of a SIMD there on
+// average.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1015,7 +1016,7 @@ struct Share {
 // each and the same tokens, whose operands they convert once for all, a share each,
 // into LDS in the order in which the lanes read them: those of the next step while
 // one is computed, from loads of the step before it.  256 columns of 2 x 8 lists of
-// 16384 FP4 tokens: 82 us, 0.84 PFLOP/s on the matrix cores (K once, V with three
+// 16384 FP4 tokens: 83 us, 0.83 PFLOP/s on the matrix cores (K once, V with three
 // pieces), which are busy for a third of the time; the vector ALU's share, the
 // exponentials and the weights' pieces, is 40 %, and the two meet at a step's barrier.
 template <int TYPE, int D>
@@ -1134,8 +1135,8 @@ constexpr int kCus = 256;
 // 59, 57, 58, 54; 32 lists of 98-2480 tokens: 256 tokens 8.5 us, 512 11; 128, a step of a
 // wavefront, 15).
 // Shared lists: as many blocks as there are CUs, beside which own lists find room (64
-// rows on a prefix of 2048 INT8 tokens: 256 blocks 58 us, 384 61, 512 63; the own lists'
-// blocks first 74).
+// rows on a prefix of 2048 INT8 tokens: 256 blocks 54.3 us, 384 53.4, 512 55.1; the own
+// lists' blocks first 70).
 constexpr int kLeastChunk = 2 * kUnit, kOwnMost = 8 * kUnit, kSharedMost = 64 * kStep;
 int chunk_of(int max_len, int64_t want, int most) {
     const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
@@ -1186,9 +1187,9 @@ struct Split {
     // for four at a time.  A block and a wavefront, tokens from memory, lengths from an
     // eighth of the longest on, us: INT8, d = 128, 512 lists of up to 32 tokens 5.5 and
     // 5.5, 64 6.5 and 7.3; 1024 of 64 9.3 and 8.2, 96 9.8 and 9.8, 128 10.6 and 11.5; 2048
-    // of 128 16.5 and 15.1, 256 22.2 and 21.3; 4096 of 512 61.5 and 61.6; 12288 of 128 77
+    // of 128 16.5 and 15.1, 256 22.2 and 21.2; 4096 of 512 61.5 and 61.6; 12288 of 128 77
     // and 55, 1536 481 and 455; FP4, d = 64, 1024 of 64 5.6 and 5.5, 96 6.0 and 6.6; 2048 of
-    // 256 12.4 and 12.9; 4096 of 512 27.8 and 24.8; BF16, d = 128, 512 of 32 5.7 and 6.5, 1024
+    // 256 12.3 and 12.9; 4096 of 512 27.8 and 24.8; BF16, d = 128, 512 of 32 5.7 and 6.5, 1024
     // of 64 11.0 and 9.7; 2048 of 192 28.7 and 28.3, 256 33.4 and 35.2.
     bool single;
     // offsets, and the total
@@ -1209,8 +1210,9 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
         const int64_t blocks = (mean + 15) / 16 * shared->lists * c.heads *
                                parts_of(shared->max_len, kLeastChunk);  // of 16 columns, 256 tokens
-        s.wide = mean >= (c.type == kBf16 ? 96 : c.type == kInt8 ? 160 : 192) &&
-                 blocks >= (c.type == kBf16 ? 3072 : c.type == kInt8 ? 8192 : 16384);
+        s.wide = c.type == kBf16   ? mean >= 96 && blocks >= 3072
+                 : c.type == kInt8 ? mean >= 96 && blocks >= (mean < 160 ? 12288 : 8192)
+                                   : mean >= 192 && blocks >= 16384;
         const int cols = s.wide ? kWideCols : 16;
         s.tiles = (int)((mean + cols - 1) / cols);
         const int64_t want = wanted(kCus, (int64_t)shared->lists * c.heads * s.tiles);

@@ -129,6 +129,7 @@ def test_many_short_lists(call, lists, most, single):
     ("FP4", 32, 1, 96, 1, 16384, False), ("FP4", 32, 1, 256, 1, 8192, True),
     ("INT8", 8, 4, 32, 1, 16384, False), ("INT8", 8, 4, 48, 1, 16384, False),
     ("INT8", 32, 4, 128, 1, 2048, True), ("INT8", 32, 1, 192, 1, 8192, True),
+    ("INT8", 32, 1, 96, 1, 16384, True), ("INT8", 32, 1, 128, 1, 8192, False),
     ("INT8", 8, 4, 64, 1, 2048, False),
     ("BF16", 8, 4, 24, 1, 16384, True), ("BF16", 8, 4, 32, 1, 16384, True),
     ("BF16", 32, 1, 96, 1, 2048, False), ("BF16", 32, 1, 96, 1, 8192, True)))
