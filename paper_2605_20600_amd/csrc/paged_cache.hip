@@ -11,8 +11,9 @@
 // One MI355X: 16 images of up to 2352 tokens, 32 heads of 128, INT8: read back (with
 // zeros past their ends) 113 us, 6.0 TB/s, bound by the bytes; written 59 us for 166 MB,
 // 2.8 TB/s, the vector ALU busy for 46 % of the time and four of five wavefronts there
-// for tokens that a short image does not have.  One token for 8 x 32 lists: 3.0 and 3.3
-// us, a launch's time.
+// for tokens that a short image does not have (BF16 64 us, FP4 53; images that are all
+// whole 191 us for 930 MB, 4.9 TB/s).  One token for 8 x 32 lists: 3.0 and 3.4 us, a
+// launch's time.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
