@@ -137,3 +137,17 @@ def test_prefixes_of_many_columns(call, kind, heads, group, rows, prefixes, toke
     st, got = call(f"attn(cfg(kv_type=B.HEADKV_KV_{kind}, head_dim=128, kv_heads={heads}, "
                    f"group={group}), lists({rows}), lists({prefixes}, 64, {tokens}))")
     assert st == B.HEADKV_OK and (512 in [b for _, b in got]) == wide, got
+
+
+@pytest.mark.parametrize("kind", ("BF16", "INT8", "FP4"))
+@pytest.mark.parametrize("rows,heads,group", ((256, 8, 1), (64, 8, 4), (40, 32, 4), (16, 2, 16), (12, 20, 13)))
+def test_workspaces_hold_every_shorter_prefix(kind, rows, heads, group):
+    # also where a longer prefix goes to the other kind of blocks
+    cfg = B.PagedConfig(getattr(B, f"HEADKV_KV_{kind}"), 128, heads, group, 64, 100)
+    for prefixes in (1, 2):
+        last = 0
+        for n in range(0, 40000, 32):
+            need = B.headkv_paged_attn_plan(cfg, B.PagedListsArg(None, None, None, None, rows, 9, 0, 576),
+                                            B.PagedListsArg(None, None, None, None, prefixes, 1000, 0, n))
+            assert need >= last, n
+            last = need
