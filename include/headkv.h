@@ -458,7 +458,8 @@ headkv_status headkv_logprobs_plan(int32_t rows, int32_t vocab, int32_t top,
  * (fp32 and int32, device; entropy and rank may be NULL, the last two are NULL if
  * top is 0).  Logits of -inf have p = 0; in a row that has no other, log p is
  * -inf and the entropy 0.  A row with a NaN or +inf gets NaN in every fp32 and
- * -1 in every int32 result.  temperature > 0.  Sums in fp32.
+ * -1 in every int32 result.  temperature > 0, it and its inverse finite; logits of any
+ * size.  Sums in fp32.
  * workspace: device, 256-byte aligned, headkv_logprobs_plan bytes, zeroed by the
  * caller before its first use; any calls may use it one after the other, calls
  * that overlap need one each. */
