@@ -470,6 +470,99 @@ headkv_status headkv_token_logprobs(const void* logits, int32_t logits_type, int
                                     int32_t* top_index, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/* ---- Norms of queries and keys with rotary positions, for a decoder whose keys are
+ * cached as they are attended: rotated, each at the position it had, whatever is
+ * evicted later.  These calls need no handle.
+ *
+ * A head's row x of d values is first normalised (or not), in fp32, by a weight w and a
+ * bias b:
+ *   HEADKV_NORM_RMS    y = x / sqrt(mean(x^2) + eps) w + b
+ *   HEADKV_NORM_LAYER  y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) w + b
+ * Then its first r = rotary_dims values turn in r / 2 pairs, pair j being (y[j],
+ * y[j + r/2]) with HEADKV_ROPE_HALF and (y[2 j], y[2 j + 1]) with HEADKV_ROPE_PAIRS:
+ *   (a, b) -> scale (a cos(t) - b sin(t), a sin(t) + b cos(t)),  t = c_j omega_j.
+ * The others stay.  With one axis c_j is the position; with two (row and column of an
+ * image) the first r / 4 pairs turn by the first coordinate, the others by the second.
+ * With n = r / axes and i = j mod n / 2, omega_j = base^(-2 i / n), changed for contexts
+ * `factor` times as long as trained:
+ *   HEADKV_SCALE_LINEAR  omega / factor
+ *   HEADKV_SCALE_BASE    base factor^(n / (n - 2)) for base (n > 2)
+ *   HEADKV_SCALE_BANDS   by m, the turns in original_len positions: omega if m >= high,
+ *                        omega / factor if m <= low, between them the mean of the two by
+ *                        how far on m is
+ * (scale is 1 but for methods that sharpen or flatten the attention with it.)  Angles are
+ * computed in 64 bits, for any int32 coordinate; results are rounded to bf16 once. */
+
+#define HEADKV_ROPE_HALF 0
+#define HEADKV_ROPE_PAIRS 1
+
+#define HEADKV_NORM_NONE 0
+#define HEADKV_NORM_RMS 1
+#define HEADKV_NORM_LAYER 2
+
+#define HEADKV_SCALE_NONE 0
+#define HEADKV_SCALE_LINEAR 1
+#define HEADKV_SCALE_BASE 2
+#define HEADKV_SCALE_BANDS 3
+
+typedef struct headkv_rotary_config {
+    int32_t head_dim;    /* d: 64 or 128 */
+    int32_t rotary_dims; /* r: a multiple of 16 in [0, d] */
+    int32_t layout;      /* HEADKV_ROPE_* */
+    int32_t axes;        /* coordinates of a position: 1 or 2 */
+    int32_t norm;        /* HEADKV_NORM_* */
+    float eps;           /* >= 0, finite */
+    float scale;         /* finite */
+    /* of headkv_rotary_plan alone: */
+    int32_t scaling;      /* HEADKV_SCALE_* */
+    int32_t original_len; /* BANDS: >= 1 */
+    double base;          /* > 0, finite */
+    double factor;        /* scaled: > 0, finite */
+    double low, high;     /* BANDS: 0 <= low < high, finite */
+} headkv_rotary_config;
+
+/* Query or key rows of a call: head h of token i of row b starts in_row b + in_token i +
+ * in_head h elements on (strides >= 0, multiples of 8; bf16, device, 16-byte aligned),
+ * and so its result in `out`.  out may be in with the same strides; else they must not
+ * overlap. */
+typedef struct headkv_rotary_rows {
+    const uint16_t* in;
+    uint16_t* out;
+    int64_t in_row, in_token, in_head;
+    int64_t out_row, out_token, out_head;
+    const float* weight; /* [d] fp32 or, if per_head, [heads][d], device, 16-byte aligned;
+                            NULL: ones */
+    const float* bias;   /* likewise; NULL: zeros.  Both are used with a norm only */
+    int32_t heads;       /* 0..65536 */
+    int32_t per_head;    /* 0 or 1 */
+} headkv_rotary_rows;
+
+/* turns [rotary_dims / 2] (host; the caller copies them to the device): omega_j / 2 pi. */
+headkv_status headkv_rotary_plan(const headkv_rotary_config* cfg, double* turns);
+
+/* Norm and rotation of the first counts[b] (int32 [rows], device; NULL: all) of `tokens`
+ * tokens of each row; what lies behind them in `out` is left as it is.  turns: device,
+ * [rotary_dims / 2]; positions: int32 [rows][tokens][axes], device (both NULL allowed if
+ * rotary_dims is 0).  q or k may be NULL or have no heads.  rows * tokens * (heads / 8 + 1)
+ * may be 2^25; calls of four times that and more get HEADKV_ERR_UNSUPPORTED. */
+headkv_status headkv_rotary(const headkv_rotary_config* cfg, const double* turns,
+                            const int32_t* positions, int32_t rows, int32_t tokens,
+                            const int32_t* counts, const headkv_rotary_rows* q,
+                            const headkv_rotary_rows* k, void* stream);
+
+/* headkv_rotary on q and k with rows = lists->lists, and headkv_paged_write of the keys
+ * that it gives and of v, in one launch: k->out is not used and k->heads must be kv_heads;
+ * q is optional, its heads any.  v: as for headkv_paged_write.  The cache holds bit for bit
+ * what the two calls would leave in it. */
+headkv_status headkv_paged_write_rotary(const headkv_paged_config* cfg, void* pool,
+                                        const headkv_paged_lists* lists,
+                                        const headkv_rotary_config* rotary, const double* turns,
+                                        const int32_t* positions, int32_t tokens,
+                                        const int32_t* counts, const headkv_rotary_rows* q,
+                                        const headkv_rotary_rows* k, const uint16_t* v,
+                                        int64_t v_list_stride, int64_t v_token_stride,
+                                        int64_t v_head_stride, void* stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* headkv_last_error(void);
 

@@ -51,6 +51,18 @@ KV_TYPES = {"bf16": HEADKV_KV_BF16, "int8": HEADKV_KV_INT8, "fp4": HEADKV_KV_FP4
 HEADKV_MAX_GROUP = 16
 HEADKV_MAX_TOP = 32
 
+HEADKV_ROPE_HALF = 0
+HEADKV_ROPE_PAIRS = 1
+ROPE_LAYOUTS = {"half": HEADKV_ROPE_HALF, "pairs": HEADKV_ROPE_PAIRS}
+HEADKV_NORM_NONE = 0
+HEADKV_NORM_RMS = 1
+HEADKV_NORM_LAYER = 2
+NORMS = {None: HEADKV_NORM_NONE, "rms": HEADKV_NORM_RMS, "layer": HEADKV_NORM_LAYER}
+HEADKV_SCALE_NONE = 0
+HEADKV_SCALE_LINEAR = 1
+HEADKV_SCALE_BASE = 2
+HEADKV_SCALE_BANDS = 3
+
 HEADKV_LOGITS_BF16 = 0
 HEADKV_LOGITS_F32 = 1
 
@@ -62,7 +74,8 @@ EXPORTED = (
     "headkv_export_retained",
     "headkv_run_steps", "headkv_timing_reserve", "headkv_timing_collect",
     "headkv_paged_plan", "headkv_paged_write", "headkv_paged_read", "headkv_paged_attn_plan",
-    "headkv_paged_attn", "headkv_logprobs_plan", "headkv_token_logprobs",
+    "headkv_paged_attn", "headkv_rotary_plan", "headkv_rotary", "headkv_paged_write_rotary",
+    "headkv_logprobs_plan", "headkv_token_logprobs",
     "headkv_last_error",
 )
 
@@ -97,6 +110,22 @@ class PagedListsArg(ctypes.Structure):
         ("order", ctypes.c_void_p), ("lists", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("extra", ctypes.c_int32),
         ("max_len", ctypes.c_int32),
     ]
+
+
+class RotaryConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rotary_dims", "layout", "axes",
+                                              "norm")]
+    _fields_ += [("eps", ctypes.c_float), ("scale", ctypes.c_float), ("scaling", ctypes.c_int32),
+                 ("original_len", ctypes.c_int32)]
+    _fields_ += [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")]
+
+
+class RotaryRowsArg(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p)]
+    _fields_ += [(n, ctypes.c_int64) for n in ("in_row", "in_token", "in_head", "out_row",
+                                               "out_token", "out_head")]
+    _fields_ += [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                 ("heads", ctypes.c_int32), ("per_head", ctypes.c_int32)]
 
 
 class HeadKVError(RuntimeError):
@@ -279,12 +308,16 @@ def load_paged() -> ctypes.CDLL:
         return L
     P, I, Z, S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int64
     cfg, lists, size = (ctypes.POINTER(t) for t in (PagedConfig, PagedListsArg, Z))
+    rot, rows = ctypes.POINTER(RotaryConfig), ctypes.POINTER(RotaryRowsArg)
     sig = {
         "headkv_paged_plan": [cfg, size, size],
         "headkv_paged_write": [cfg, P, lists, P, P, S, S, S, I, P, P],
         "headkv_paged_read": [cfg, P, lists, I, I, P, P, S, S, S, P],
         "headkv_paged_attn_plan": [cfg, lists, lists, size],
         "headkv_paged_attn": [cfg, P, lists, lists, P, P, S, P, P, P, Z, P],
+        "headkv_rotary_plan": [rot, P],
+        "headkv_rotary": [rot, P, P, I, I, P, rows, rows, P],
+        "headkv_paged_write_rotary": [cfg, P, lists, rot, P, P, I, P, rows, rows, P, S, S, S, P],
         "headkv_logprobs_plan": [I, I, I, size],
         "headkv_token_logprobs": [P, I, I, I, S, P, ctypes.c_float, I, P, P, P, P, P, P, Z, P],
     }
@@ -331,6 +364,31 @@ def headkv_paged_attn(cfg: PagedConfig, pool: int, own: PagedListsArg,
     _check(load_paged().headkv_paged_attn(cfg, pool, own, shared, share, q, q_stride, out, lse,
                                           workspace, workspace_bytes, stream),
            "headkv_paged_attn")
+
+
+def headkv_rotary_plan(cfg: RotaryConfig) -> Sequence[float]:
+    """Turns a position of each pair."""
+    turns = (ctypes.c_double * (max(cfg.rotary_dims, 0) // 2))()
+    _check(load_paged().headkv_rotary_plan(cfg, turns), "headkv_rotary_plan")
+    return list(turns)
+
+
+def headkv_rotary(cfg: RotaryConfig, turns: Optional[int], positions: Optional[int], rows: int,
+                  tokens: int, counts: Optional[int], q: Optional[RotaryRowsArg],
+                  k: Optional[RotaryRowsArg], stream: int = 0) -> None:
+    _check(load_paged().headkv_rotary(cfg, turns, positions, rows, tokens, counts, q, k, stream),
+           "headkv_rotary")
+
+
+def headkv_paged_write_rotary(cfg: PagedConfig, pool: int, lists: PagedListsArg,
+                              rotary: RotaryConfig, turns: Optional[int],
+                              positions: Optional[int], tokens: int, counts: Optional[int],
+                              q: Optional[RotaryRowsArg], k: RotaryRowsArg, v: int,
+                              v_strides: Sequence[int], stream: int = 0) -> None:
+    """v_strides: elements between lists, tokens and heads of v."""
+    _check(load_paged().headkv_paged_write_rotary(cfg, pool, lists, rotary, turns, positions,
+                                                  tokens, counts, q, k, v, *v_strides, stream),
+           "headkv_paged_write_rotary")
 
 
 def headkv_logprobs_plan(rows: int, vocab: int, top: int) -> int:

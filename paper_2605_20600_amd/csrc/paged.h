@@ -1,5 +1,5 @@
 // Layout of a paged cache and the launchers of its kernels (paged_cache.hip,
-// paged_attn.hip) and of the token scores (token_logprobs.hip).  Launchers
+// paged_attn.hip, rotary.hip) and of the token scores (token_logprobs.hip).  Launchers
 // return a hipError_t as an int, or kTooLarge; paged_abi.cpp has validated what they
 // get.
 //
@@ -61,6 +61,34 @@ size_t paged_attn_workspace(const PagedDims& c, const PagedLists& own, const Pag
 int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& own,
                       const PagedLists* shared, const int32_t* share, const uint16_t* q,
                       int64_t q_stride, float* out, float* lse, void* ws, void* stream);
+
+// Queries or keys of the rotary kernel.
+struct RotaryRows {
+    const uint16_t* in;
+    uint16_t* out;
+    PagedRows from, to;
+    const float* weight;
+    const float* bias;
+    int heads, step;  // elements from a head's weights to the next's: 0 or d
+};
+struct RotaryArgs {
+    RotaryRows q, k;
+    const double* turns;
+    const int32_t* positions;
+    const int32_t* counts;
+    int d, rows, tokens;
+    int r, axes, layout, norm;
+    float eps, scale;
+};
+struct RotaryCache {  // where keys and values go
+    PagedDims c;
+    char* pool;
+    PagedLists lists;
+    const uint16_t* v;
+    PagedRows v_rows;
+};
+// cache: NULL for rows that come back as rows
+int launch_rotary(const RotaryArgs& a, const RotaryCache* cache, void* stream);
 
 struct ScoreArgs {
     const void* logits;

@@ -13,31 +13,8 @@ from typing import Dict, List, Optional, Tuple, Union
 import torch
 
 from . import binding as B
+from .rotary import NormWeights, Rotary, _device_int32, _stream, row_strides
 from .session import _ptr
-
-
-# torch's public calls where a torch has no such private ones, which cost less (see
-# Session.stream)
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
-                      lambda index: torch.cuda.current_stream(index).cuda_stream)
-
-
-def _stream(index: int) -> int:
-    """The current stream, of device `index`."""
-    if _current_device() != index:
-        raise ValueError(f"tensors on cuda:{index}, but the current device is "
-                         f"cuda:{_current_device()}")
-    return _raw_stream(index)
-
-
-def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str, index: int) -> torch.Tensor:
-    if t.dtype != torch.int32 or t.shape != shape or t.get_device() != index or index < 0 \
-            or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on "
-                         f"{'a GPU' if index < 0 else f'cuda:{index}'}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t
 
 
 def _new_workspace(need: int, device) -> torch.Tensor:
@@ -168,6 +145,32 @@ class PagedKV:
             _device_int32(counts, (lists.n,), "counts", self.index)
         B.headkv_paged_write(self.cfg, self.pool.data_ptr(), lists.arg, k.data_ptr(),
                              v.data_ptr(), strides, tokens, _ptr(counts), _stream(self.index))
+
+    def write_rotary(self, lists: Lists, rotary: Rotary, q: Optional[torch.Tensor],
+                     k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
+                     weights: Optional[NormWeights] = None,
+                     counts: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """write(), with keys that `rotary` has normalised and turned, and queries: returns
+        rotary's of q (bf16 [lists][tokens][heads][head_dim], any strides; None: none).  One
+        launch; arguments as for write() and for a call of `rotary`."""
+        n, tokens = k.shape[:2]
+        if k.shape != (lists.n, tokens, self.kv_heads, self.head_dim) or v.shape != k.shape:
+            raise ValueError(f"k and v must be [{lists.n}][tokens][{self.kv_heads}]"
+                             f"[{self.head_dim}], got {tuple(k.shape)} and {tuple(v.shape)}")
+        if q is not None and q.shape[2:] != (self.heads, self.head_dim):
+            raise ValueError(f"q must be [{lists.n}][tokens][{self.heads}][{self.head_dim}], got "
+                             f"{tuple(q.shape)}")
+        if lists.kv_heads != self.kv_heads or lists.index != self.index:
+            self._check_lists(lists)
+        call = rotary.rows(q, k, positions, weights, counts, q_out, None, cached=True)
+        if call.index != self.index:
+            raise ValueError(f"q and k on cuda:{call.index} for a cache on {self.device}")
+        B.headkv_paged_write_rotary(self.cfg, self.pool.data_ptr(), lists.arg, rotary.cfg,
+                                    _ptr(rotary.turns), _ptr(positions), tokens, _ptr(counts),
+                                    call.q, call.k, v.data_ptr(), row_strides(v, "v", self.index),
+                                    _stream(self.index))
+        return call.q_out
 
     def read(self, lists: Lists, tokens: int, begin: int = 0, k: Optional[torch.Tensor] = None,
              v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
