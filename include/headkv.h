@@ -470,6 +470,51 @@ headkv_status headkv_token_logprobs(const void* logits, int32_t logits_type, int
                                     int32_t* top_index, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/* ---- Verification of drafted tokens: which of the tokens that a smaller model (or a
+ * guess) proposes a row keeps, and the one that follows them, so that what comes out is
+ * distributed as if the target had sampled every token itself.
+ *
+ * Row r has `logits` of drafts + 1 positions (that of draft i at row_stride r +
+ * token_stride i elements, vocab values; the last follows all drafts) and with
+ * `draft_logits` the distributions that its drafts were sampled from, one for each of the
+ * `drafts` positions (NULL: each draft was certain).  With p_i = softmax(logits / T), q_i =
+ * softmax(draft logits / T), 64-bit sums, and u = uniforms [rows][drafts + 1] in [0, 1):
+ *   draft i = 0, 1, ... with token t is kept if u_i q_i(t) < p_i(t)
+ *   at the first that is not, the next token is the least v with sum over w <= v of r(w)
+ *   > u_drafts sum of r, where r = max(p_i - q_i, 0) (p_i if that sums to less than 2^-40)
+ *   if all are kept, so with r = p of the position behind them
+ * T = 0: p is 1 at the largest logit, the first of equal ones; no draft logits are read.
+ * A row's drafts end at counts[r] (int32 [rows], device, or NULL: all) and before the
+ * first token outside [0, vocab).  counts[r] < 0: the row is left out.
+ * Results (device): out_tokens [rows][drafts + 1] int32, the drafts that are kept, the next
+ * token and -1 from there on; out_count [rows] int32, how many that are; out_logprob
+ * [rows][drafts + 1] fp32 or NULL, their log p, 0 from there on.
+ * Logits of -inf have p = 0.  Where the next decision needs a position whose target logits
+ * hold a NaN or +inf or are all -inf, or whose draft logits hold a NaN or +inf, a row ends
+ * without a next token.  Draft logits that are all -inf stand for q = 0. */
+
+#define HEADKV_MAX_DRAFTS 63
+
+/* Bytes of the workspace of headkv_verify_drafts; it grows with each argument. */
+headkv_status headkv_verify_plan(int32_t rows, int32_t drafts, int32_t vocab,
+                                 size_t* workspace_bytes);
+
+/* tokens: int32 [rows][drafts], device.  logits, draft_logits: device, both of logits_type,
+ * aligned to it, strides >= 0.  drafts: 0..HEADKV_MAX_DRAFTS.  temperature: T, 0 or a number
+ * > 0, it and log2(e) / T finite.  A uniform outside [0, 1) keeps no draft (>= 1, NaN) or
+ * counts as 0 (< 0) or as the largest below 1.
+ * workspace: device, 256-byte aligned, headkv_verify_plan bytes, zeroed by the caller before
+ * its first use; any calls may use it one after the other, calls that overlap need one
+ * each. */
+headkv_status headkv_verify_drafts(const void* logits, const void* draft_logits,
+                                   int32_t logits_type, int32_t rows, int32_t drafts,
+                                   int32_t vocab, int64_t row_stride, int64_t token_stride,
+                                   int64_t draft_row_stride, int64_t draft_token_stride,
+                                   const int32_t* tokens, const int32_t* counts,
+                                   const float* uniforms, double temperature, int32_t* out_tokens,
+                                   int32_t* out_count, float* out_logprob, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
 /* ---- Norms of queries and keys with rotary positions, for a decoder whose keys are
  * cached as they are attended: rotated, each at the position it had, whatever is
  * evicted later.  These calls need no handle.

@@ -51,6 +51,8 @@ KV_TYPES = {"bf16": HEADKV_KV_BF16, "int8": HEADKV_KV_INT8, "fp4": HEADKV_KV_FP4
 HEADKV_MAX_GROUP = 16
 HEADKV_MAX_TOP = 32
 
+HEADKV_MAX_DRAFTS = 63
+
 HEADKV_ROPE_HALF = 0
 HEADKV_ROPE_PAIRS = 1
 ROPE_LAYOUTS = {"half": HEADKV_ROPE_HALF, "pairs": HEADKV_ROPE_PAIRS}
@@ -75,7 +77,7 @@ EXPORTED = (
     "headkv_run_steps", "headkv_timing_reserve", "headkv_timing_collect",
     "headkv_paged_plan", "headkv_paged_write", "headkv_paged_read", "headkv_paged_attn_plan",
     "headkv_paged_attn", "headkv_rotary_plan", "headkv_rotary", "headkv_paged_write_rotary",
-    "headkv_logprobs_plan", "headkv_token_logprobs",
+    "headkv_logprobs_plan", "headkv_token_logprobs", "headkv_verify_plan", "headkv_verify_drafts",
     "headkv_last_error",
 )
 
@@ -318,6 +320,9 @@ def load_paged() -> ctypes.CDLL:
         "headkv_rotary_plan": [rot, P],
         "headkv_rotary": [rot, P, P, I, I, P, rows, rows, P],
         "headkv_paged_write_rotary": [cfg, P, lists, rot, P, P, I, P, rows, rows, P, S, S, S, P],
+        "headkv_verify_plan": [I, I, I, size],
+        "headkv_verify_drafts": [P, P, I, I, I, I, S, S, S, S, P, P, P, ctypes.c_double, P, P,
+                                 P, P, Z, P],
         "headkv_logprobs_plan": [I, I, I, size],
         "headkv_token_logprobs": [P, I, I, I, S, P, ctypes.c_float, I, P, P, P, P, P, P, Z, P],
     }
@@ -407,3 +412,21 @@ def headkv_token_logprobs(logits: int, logits_type: int, rows: int, vocab: int, 
         logits, logits_type, rows, vocab, row_stride, tokens, temperature, top, logprob, entropy,
         rank, top_logprob, top_index, workspace, workspace_bytes, stream),
         "headkv_token_logprobs")
+
+
+def headkv_verify_plan(rows: int, drafts: int, vocab: int) -> int:
+    size = ctypes.c_size_t()
+    _check(load_paged().headkv_verify_plan(rows, drafts, vocab, size), "headkv_verify_plan")
+    return size.value
+
+
+def headkv_verify_drafts(logits: int, draft_logits: Optional[int], logits_type: int, rows: int,
+                         drafts: int, vocab: int, strides: Sequence[int], tokens: Optional[int],
+                         counts: Optional[int], uniforms: int, temperature: float,
+                         out_tokens: int, out_count: int, out_logprob: Optional[int],
+                         workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """strides: elements between rows and positions of logits, then of draft_logits."""
+    _check(load_paged().headkv_verify_drafts(
+        logits, draft_logits, logits_type, rows, drafts, vocab, *strides, tokens, counts,
+        uniforms, temperature, out_tokens, out_count, out_logprob, workspace, workspace_bytes,
+        stream), "headkv_verify_drafts")

@@ -1,5 +1,6 @@
 // Layout of a paged cache and the launchers of its kernels (paged_cache.hip,
-// paged_attn.hip, rotary.hip) and of the token scores (token_logprobs.hip).  Launchers
+// paged_attn.hip, rotary.hip), of the token scores (token_logprobs.hip) and of the
+// verification of drafted tokens (verify_drafts.hip).  Launchers
 // return a hipError_t as an int, or kTooLarge; paged_abi.cpp has validated what they
 // get.
 //
@@ -101,6 +102,21 @@ struct ScoreArgs {
     int rows, vocab, top;
     float scale;  // 1 / temperature
 };
+struct VerifyArgs {
+    const void* logits;
+    const void* draft;  // NULL: certain drafts
+    const int32_t* tokens;
+    const int32_t* counts;
+    const float* uniforms;
+    int32_t *out_tokens, *out_count;
+    float* out_logprob;
+    int64_t row, token, draft_row, draft_token;  // element strides
+    int rows, drafts, vocab;
+    double k;  // log2(e) / temperature, 0: the largest logit
+};
+size_t verify_workspace(int rows, int drafts, int vocab);
+int launch_verify(const VerifyArgs& a, int logits_type, void* ws, void* stream);
+
 size_t logprobs_workspace(int rows, int vocab, int top);
 int launch_token_logprobs(const ScoreArgs& a, int logits_type, void* ws, void* stream);
 

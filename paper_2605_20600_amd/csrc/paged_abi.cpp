@@ -126,7 +126,7 @@ headkv_status headkv_token_logprobs(const void* logits, int32_t logits_type, int
     if (headkv_status st = check_scores(rows, vocab, top)) return st;
     if (logits_type != HEADKV_LOGITS_BF16 && logits_type != HEADKV_LOGITS_F32)
         return bad("unknown logits_type");
-    if (!is_temperature(temperature))
+    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
         return bad("temperature must be > 0");
     if (row_stride < vocab) return bad("row_stride < vocab");
     if (rows == 0) return HEADKV_OK;

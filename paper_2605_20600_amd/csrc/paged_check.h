@@ -78,9 +78,6 @@ inline headkv_status check_rows(const void* k, const void* v, int64_t list, int6
     return HEADKV_OK;
 }
 
-// A temperature that softmax takes: it and its inverse are finite.
-inline bool is_temperature(float t) { return t > 0.f && std::isfinite(t) && std::isfinite(1.f / t); }
-
 inline headkv_status check_workspace(const void* ws, size_t have, size_t need) {
     if (have < need)
         return set_error(HEADKV_ERR_CAPACITY, "workspace of " + std::to_string(have) +
