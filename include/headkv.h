@@ -470,6 +470,61 @@ headkv_status headkv_token_logprobs(const void* logits, int32_t logits_type, int
                                     int32_t* top_index, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/* ---- Page tables, windows and lengths of many lists brought from one step to the next on
+ * the device, where what a row has gained is known there alone (drafted tokens).  These
+ * calls need no handle.
+ *
+ * The pages that no list holds are a ring of free_state[1] page numbers, from place
+ * free_state[0] of free_pages on.  headkv_paged_extend does for every list l (which belongs
+ * to row l mod rows: `lists` may be those of all layers of a model, layer by layer) and kv
+ * head, with ptok = page_tokens and a page being held if its number is in [0, num_pages):
+ *   advance[row] < 0   the list ends: len = first = 0, its table entries become -1, and the
+ *                      pages that it held join the ring's end
+ *   else               len += advance[row], to max_pages ptok at most
+ *   window > 0         first = max(first, len + 1 - window), and the pages that it held of
+ *                      the table's places from first's old to before its new one, first / ptok,
+ *                      join the ring's end, their entries -1
+ *   n = min(max(counts[row], 0), tokens) more tokens come next: a place from ceil(len / ptok)
+ *                      to before ceil((len + n) / ptok), and max_pages, that holds no page
+ *                      gets the one at the ring's beginning
+ * in this order for all lists: first every page that becomes free joins, in the order of the
+ * tables, then pages leave, in that order too.  Once the ring is empty places stay as they
+ * are, and free_state[2] is the number of those that got nothing (else 0).  What a list did
+ * not use of its places stays with it for the next call.
+ * order: of each layer's rows * kv_heads lists, the numbers of headkv_paged_lists' order, by
+ * len + n - first in eighths of an octave (whole numbers below 8), most first, equal ones
+ * by their number.
+ * All arrays are device memory, contiguous, int32.  A page may be in one list or in the ring
+ * once; a ring of more than num_pages pages loses those at its end. */
+
+typedef struct headkv_paged_tables {
+    int32_t* pages;        /* [lists][kv_heads][max_pages] */
+    int32_t* len;          /* [lists][kv_heads] */
+    int32_t* first;        /* [lists][kv_heads], 0 at the start */
+    int32_t* order;        /* [lists * kv_heads], or NULL: not wanted */
+    const int32_t* window; /* [lists][kv_heads] tokens that the next token attends, itself
+                              among them; 0 or less: all.  NULL: all */
+    int32_t* free_pages;   /* [num_pages] */
+    int32_t* free_state;   /* [4], the last one not used */
+    int32_t kv_heads;      /* 1..1024 */
+    int32_t page_tokens;   /* 32, 64, 128 or 256 */
+    int32_t num_pages;     /* >= 1 */
+    int32_t lists;         /* a multiple of rows; lists * kv_heads <= 2^24 */
+    int32_t rows;          /* >= 1 */
+    int32_t max_pages;     /* >= 1; lists * kv_heads * max_pages < 2^31 */
+} headkv_paged_tables;
+
+/* Bytes of the workspace of headkv_paged_extend. */
+headkv_status headkv_paged_extend_plan(const headkv_paged_tables* tables,
+                                       size_t* workspace_bytes);
+
+/* advance, counts: int32 [rows], device, or NULL (0 and `tokens` for all).  tokens: 0..2^24.
+ * workspace: device, 256-byte aligned, headkv_paged_extend_plan bytes, in any state; calls
+ * that overlap need one each. */
+headkv_status headkv_paged_extend(const headkv_paged_tables* tables, const int32_t* advance,
+                                  const int32_t* counts, int32_t tokens, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
 /* ---- Verification of drafted tokens: which of the tokens that a smaller model (or a
  * guess) proposes a row keeps, and the one that follows them, so that what comes out is
  * distributed as if the target had sampled every token itself.

@@ -77,6 +77,7 @@ EXPORTED = (
     "headkv_run_steps", "headkv_timing_reserve", "headkv_timing_collect",
     "headkv_paged_plan", "headkv_paged_write", "headkv_paged_read", "headkv_paged_attn_plan",
     "headkv_paged_attn", "headkv_rotary_plan", "headkv_rotary", "headkv_paged_write_rotary",
+    "headkv_paged_extend_plan", "headkv_paged_extend",
     "headkv_logprobs_plan", "headkv_token_logprobs", "headkv_verify_plan", "headkv_verify_drafts",
     "headkv_last_error",
 )
@@ -112,6 +113,13 @@ class PagedListsArg(ctypes.Structure):
         ("order", ctypes.c_void_p), ("lists", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("extra", ctypes.c_int32),
         ("max_len", ctypes.c_int32),
     ]
+
+
+class PagedTablesArg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "len", "first", "order", "window",
+                                               "free_pages", "free_state")]
+    _fields_ += [(n, ctypes.c_int32) for n in ("kv_heads", "page_tokens", "num_pages", "lists",
+                                               "rows", "max_pages")]
 
 
 class RotaryConfig(ctypes.Structure):
@@ -310,6 +318,7 @@ def load_paged() -> ctypes.CDLL:
         return L
     P, I, Z, S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int64
     cfg, lists, size = (ctypes.POINTER(t) for t in (PagedConfig, PagedListsArg, Z))
+    tables = ctypes.POINTER(PagedTablesArg)
     rot, rows = ctypes.POINTER(RotaryConfig), ctypes.POINTER(RotaryRowsArg)
     sig = {
         "headkv_paged_plan": [cfg, size, size],
@@ -320,6 +329,8 @@ def load_paged() -> ctypes.CDLL:
         "headkv_rotary_plan": [rot, P],
         "headkv_rotary": [rot, P, P, I, I, P, rows, rows, P],
         "headkv_paged_write_rotary": [cfg, P, lists, rot, P, P, I, P, rows, rows, P, S, S, S, P],
+        "headkv_paged_extend_plan": [tables, size],
+        "headkv_paged_extend": [tables, P, P, I, P, Z, P],
         "headkv_verify_plan": [I, I, I, size],
         "headkv_verify_drafts": [P, P, I, I, I, I, S, S, S, S, P, P, P, ctypes.c_double, P, P,
                                  P, P, Z, P],
@@ -412,6 +423,19 @@ def headkv_token_logprobs(logits: int, logits_type: int, rows: int, vocab: int, 
         logits, logits_type, rows, vocab, row_stride, tokens, temperature, top, logprob, entropy,
         rank, top_logprob, top_index, workspace, workspace_bytes, stream),
         "headkv_token_logprobs")
+
+
+def headkv_paged_extend_plan(tables: PagedTablesArg) -> int:
+    size = ctypes.c_size_t()
+    _check(load_paged().headkv_paged_extend_plan(tables, size), "headkv_paged_extend_plan")
+    return size.value
+
+
+def headkv_paged_extend(tables: PagedTablesArg, advance: Optional[int], counts: Optional[int],
+                        tokens: int, workspace: int, workspace_bytes: int,
+                        stream: int = 0) -> None:
+    _check(load_paged().headkv_paged_extend(tables, advance, counts, tokens, workspace,
+                                            workspace_bytes, stream), "headkv_paged_extend")
 
 
 def headkv_verify_plan(rows: int, drafts: int, vocab: int) -> int:

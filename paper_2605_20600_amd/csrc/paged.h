@@ -1,8 +1,8 @@
 // Layout of a paged cache and the launchers of its kernels (paged_cache.hip,
-// paged_attn.hip, rotary.hip), of the token scores (token_logprobs.hip) and of the
-// verification of drafted tokens (verify_drafts.hip).  Launchers
-// return a hipError_t as an int, or kTooLarge; paged_abi.cpp has validated what they
-// get.
+// paged_attn.hip, rotary.hip, page_tables.hip), of the token scores (token_logprobs.hip)
+// and of the verification of drafted tokens (verify_drafts.hip).  Launchers return a
+// hipError_t as an int, or kTooLarge; the entry points (paged_abi.cpp, rotary_abi.cpp,
+// drafts_abi.cpp) have validated what they get.
 //
 // A page holds page_tokens tokens of one key/value head:
 //   K rows     [token][d]: a token's key, contiguous (FP4: dim 2 i in the low
@@ -114,6 +114,10 @@ struct VerifyArgs {
     int rows, drafts, vocab;
     double k;  // log2(e) / temperature, 0: the largest logit
 };
+size_t extend_workspace();
+int launch_extend(const headkv_paged_tables& t, const int32_t* advance, const int32_t* counts,
+                  int tokens, void* ws, void* stream);
+
 size_t verify_workspace(int rows, int drafts, int vocab);
 int launch_verify(const VerifyArgs& a, int logits_type, void* ws, void* stream);
 
