@@ -436,6 +436,33 @@ headkv_status headkv_paged_attn(const headkv_paged_config* cfg, const void* pool
                                 float* out, float* lse, void* workspace, size_t workspace_bytes,
                                 void* stream);
 
+/* Attention of several new tokens of each row, written behind its list already (by
+ * headkv_paged_write with the same lists): drafted tokens, or a piece of a prompt.  Token i <
+ * tokens of row b (and i < counts[b]; int32 [batch], device, or NULL: all) attends of its own
+ * list the tokens [f, len + extra + i + 1), len + extra at most max_len, where f is `first`
+ * or, with window[b][kv head] > 0 (int32 [batch][kv_heads], device, or NULL: no windows), the
+ * larger of it and len + extra + i + 1 - window; and of `shared` as headkv_paged_attn does.
+ * q: bf16, device, 16-byte aligned, token i of row b at q + b q_row_stride + i q_token_stride
+ * (multiples of 8, >= 0), there [kv_heads * group][d].  out: [batch][tokens][kv_heads *
+ * group][d] fp32, 16-byte aligned; lse: [batch][tokens][kv_heads * group] fp32 or NULL; rows
+ * of tokens behind counts[b] are left as they are.  What else is said of headkv_paged_attn
+ * holds, the workspace's size being headkv_paged_attn_tokens_plan's, which need not grow with
+ * `tokens`.  With 16 / group (rounded down, at least 1) tokens to a cut, batch * kv_heads *
+ * cuts of a row may be 2^24, and tokens too (HEADKV_ERR_UNSUPPORTED beyond). */
+headkv_status headkv_paged_attn_tokens_plan(const headkv_paged_config* cfg,
+                                            const headkv_paged_lists* own,
+                                            const headkv_paged_lists* shared, int32_t tokens,
+                                            size_t* workspace_bytes);
+
+headkv_status headkv_paged_attn_tokens(const headkv_paged_config* cfg, const void* pool,
+                                       const headkv_paged_lists* own,
+                                       const headkv_paged_lists* shared, const int32_t* share,
+                                       int32_t tokens, const int32_t* counts,
+                                       const int32_t* window, const uint16_t* q,
+                                       int64_t q_row_stride, int64_t q_token_stride, float* out,
+                                       float* lse, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+
 /* Types of logits. */
 #define HEADKV_LOGITS_BF16 0
 #define HEADKV_LOGITS_F32 1

@@ -76,7 +76,8 @@ EXPORTED = (
     "headkv_export_retained",
     "headkv_run_steps", "headkv_timing_reserve", "headkv_timing_collect",
     "headkv_paged_plan", "headkv_paged_write", "headkv_paged_read", "headkv_paged_attn_plan",
-    "headkv_paged_attn", "headkv_rotary_plan", "headkv_rotary", "headkv_paged_write_rotary",
+    "headkv_paged_attn", "headkv_paged_attn_tokens_plan", "headkv_paged_attn_tokens",
+    "headkv_rotary_plan", "headkv_rotary", "headkv_paged_write_rotary",
     "headkv_paged_extend_plan", "headkv_paged_extend",
     "headkv_logprobs_plan", "headkv_token_logprobs", "headkv_verify_plan", "headkv_verify_drafts",
     "headkv_last_error",
@@ -326,6 +327,8 @@ def load_paged() -> ctypes.CDLL:
         "headkv_paged_read": [cfg, P, lists, I, I, P, P, S, S, S, P],
         "headkv_paged_attn_plan": [cfg, lists, lists, size],
         "headkv_paged_attn": [cfg, P, lists, lists, P, P, S, P, P, P, Z, P],
+        "headkv_paged_attn_tokens_plan": [cfg, lists, lists, I, size],
+        "headkv_paged_attn_tokens": [cfg, P, lists, lists, P, I, P, P, P, S, S, P, P, P, Z, P],
         "headkv_rotary_plan": [rot, P],
         "headkv_rotary": [rot, P, P, I, I, P, rows, rows, P],
         "headkv_paged_write_rotary": [cfg, P, lists, rot, P, P, I, P, rows, rows, P, S, S, S, P],
@@ -380,6 +383,27 @@ def headkv_paged_attn(cfg: PagedConfig, pool: int, own: PagedListsArg,
     _check(load_paged().headkv_paged_attn(cfg, pool, own, shared, share, q, q_stride, out, lse,
                                           workspace, workspace_bytes, stream),
            "headkv_paged_attn")
+
+
+def headkv_paged_attn_tokens_plan(cfg: PagedConfig, own: PagedListsArg,
+                                  shared: Optional[PagedListsArg], tokens: int) -> int:
+    size = ctypes.c_size_t()
+    _check(load_paged().headkv_paged_attn_tokens_plan(cfg, own, shared, tokens, size),
+           "headkv_paged_attn_tokens_plan")
+    return size.value
+
+
+def headkv_paged_attn_tokens(cfg: PagedConfig, pool: int, own: PagedListsArg,
+                             shared: Optional[PagedListsArg], share: Optional[int], tokens: int,
+                             counts: Optional[int], window: Optional[int], q: int,
+                             q_strides: Sequence[int], out: int, lse: Optional[int],
+                             workspace: Optional[int], workspace_bytes: int,
+                             stream: int = 0) -> None:
+    """q_strides: elements between rows and tokens of q."""
+    _check(load_paged().headkv_paged_attn_tokens(cfg, pool, own, shared, share, tokens, counts,
+                                                 window, q, *q_strides, out, lse, workspace,
+                                                 workspace_bytes, stream),
+           "headkv_paged_attn_tokens")
 
 
 def headkv_rotary_plan(cfg: RotaryConfig) -> Sequence[float]:

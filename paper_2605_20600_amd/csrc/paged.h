@@ -63,6 +63,20 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
                       const PagedLists* shared, const int32_t* share, const uint16_t* q,
                       int64_t q_stride, float* out, float* lse, void* ws, void* stream);
 
+// Several tokens of each row.
+struct PagedTokens {
+    int tokens;
+    const int32_t* counts;
+    const int32_t* window;
+    const uint16_t* q;
+    int64_t q_row, q_token;
+};
+// 0: more tokens than one call takes
+size_t paged_attn_tokens_workspace(PagedDims c, PagedLists own, const PagedLists* shared, int tokens);
+int launch_paged_attn_tokens(const PagedTokens& t, const PagedDims& c, const char* pool,
+                             const PagedLists& own, const PagedLists* shared, const int32_t* share,
+                             float* out, float* lse, void* ws, void* stream);
+
 // Queries or keys of the rotary kernel.
 struct RotaryRows {
     const uint16_t* in;

@@ -101,6 +101,63 @@ headkv_status headkv_paged_attn(const headkv_paged_config* cfg, const void* pool
                       "paged attention launch");
 }
 
+static constexpr int kMostTokens = 1 << 24;  // of a row: sums with lengths are 32-bit numbers
+
+headkv_status headkv_paged_attn_tokens_plan(const headkv_paged_config* cfg,
+                                            const headkv_paged_lists* own,
+                                            const headkv_paged_lists* shared, int32_t tokens,
+                                            size_t* workspace_bytes) {
+    PagedDims c;
+    PagedLists o, s;
+    if (headkv_status st = make_dims(cfg, &c)) return st;
+    if (headkv_status st = make_lists(c, own, false, &o)) return st;
+    if (shared)
+        if (headkv_status st = make_lists(c, shared, false, &s)) return st;
+    if (tokens < 0) return bad("tokens must be >= 0");
+    if (tokens > kMostTokens) return hip_status(kTooLarge, "");
+    if (!workspace_bytes) return bad("workspace_bytes is NULL");
+    const size_t need = paged_attn_tokens_workspace(c, o, shared ? &s : nullptr, tokens);
+    if (!need) return hip_status(kTooLarge, "");
+    *workspace_bytes = need;
+    return HEADKV_OK;
+}
+
+headkv_status headkv_paged_attn_tokens(const headkv_paged_config* cfg, const void* pool,
+                                       const headkv_paged_lists* own,
+                                       const headkv_paged_lists* shared, const int32_t* share,
+                                       int32_t tokens, const int32_t* counts,
+                                       const int32_t* window, const uint16_t* q,
+                                       int64_t q_row_stride, int64_t q_token_stride, float* out,
+                                       float* lse, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
+    PagedDims c;
+    PagedLists o, s;
+    if (headkv_status st = make_dims(cfg, &c)) return st;
+    if (headkv_status st = make_lists(c, own, true, &o)) return st;
+    if ((shared != nullptr) != (share != nullptr))
+        return bad("shared and share must both be given or both be NULL");
+    if (shared)
+        if (headkv_status st = make_lists(c, shared, true, &s)) return st;
+    if (tokens < 0) return bad("tokens must be >= 0");
+    if (tokens == 0) return HEADKV_OK;  // rows of no tokens may have no address
+    if (tokens > kMostTokens) return hip_status(kTooLarge, "");
+    if (!pool || !aligned(pool, 256)) return bad("pool is NULL or not 256-byte aligned");
+    if (!q || !out) return bad("q / out is NULL");
+    if (!aligned(q, 16) || !aligned(out, 16)) return bad("q / out not 16-byte aligned");
+    if (!aligned(lse, 4) || !aligned(share, 4) || !aligned(counts, 4) || !aligned(window, 4))
+        return bad("lse / share / counts / window not aligned");
+    if (q_row_stride < 0 || q_row_stride % 8 || q_token_stride < 0 || q_token_stride % 8)
+        return bad("strides of q must be >= 0 and multiples of 8");
+    const size_t need = paged_attn_tokens_workspace(c, o, shared ? &s : nullptr, tokens);
+    if (!need) return hip_status(kTooLarge, "");
+    if (headkv_status st = check_workspace(workspace, workspace_bytes, need)) return st;
+    const PagedTokens t{tokens, counts, window, q, q_row_stride, q_token_stride};
+    return hip_status(launch_paged_attn_tokens(t, c, static_cast<const char*>(pool), o,
+                                               shared ? &s : nullptr, share, out, lse, workspace,
+                                               stream),
+                      "paged attention launch");
+}
+
 static headkv_status check_scores(int32_t rows, int32_t vocab, int32_t top) {
     if (rows < 0 || vocab < 1) return bad("rows must be >= 0 and vocab >= 1");
     if (vocab > (1 << 24)) return unsupported("vocab > 2^24");

@@ -37,6 +37,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "paged.h"
 #include "paged_device.h"
@@ -77,6 +78,23 @@ struct AttnCall {
     int shared_chunk, shared_parts;  // (0: no shared lists)
     int tiles;                       // column tiles in the grid, per shared list
     int shared_block0, shared_blocks;  // of this launch, before those of own lists
+    // Several tokens of each row (TOK): a row's tokens are cut into `cuts` of `cut` each,
+    // and a cut takes the place of a row: own.lists counts cuts, c.group is the columns of
+    // one, `cut` tokens of `heads` query heads.
+    int tokens, cuts, cut, heads, reach;  // reach: no list has more tokens, new ones too
+    int64_t q_token;
+    const int32_t* counts;
+    const int32_t* window;
+};
+
+// The tokens of a cut: n from token0 of row b on; n <= 0: none.
+struct Cut {
+    int b, token0, n;
+    __device__ __forceinline__ Cut(const AttnCall& a, int v) {
+        b = v / a.cuts;
+        token0 = (v - b * a.cuts) * a.cut;
+        n = min(a.cut, (a.counts ? min(a.counts[b], a.tokens) : a.tokens) - token0);
+    }
 };
 
 __device__ __forceinline__ u32x4_t nt16(const char* p) {
@@ -476,6 +494,24 @@ struct Wave {
              t.ks, t.vs, partial, seen);
     }
 
+    // The same where columns differ in what they attend: the lane's own is [first, end); all
+    // of them attend [all_first, all_end), none outside [any_first, any_end).
+    struct Seen {
+        int first, end, all_first, all_end, any_first, any_end;
+    };
+    __device__ __forceinline__ void step_at(Tile<TYPE, D>& t, int at, const Seen& s, int lane) {
+        const bool partial = at < s.all_first || at + kStep > s.all_end;
+        uint32_t seen = 0xffu;
+        if (partial) {
+            t.blank(seen_of(at, s.any_first, s.any_end, lane));
+            seen = seen_of(at, s.first, s.end, lane);
+        }
+        constexpr int kPer = KS / Tile<TYPE, D>::KN;
+        step([&](int u, int s) { return key_operand<TYPE>(t.k[u][s / kPer], t.ke[u], s % kPer); },
+             [&](int j, bf16x8_t* a) { value_operands<TYPE>(t.v[j], t.ve[TYPE == kFp4 ? j : 0], a); },
+             t.ks, t.vs, partial, seen);
+    }
+
     // Lane n: the page of the wavefront's n-th step of the tokens [t0, t1).
     template <int W>
     static __device__ __forceinline__ int pages_of(const PagedDims& c, const int32_t* pages, int t0,
@@ -489,6 +525,13 @@ struct Wave {
     template <bool ONCE, int W>
     __device__ __forceinline__ void run(const PagedDims& c, const char* pool, int page, int t0, int t1,
                                         int first, int wave, int lane) {
+        run_steps<ONCE, W>(c, pool, page, t0, t1, wave, lane, [&](Tile<TYPE, D>& t, int at) {
+            step_at(t, at, first, t1, lane);
+        });
+    }
+    template <bool ONCE, int W, typename Step>
+    __device__ __forceinline__ void run_steps(const PagedDims& c, const char* pool, int page, int t0,
+                                              int t1, int wave, int lane, Step step) {
         if (t0 + (wave + W * lane) * kStep >= t1) page = -1;
         uint64_t todo = __builtin_amdgcn_ballot_w64(page >= 0 && page < c.num_pages);
         if (!todo) return;
@@ -504,7 +547,7 @@ struct Wave {
             todo &= todo - 1;
             const int after = todo ? __builtin_ctzll(todo) : -1;
             if (after >= 0) fetch(next, after);
-            step_at(now, t0 + (wave + W * n) * kStep, first, t1, lane);
+            step(now, t0 + (wave + W * n) * kStep);
             if (after < 0) break;
             // Two tiles in turn, without the copy, take 12 to 30 more registers: 64 x 32
             // lists of 1000 INT8 tokens 42 us instead of 39.
@@ -568,6 +611,7 @@ constexpr size_t join_bytes(int d, int cols, int W = kWaves) {
 
 __device__ __forceinline__ void write_out(const AttnCall& a, int64_t row, int d, int D, f32x4_t v,
                                           float m, float sum) {
+    if (row < 0) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     *reinterpret_cast<f32x4_t*>(a.out + row * D + d) = v * inv;
     if (a.lse && d == 0)
@@ -585,6 +629,53 @@ __device__ __forceinline__ Span span_of(const PagedLists& p, int ptok, int64_t l
     s.start = s.first & ~(kStep - 1);
     s.chunks = s.len > s.first ? (s.len - s.start + chunk - 1) / chunk : 0;
     return s;
+}
+
+// The same of a cut, whose first token sees least of what is behind a window.
+__device__ __forceinline__ Span span_of_cut(const AttnCall& a, int64_t real, const Cut& cut, int chunk,
+                                            int* base, int* window) {
+    Span s;
+    *base = list_len(a.own, a.c.ptok, real);
+    *window = a.window ? a.window[real] : 0;
+    s.first = a.own.first ? max(a.own.first[real], 0) : 0;
+    if (*window > 0) s.first = max(s.first, *base + cut.token0 + 1 - *window);
+    s.len = min(*base + cut.token0 + cut.n, a.own.max_pages * a.c.ptok);
+    s.start = s.first & ~(kStep - 1);
+    s.chunks = s.len > s.first ? (s.len - s.start + chunk - 1) / chunk : 0;
+    return s;
+}
+// Chunks of the own list of row (TOK: cut) v, kv head h.
+template <bool TOK>
+__device__ __forceinline__ int own_chunks(const AttnCall& a, int v, int h) {
+    if constexpr (TOK) {
+        const Cut cut(a, v);
+        int base, window;
+        return span_of_cut(a, (int64_t)cut.b * a.c.heads + h, cut, a.own_chunk, &base, &window).chunks;
+    }
+    return span_of(a.own, a.c.ptok, (int64_t)v * a.c.heads + h, a.own_chunk).chunks;
+}
+// Row of q, of kv head h: column `col` of row (TOK: cut) v.
+template <int D, bool TOK>
+__device__ __forceinline__ const uint16_t* query(const AttnCall& a, int v, int h, int col) {
+    if constexpr (TOK) {
+        const Cut cut(a, v);
+        const int token = min(col / a.heads, max(cut.n, 1) - 1), head = col % a.heads;
+        return a.q + cut.b * a.q_stride + (cut.token0 + token) * a.q_token + (h * a.heads + head) * D;
+    }
+    return a.q + v * a.q_stride + (h * a.c.group + col) * D;
+}
+// Its row of the output; -1: none, a token behind the row's last.
+template <bool TOK>
+__device__ __forceinline__ int64_t out_row(const AttnCall& a, int lh, int col) {
+    if constexpr (TOK) {
+        const int v = lh / a.c.heads, h = lh - v * a.c.heads;
+        const Cut cut(a, v);
+        const int token = col / a.heads;
+        if (token >= cut.n) return -1;
+        return (((int64_t)cut.b * a.tokens + cut.token0 + token) * a.c.heads + h) * a.heads +
+               col % a.heads;
+    }
+    return (int64_t)lh * a.c.group + col;
 }
 
 // Parts that a block of another XCD reads in the same launch: written through,
@@ -636,14 +727,22 @@ struct Sum {
 
 // The rows whose columns a block of a shared list has: `members` of its rows, counted
 // up to rank1, those of ranks [rank0, rank1) in row_of.  W wavefronts.
-template <int W>
+template <int W, bool TOK>
 __device__ __forceinline__ int find_members(const AttnCall& a, int list, int rank0, int rank1,
                                             int* row_of, int* found, int tid) {
     const int lane = tid & 63, wave = tid >> 6;
     int members = 0;
     for (int b0 = 0; b0 < a.own.lists && members < rank1; b0 += 64 * W) {
         const int b = b0 + tid;
-        const bool is = b < a.own.lists && a.share[b] == list;
+        bool is = b < a.own.lists;
+        if constexpr (TOK) {
+            if (is) {
+                const Cut cut(a, b);
+                is = cut.n > 0 && a.share[cut.b] == list;
+            }
+        } else {
+            is = is && a.share[b] == list;
+        }
         const uint64_t mask = __builtin_amdgcn_ballot_w64(is);
         if (lane == 0) found[wave] = __builtin_popcountll(mask);
         __syncthreads();
@@ -659,12 +758,11 @@ __device__ __forceinline__ int find_members(const AttnCall& a, int list, int ran
 }
 
 // Column `col` of a shared list is a query head of the member of rank col / group.
-template <int TYPE, int D>
+template <int TYPE, int D, bool TOK>
 __device__ __forceinline__ void load_queries(const AttnCall& a, int h, int col, int rank0,
                                              const int* row_of, int lane, bf16x8_t* q) {
     const int group = a.c.group;
-    const uint16_t* from = a.q + row_of[col / group - rank0] * a.q_stride +
-                           (h * group + col % group) * D;
+    const uint16_t* from = query<D, TOK>(a, row_of[col / group - rank0], h, col % group);
 #pragma unroll
     for (int k = 0; k < D / 32; ++k)
         q[k] = *reinterpret_cast<const bf16x8_t*>(from + key_dim<TYPE, D>(k, lane >> 4));
@@ -677,7 +775,7 @@ __device__ __forceinline__ int64_t shared_slot(const AttnCall& a, int h, int col
     return row * a.shared_parts + chunk;
 }
 
-// Parts of the prefix that row b shares, for kv head h.
+// Parts of the prefix that row (of a cut: its row) b shares, for kv head h.
 __device__ __forceinline__ int prefix_parts(const AttnCall& a, int b, int h) {
     if (!a.shared_parts) return 0;
     const int l = a.share[b];
@@ -700,7 +798,7 @@ __device__ __forceinline__ void add_prefix(const AttnCall& a, Sum& all, int64_t 
         },
         [&](int j) { return WITH ? published(a.shared_ml + at + j) : a.shared_ml[at + j]; });
 }
-template <int D, bool WITH>
+template <int D, bool WITH, bool TOK>
 __device__ __forceinline__ void finish(const AttnCall& a, int lh, int chunks, int prefix, int col, int d) {
     const int64_t row = (int64_t)lh * a.c.group + col, slot = row * a.own_parts;
     Sum all;
@@ -713,7 +811,7 @@ __device__ __forceinline__ void finish(const AttnCall& a, int lh, int chunks, in
         },
         [&](int j) { return published(a.ml + slot + j); });
     add_prefix<D, WITH>(a, all, row, prefix, d);
-    write_out(a, row, d, D, all.v, all.m, all.s);
+    write_out(a, out_row<TOK>(a, lh, col), d, D, all.v, all.m, all.s);
 }
 
 // `columns` of a list's part have arrived; true for the last of `total`.
@@ -726,7 +824,7 @@ __device__ __forceinline__ bool arrive(int* counter, int columns, int total) {
 
 // A row's own list: one block, or with W = 1 one wavefront, per (row, kv head, chunk),
 // the first also for an empty list.
-template <int TYPE, int D, bool WITH, int W>
+template <int TYPE, int D, bool WITH, int W, bool TOK>
 __device__ __forceinline__ void own_block(const AttnCall& a, int block, float* lds, int* flags) {
     const int lane = threadIdx.x & 63;
     int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -741,14 +839,32 @@ __device__ __forceinline__ void own_block(const AttnCall& a, int block, float* l
     const int tid = wave * 64 + lane;
     const int group = a.c.group;
     const int rank = unit % a.lists, chunk = unit / a.lists;
-    const int at = a.list0 + rank;
-    const int lh = a.own.order ? min(max(a.own.order[at], 0), a.own.lists * a.c.heads - 1) : at;
+    int at = a.list0 + rank, last = a.own.lists * a.c.heads - 1, cut_at = 0;
+    if constexpr (TOK) {  // the last cut of every row first, which attends most
+        const int lists = a.own.lists / a.cuts * a.c.heads;
+        cut_at = at / lists;
+        at -= cut_at * lists;
+        cut_at = a.cuts - 1 - cut_at;
+        last = lists - 1;
+    }
+    int lh = a.own.order ? min(max(a.own.order[at], 0), last) : at;
     const int b = lh / a.c.heads, h = lh % a.c.heads;
     // the pages as they are without a window, before the length is known
     const int32_t* pages = a.own.pages + (int64_t)lh * a.own.max_pages;
-    const int g0 = chunk * a.own_chunk, g1 = min(g0 + a.own_chunk, a.own.max_len);
+    const int g0 = chunk * a.own_chunk, g1 = min(g0 + a.own_chunk, TOK ? a.reach : a.own.max_len);
     int page = Wave<TYPE, D, 1>::template pages_of<W>(a.c, pages, g0, g1, wave, lane);
-    const Span s = span_of(a.own, a.c.ptok, lh, a.own_chunk);
+    Span s;
+    int base = 0, window = 0, v = b, token0 = 0;
+    if constexpr (TOK) {
+        v = b * a.cuts + cut_at;
+        const Cut cut(a, v);
+        if (cut.n <= 0) return;
+        token0 = cut.token0;
+        s = span_of_cut(a, lh, cut, a.own_chunk, &base, &window);
+        lh = v * a.c.heads + h;
+    } else {
+        s = span_of(a.own, a.c.ptok, lh, a.own_chunk);
+    }
     const int chunks = max(s.chunks, 1);
     if (chunk >= chunks) return;
     const int t0 = s.start + chunk * a.own_chunk, t1 = min(s.len, t0 + a.own_chunk);
@@ -757,13 +873,27 @@ __device__ __forceinline__ void own_block(const AttnCall& a, int block, float* l
 
     Wave<TYPE, D, 1> w;
     w.clear();
-    const uint16_t* q = a.q + b * a.q_stride + (h * group + min(lane & 15, group - 1)) * D;
+    const uint16_t* q = query<D, TOK>(a, v, h, min(lane & 15, group - 1));
 #pragma unroll
     for (int k = 0; k < D / 32; ++k)
         w.q[0][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
     if (s.chunks > 0) {  // (else t0 may be past what an int holds)
         if (s.start > 0) page = Wave<TYPE, D, 1>::template pages_of<W>(a.c, pages, t0, t1, wave, lane);
-        w.template run<true, W>(a.c, a.pool, page, t0, t1, s.first, wave, lane);
+        if constexpr (TOK) {
+            // the lane's column, the first and the last
+            const int list_first = a.own.first ? max(a.own.first[(int64_t)b * a.c.heads + h], 0) : 0;
+            const int token = min((lane & 15) / a.heads, a.cut - 1);
+            auto first_of = [&](int token) {
+                return window > 0 ? max(list_first, base + token0 + token + 1 - window) : list_first;
+            };
+            const typename Wave<TYPE, D, 1>::Seen seen{
+                first_of(token), min(base + token0 + token + 1, t1), first_of(a.cut - 1),
+                min(base + token0 + 1, t1), s.first, t1};
+            w.template run_steps<false, W>(a.c, a.pool, page, t0, t1, wave, lane,
+                                           [&](Tile<TYPE, D>& t, int at) { w.step_at(t, at, seen, lane); });
+        } else {
+            w.template run<true, W>(a.c, a.pool, page, t0, t1, s.first, wave, lane);
+        }
     }
 
     int* counter = a.arrived + (WITH ? lh : rank);
@@ -778,7 +908,7 @@ __device__ __forceinline__ void own_block(const AttnCall& a, int block, float* l
         if (alone) {
             Sum all{v, m, sum};
             add_prefix<D, WITH>(a, all, row0 + col, prefix, d);
-            write_out(a, row0 + col, d, D, all.v, all.m, all.s);
+            write_out(a, out_row<TOK>(a, lh, col), d, D, all.v, all.m, all.s);
         } else {
             const int64_t slot = (row0 + col) * a.own_parts + chunk;
             publish4(a.part + slot * D + d, v);
@@ -798,7 +928,7 @@ __device__ __forceinline__ void own_block(const AttnCall& a, int block, float* l
     together<W>();
     if (!*flags) return;
     for (int i = tid; i < group * (D / 4); i += 64 * W)
-        finish<D, WITH>(a, lh, chunks, prefix, i / (D / 4), i % (D / 4) * 4);
+        finish<D, WITH, TOK>(a, lh, chunks, prefix, i / (D / 4), i % (D / 4) * 4);
 }
 
 // A shared list of few columns (members * group of them): one block per (list, kv
@@ -808,7 +938,7 @@ struct SharedLds {
     int chunks[16];       // of the members' own lists
     int done[16], count;  // members (of the tile) whose parts are all there
 };
-template <int TYPE, int D>
+template <int TYPE, int D, bool TOK>
 __device__ __forceinline__ void shared_block(const AttnCall& a, int block, float* lds, SharedLds& ints) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -823,7 +953,7 @@ __device__ __forceinline__ void shared_block(const AttnCall& a, int block, float
 
     for (int tile = tile0;; tile += a.tiles) {
         const int c0 = tile * 16, rank0 = c0 / group, rank1 = (c0 + 15) / group + 1;
-        const int members = find_members<kWaves>(a, list, rank0, rank1, row_of, ints.found, tid);
+        const int members = find_members<kWaves, TOK>(a, list, rank0, rank1, row_of, ints.found, tid);
         const int cols = min(16, members * group - c0);
         if (cols <= 0 || chunk >= s.chunks) return;  // (the length is not waited for alone)
         const int t0 = s.start + chunk * a.shared_chunk, t1 = min(s.len, t0 + a.shared_chunk);
@@ -833,10 +963,9 @@ __device__ __forceinline__ void shared_block(const AttnCall& a, int block, float
         };
         Wave<TYPE, D, 1> w;
         w.clear();
-        load_queries<TYPE, D>(a, h, c0 + min(lane & 15, cols - 1), rank0, row_of, lane, w.q[0]);
+        load_queries<TYPE, D, TOK>(a, h, c0 + min(lane & 15, cols - 1), rank0, row_of, lane, w.q[0]);
         if (wave == 0 && columns() > 0)
-            ints.chunks[lane] = max(span_of(a.own, a.c.ptok, (int64_t)row_of[lane] * a.c.heads + h,
-                                            a.own_chunk).chunks, 1);
+            ints.chunks[lane] = max(own_chunks<TOK>(a, row_of[lane], h), 1);
         const int page = Wave<TYPE, D, 1>::template pages_of<kWaves>(a.c, pages, t0, t1, wave, lane);
         w.template run<false, kWaves>(a.c, a.pool, page, t0, t1, s.first, wave, lane);
         join_waves<kWaves>(w, lds, cols, wave, lane, [&](int n, int d, f32x4_t v, float m, float sum) {
@@ -859,7 +988,7 @@ __device__ __forceinline__ void shared_block(const AttnCall& a, int block, float
         const int per = group * (D / 4);
         for (int i = tid; i < ints.count * per; i += kThreads) {
             const int n = ints.done[i / per], k = i % per;
-            finish<D, true>(a, row_of[n] * a.c.heads + h, ints.chunks[n], s.chunks, k / (D / 4),
+            finish<D, true, TOK>(a, row_of[n] * a.c.heads + h, ints.chunks[n], s.chunks, k / (D / 4),
                             k % (D / 4) * 4);
         }
         __syncthreads();  // row_of and done are written again
@@ -873,12 +1002,12 @@ constexpr int own_waves() { return D == 64 || TYPE == kFp4 ? 4 : TYPE == kInt8 ?
 template <int TYPE, int D>
 constexpr int with_shared_waves() { return D == 64 ? 4 : TYPE == kBf16 ? 2 : 3; }
 
-template <int TYPE, int D, int W>
+template <int TYPE, int D, int W, bool TOK>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(own_waves<TYPE, D>())))
 void k_attn_own(AttnCall a) {
     extern __shared__ __align__(16) float lds[];  // join_bytes(D, group)
     __shared__ int flags[kWaves];
-    own_block<TYPE, D, false, W>(a, blockIdx.x, lds, flags);
+    own_block<TYPE, D, false, W, TOK>(a, blockIdx.x, lds, flags);
 }
 
 // Shared lists of few columns and the rows' own ones in one launch: the shared ones'
@@ -886,14 +1015,14 @@ void k_attn_own(AttnCall a) {
 // them.  Whichever brings the last part of a row's list joins them all.  (64 rows on a
 // prefix of 2048 INT8 tokens with own lists of 64 to 1024, 32 heads: 55 us; in two
 // launches, with the prefix's parts read by the second, 62.)
-template <int TYPE, int D, int W>
+template <int TYPE, int D, int W, bool TOK>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(with_shared_waves<TYPE, D>())))
 void k_attn_with_shared(AttnCall a) {
     extern __shared__ __align__(16) float lds[];  // join_bytes(D, 16)
     __shared__ SharedLds ints;
     const int block = blockIdx.x;
-    if (block < a.shared_blocks) shared_block<TYPE, D>(a, a.shared_block0 + block, lds, ints);
-    else own_block<TYPE, D, true, W>(a, block - a.shared_blocks, lds, ints.found);
+    if (block < a.shared_blocks) shared_block<TYPE, D, TOK>(a, a.shared_block0 + block, lds, ints);
+    else own_block<TYPE, D, true, W, TOK>(a, block - a.shared_blocks, lds, ints.found);
 }
 
 // What a wavefront of k_attn_shared_wide does of a step's operands: the first four
@@ -1019,7 +1148,7 @@ struct Share {
 // 16384 FP4 tokens: 83 us, 0.83 PFLOP/s on the matrix cores (K once, V with three
 // pieces), which are busy for a third of the time; the vector ALU's share, the
 // exponentials and the weights' pieces, is 40 %, and the two meet at a step's barrier.
-template <int TYPE, int D>
+template <int TYPE, int D, bool TOK>
 __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     using T = Tile<TYPE, D>;
     constexpr int W = kWideWaves, COLS = kWideCols, NB = COLS / (16 * W);
@@ -1050,7 +1179,7 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     for (int tile = tile0;; tile += a.tiles) {
         // the members that the tile's columns belong to: ranks [rank0, rank1)
         const int c0 = tile * COLS, rank0 = c0 / group, rank1 = (c0 + COLS - 1) / group + 1;
-        const int members = find_members<W>(a, list, rank0, rank1, row_of, found, tid);
+        const int members = find_members<W, TOK>(a, list, rank0, rank1, row_of, found, tid);
         const int cols = min(COLS, members * group - c0);  // of this tile
         if (cols <= 0) return;
         const int w0 = wave * 16 * NB;  // the wavefront's first column
@@ -1058,7 +1187,7 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
         w.clear();
 #pragma unroll
         for (int n = 0; n < NB; ++n)
-            load_queries<TYPE, D>(a, h, c0 + min(w0 + 16 * n + (lane & 15), cols - 1), rank0, row_of,
+            load_queries<TYPE, D, TOK>(a, h, c0 + min(w0 + 16 * n + (lane & 15), cols - 1), rank0, row_of,
                                   lane, w.q[n]);
         auto part_of = [&](int n, uint32_t* seen) {  // step n: is it attended in part
             const int at = t0 + n * kStep;
@@ -1230,7 +1359,7 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     return s;
 }
 
-template <int TYPE, int D>
+template <int TYPE, int D, bool TOK>
 int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
     const int lists = a.own.lists * a.c.heads;
     // (a launch has fewer than 2^32 threads)
@@ -1252,12 +1381,12 @@ int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
             a.shared_block0 = (int)b0;
             a.shared_blocks = (int)std::min(blocks - b0, part);
             if (wide) {
-                k_attn_shared_wide<TYPE, D><<<a.shared_blocks, kWideThreads, 0, st>>>(a);
+                k_attn_shared_wide<TYPE, D, TOK><<<a.shared_blocks, kWideThreads, 0, st>>>(a);
             } else {
                 const unsigned grid = (unsigned)(a.shared_blocks + own_blocks());
                 const size_t lds = join_bytes(D, 16);
-                if (single) k_attn_with_shared<TYPE, D, 1><<<grid, kThreads, lds, st>>>(a);
-                else k_attn_with_shared<TYPE, D, kWaves><<<grid, kThreads, lds, st>>>(a);
+                if (single) k_attn_with_shared<TYPE, D, 1, TOK><<<grid, kThreads, lds, st>>>(a);
+                else k_attn_with_shared<TYPE, D, kWaves, TOK><<<grid, kThreads, lds, st>>>(a);
             }
             if (int e = (int)hipGetLastError()) return e;
         }
@@ -1268,8 +1397,8 @@ int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
         a.lists = std::min(lists - l0, most);
         const unsigned grid = (unsigned)own_blocks();
         const size_t lds = join_bytes(D, a.c.group);
-        if (single) k_attn_own<TYPE, D, 1><<<grid, kThreads, lds, st>>>(a);
-        else k_attn_own<TYPE, D, kWaves><<<grid, kThreads, lds, st>>>(a);
+        if (single) k_attn_own<TYPE, D, 1, TOK><<<grid, kThreads, lds, st>>>(a);
+        else k_attn_own<TYPE, D, kWaves, TOK><<<grid, kThreads, lds, st>>>(a);
         if (int e = (int)hipGetLastError()) return e;
     }
     return 0;
@@ -1281,20 +1410,7 @@ size_t paged_attn_workspace(const PagedDims& c, const PagedLists& own, const Pag
     return split_of(c, own, shared).bytes;
 }
 
-int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& own,
-                      const PagedLists* shared, const int32_t* share, const uint16_t* q,
-                      int64_t q_stride, float* out, float* lse, void* ws, void* stream) {
-    const Split s = split_of(c, own, shared);
-    AttnCall a{};
-    a.c = c;
-    a.pool = pool;
-    a.own = own;
-    if (shared) a.shared = *shared;
-    a.share = share;
-    a.q = q;
-    a.q_stride = q_stride;
-    a.out = out;
-    a.lse = lse;
+static int launch_call(AttnCall a, const Split& s, void* ws, bool tok, void* stream) {
     char* w = static_cast<char*>(ws);
     a.arrived = reinterpret_cast<int*>(w);
     a.ml = reinterpret_cast<f32x2_t*>(w + s.ml);
@@ -1307,13 +1423,75 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
     a.shared_parts = s.shared_parts;
     a.tiles = s.tiles;
     hipStream_t st = (hipStream_t)stream;
-    if (c.d == 128)
-        return c.type == kBf16   ? attn_launch<kBf16, 128>(a, s.wide, s.single, st)
-               : c.type == kInt8 ? attn_launch<kInt8, 128>(a, s.wide, s.single, st)
-                                 : attn_launch<kFp4, 128>(a, s.wide, s.single, st);
-    return c.type == kBf16   ? attn_launch<kBf16, 64>(a, s.wide, s.single, st)
-           : c.type == kInt8 ? attn_launch<kInt8, 64>(a, s.wide, s.single, st)
-                             : attn_launch<kFp4, 64>(a, s.wide, s.single, st);
+    auto run = [&](auto type, auto dim) {
+        constexpr int TYPE = decltype(type)::value, D = decltype(dim)::value;
+        return tok ? attn_launch<TYPE, D, true>(a, s.wide, s.single, st)
+                   : attn_launch<TYPE, D, false>(a, s.wide, s.single, st);
+    };
+    auto of_dim = [&](auto dim) {
+        return a.c.type == kBf16   ? run(std::integral_constant<int, kBf16>{}, dim)
+               : a.c.type == kInt8 ? run(std::integral_constant<int, kInt8>{}, dim)
+                                   : run(std::integral_constant<int, kFp4>{}, dim);
+    };
+    return a.c.d == 128 ? of_dim(std::integral_constant<int, 128>{})
+                        : of_dim(std::integral_constant<int, 64>{});
+}
+
+int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& own,
+                      const PagedLists* shared, const int32_t* share, const uint16_t* q,
+                      int64_t q_stride, float* out, float* lse, void* ws, void* stream) {
+    AttnCall a{};
+    a.c = c;
+    a.pool = pool;
+    a.own = own;
+    if (shared) a.shared = *shared;
+    a.share = share;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.out = out;
+    a.lse = lse;
+    return launch_call(a, split_of(c, own, shared), ws, false, stream);
+}
+
+// Cuts in the place of rows.
+static bool cut_rows(PagedDims* c, PagedLists* own, int tokens, int* cuts, int* cut) {
+    *cut = std::max(1, std::min(16 / c->group, tokens));
+    *cuts = (tokens + *cut - 1) / *cut;
+    if ((int64_t)own->lists * *cuts * c->heads > 1 << 24) return false;
+    own->lists *= *cuts;
+    own->max_len = (int)std::min<int64_t>((int64_t)own->max_len + tokens, (int64_t)own->max_pages * c->ptok);
+    c->group *= *cut;
+    return true;
+}
+
+size_t paged_attn_tokens_workspace(PagedDims c, PagedLists own, const PagedLists* shared, int tokens) {
+    int cuts, cut;
+    return cut_rows(&c, &own, std::max(tokens, 1), &cuts, &cut) ? split_of(c, own, shared).bytes : 0;
+}
+
+int launch_paged_attn_tokens(const PagedTokens& t, const PagedDims& c, const char* pool,
+                             const PagedLists& own, const PagedLists* shared, const int32_t* share,
+                             float* out, float* lse, void* ws, void* stream) {
+    AttnCall a{};
+    a.c = c;
+    a.own = own;
+    if (!cut_rows(&a.c, &a.own, t.tokens, &a.cuts, &a.cut)) return kTooLarge;
+    const Split s = split_of(a.c, a.own, shared);
+    a.reach = a.own.max_len;
+    a.own.max_len = own.max_len;
+    a.heads = c.group;
+    a.pool = pool;
+    if (shared) a.shared = *shared;
+    a.share = share;
+    a.tokens = t.tokens;
+    a.counts = t.counts;
+    a.window = t.window;
+    a.q = t.q;
+    a.q_stride = t.q_row;
+    a.q_token = t.q_token;
+    a.out = out;
+    a.lse = lse;
+    return launch_call(a, s, ws, true, stream);
 }
 
 }  // namespace headkv

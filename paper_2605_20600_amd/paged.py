@@ -188,11 +188,13 @@ class PagedKV:
                             k.data_ptr(), v.data_ptr(), strides, _stream(self.index))
         return k, v
 
-    def _workspace(self, own: Lists, shared: Optional[Lists]) -> torch.Tensor:
+    def _workspace(self, own: Lists, shared: Optional[Lists],
+                   tokens: Optional[int] = None) -> torch.Tensor:
         """Planned once for the lists' tables, for any length that they can hold (fp32
         parts of every query head, of 256 to 1024 own and up to 2048 shared tokens:
-        128 rows of 32 query heads of 128 dims with tables of 131072 tokens 270 MB)."""
-        key = (own.pages.shape, None if shared is None else shared.pages.shape)
+        128 rows of 32 query heads of 128 dims with tables of 131072 tokens 270 MB).
+        tokens: of attn_tokens()."""
+        key = (own.pages.shape, None if shared is None else shared.pages.shape, tokens)
         if key == self._planned:
             return self._ws
         most = []
@@ -202,7 +204,10 @@ class PagedKV:
                 a = B.PagedListsArg(None, None, None, None, l.arg.lists, l.arg.max_pages, 0,
                                     l.arg.max_pages * self.cfg.page_tokens)
             most.append(a)
-        need = B.headkv_paged_attn_plan(self.cfg, *most)
+        if tokens is None:
+            need = B.headkv_paged_attn_plan(self.cfg, *most)
+        else:
+            need = B.headkv_paged_attn_tokens_plan(self.cfg, *most, tokens)
         if self._ws is None or need > self._ws.numel():
             # twice the last at least: those that are kept take no more than the one in
             # use, however often a table grows
@@ -248,6 +253,52 @@ class PagedKV:
                             None if shared is None else shared.arg, _ptr(share), q.data_ptr(),
                             row if batch > 1 else 0, out.data_ptr(), _ptr(lse), ws.data_ptr(),
                             ws.numel(), stream)
+        return out
+
+    def attn_tokens(self, own: Lists, q: torch.Tensor, counts: Optional[torch.Tensor] = None,
+                    window: Optional[torch.Tensor] = None, shared: Optional[Lists] = None,
+                    share: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of q (bf16 [batch][tokens][kv_heads * group][head_dim], any strides of
+        rows and tokens), tokens that have been written behind the rows' own lists: each
+        attends what is before it, itself, and with window (int32 [batch][kv_heads], 0: none)
+        so many tokens of its list at most.  counts: int32 [batch], tokens of each row, behind
+        which results are left as they are.  shared, share, out, lse: as for attn()."""
+        if q.dim() != 4 or q.dtype != torch.bfloat16 or q.get_device() != self.index \
+                or q.shape[0] != own.n or q.shape[2:] != (self.heads, self.head_dim):
+            raise ValueError(f"q must be bf16 [{own.n}][tokens][{self.heads}][{self.head_dim}] "
+                             f"on {self.device}, got {q.dtype} {tuple(q.shape)} on {q.device}")
+        batch, tokens, heads, d = q.shape
+        row, token, step, one = q.stride()
+        if tokens and (one != 1 or (step != d and heads > 1)):
+            raise ValueError("the heads of a token of q must be contiguous")
+        if out is None:
+            # what counts leave out is left as it is: zeros in what is allocated here
+            empty = torch.empty if counts is None else torch.zeros
+            out = empty(q.shape, dtype=torch.float32, device=self.device)
+        elif out.dtype != torch.float32 or out.shape != q.shape \
+                or out.get_device() != self.index or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous float32 {tuple(q.shape)} on {self.device}")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:3]
+                                or lse.get_device() != self.index or not lse.is_contiguous()):
+            raise ValueError(f"lse must be contiguous float32 {tuple(q.shape[:3])} on "
+                             f"{self.device}")
+        for l in (own,) if shared is None else (own, shared):
+            if l.kv_heads != self.kv_heads or l.index != self.index:
+                self._check_lists(l)
+        if share is not None:
+            _device_int32(share, (batch,), "share", self.index)
+        if counts is not None:
+            _device_int32(counts, (batch,), "counts", self.index)
+        if window is not None:
+            _device_int32(window, (batch, self.kv_heads), "window", self.index)
+        stream = _stream(self.index)
+        ws = self._workspace(own, shared, tokens)
+        B.headkv_paged_attn_tokens(self.cfg, self.pool.data_ptr(), own.arg,
+                                   None if shared is None else shared.arg, _ptr(share), tokens,
+                                   _ptr(counts), _ptr(window), q.data_ptr(),
+                                   (row if batch > 1 else 0, token if tokens > 1 else 0),
+                                   out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(), stream)
         return out
 
 

@@ -1,0 +1,73 @@
+"""Refusals of the attention of several tokens before anything is launched, and its grids
+at their limits (no GPU)."""
+import ctypes
+
+import pytest
+
+from paper_2605_20600_amd import binding as B
+from test_paged_host import _cfg, _lists
+from test_paged_launch_host import call  # noqa: F401  (a fixture)
+
+FAKE = 0x7F0000000000  # 256-byte aligned, never dereferenced by these calls
+I, U, C = B.HEADKV_ERR_INVALID_ARG, B.HEADKV_ERR_UNSUPPORTED, B.HEADKV_ERR_CAPACITY
+
+
+def _attn(cfg=None, pool=FAKE, own=None, shared=None, share=None, tokens=5, counts=None,
+          window=None, q=FAKE, strides=(5120, 1024), out=FAKE, lse=None, ws=FAKE, size=1 << 30):
+    st = B.load_paged().headkv_paged_attn_tokens(
+        cfg or _cfg(), pool, own or _lists(), shared, share, tokens, counts, window, q, *strides,
+        out, lse, ws, size, None)
+    assert st == B.HEADKV_OK or B.headkv_last_error() != ""
+    return st
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(cfg=_cfg(head_dim=96)), U), (dict(own=_lists(pages=None)), I), (dict(pool=None), I),
+    (dict(pool=FAKE + 16), I), (dict(shared=_lists()), I), (dict(share=FAKE), I),
+    (dict(shared=_lists(lists=0), share=FAKE), I), (dict(shared=_lists(), share=FAKE + 2), I),
+    (dict(tokens=-1), I), (dict(counts=FAKE + 2), I), (dict(window=FAKE + 1), I),
+    (dict(q=None), I), (dict(q=FAKE + 8), I), (dict(strides=(-8, 1024)), I),
+    (dict(strides=(5120, 12)), I), (dict(out=None), I), (dict(out=FAKE + 8), I),
+    (dict(lse=FAKE + 2), I), (dict(ws=None), I), (dict(ws=FAKE + 8), I), (dict(size=100), C),
+    (dict(own=_lists(lists=1 << 21), tokens=20), U), (dict(tokens=2 ** 31 - 1), U)])
+def test_refusals(kw, status):
+    assert _attn(**kw) == status
+
+
+def test_nothing_to_do():
+    assert _attn(tokens=0, q=None, out=None, ws=None, size=0) == B.HEADKV_OK
+
+
+def test_plan():
+    size = ctypes.c_size_t()
+    plan = B.load_paged().headkv_paged_attn_tokens_plan
+    assert plan(_cfg(), _lists(), None, -1, size) == I
+    assert plan(_cfg(), _lists(), None, 1, None) == I
+    assert plan(_cfg(), _lists(lists=1 << 21), None, 20, size) == U
+    # a length's workspace holds every shorter one's
+    last = 0
+    for n in range(0, 20000, 96):
+        need = B.headkv_paged_attn_tokens_plan(_cfg(), _lists(max_pages=400, max_len=n), None, 9)
+        assert need >= last
+        last = need
+
+
+def test_grids(call):  # noqa: F811
+    run = ("L.headkv_paged_attn_tokens(cfg(kv_heads={heads}, group={group}), FAKE, lists({rows}, 16, "
+           "{most}), None, None, {tokens}, None, None, FAKE, 0, 0, FAKE, None, FAKE, 1 << 62, None)")
+    # 16 / group tokens to a cut
+    for rows, heads, group, tokens, cuts in ((3, 2, 1, 16, 1), (3, 2, 1, 17, 2), (3, 2, 3, 5, 1),
+                                             (3, 2, 3, 6, 2), (3, 2, 16, 7, 7)):
+        st, got = call(run.format(rows=rows, heads=heads, group=group, tokens=tokens, most=100))
+        assert st == B.HEADKV_OK and got == [(rows * heads * cuts, 256)], got
+    st, got = call(run.format(rows=1 << 14, heads=1024, group=16, tokens=1, most=4000))
+    assert st == B.HEADKV_OK and all(g * b < 1 << 32 for g, b in got)
+
+
+@pytest.mark.parametrize("kind,heads,group,tokens,most", (
+    ("BF16", 2, 4, 3, 8192), ("INT8", 2, 8, 2, 16384), ("FP4", 4, 16, 1, 16384)))
+def test_blocks_of_256_columns(call, kind, heads, group, tokens, most):  # noqa: F811
+    st, got = call(f"L.headkv_paged_attn_tokens(cfg(kv_type=B.HEADKV_KV_{kind}, head_dim=128, "
+                   f"kv_heads={heads}, group={group}), FAKE, lists(65, 1, 40), lists(1, 64, {most}), "
+                   f"FAKE, {tokens}, None, None, FAKE, 0, 0, FAKE, None, FAKE, 1 << 62, None)")
+    assert st == B.HEADKV_OK and 512 in [b for _, b in got], got
