@@ -72,7 +72,8 @@ struct PagedTokens {
     int64_t q_row, q_token;
 };
 // 0: more tokens than one call takes
-size_t paged_attn_tokens_workspace(PagedDims c, PagedLists own, const PagedLists* shared, int tokens);
+size_t paged_attn_tokens_workspace(const PagedDims& c, const PagedLists& own, const PagedLists* shared,
+                                   int tokens);
 int launch_paged_attn_tokens(const PagedTokens& t, const PagedDims& c, const char* pool,
                              const PagedLists& own, const PagedLists* shared, const int32_t* share,
                              float* out, float* lse, void* ws, void* stream);

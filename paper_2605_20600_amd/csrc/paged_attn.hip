@@ -55,8 +55,11 @@ typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kStep = 32;                          // tokens of a wavefront's step
 constexpr int kUnit = kStep * kWaves;              // and of a block's
+constexpr int kSharedMost = 64 * kStep;            // tokens of a chunk at most: pages in the lanes
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
+constexpr int kCutBlocks = 256;                 // that few cuts of many columns are made into
 constexpr int kWideCols = 2 * 16 * kWideWaves;  // columns of a block of k_attn_shared_wide
+constexpr int kCutCols = 16 * kWideWaves;       // and of k_attn_cut_wide
 
 // One attention call as the kernels see it.
 struct AttnCall {
@@ -82,7 +85,8 @@ struct AttnCall {
     // and a cut takes the place of a row: own.lists counts cuts, c.group is the columns of
     // one, `cut` tokens of `heads` query heads.
     int tokens, cuts, cut, heads, reach;  // reach: no list has more tokens, new ones too
-    int64_t q_token;
+    int64_t q_token, row0;
+    int* chunk_of_all;  // the chunk that few cuts of many columns have got
     const int32_t* counts;
     const int32_t* window;
 };
@@ -351,10 +355,11 @@ struct Wave {
     }
 
     // One step: operands from key(u, s) and value(j, a), INT8 scales.  partial: not
-    // all tokens are attended, bit n of `seen` is set if token n of the lane's eight is.
-    template <typename Key, typename Value>
+    // all tokens are attended, bit n of seen_by(b) is set if token n of the lane's eight is
+    // by its column of tile b.
+    template <typename Key, typename Value, typename SeenBy>
     __device__ __forceinline__ void step(Key key, Value value, const u32x4_t& key_scales,
-                                         const u32x4_t& value_scales, bool partial, uint32_t seen) {
+                                         const u32x4_t& value_scales, bool partial, SeenBy seen_by) {
         constexpr float kScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0));
         f32x4_t st[NB][2];
 #pragma unroll
@@ -386,6 +391,7 @@ struct Wave {
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             // scores less the reference, log2
+            const uint32_t seen = seen_by(b);
             float x[8];
             auto less = [&](bool twice) {
 #pragma unroll
@@ -491,7 +497,7 @@ struct Wave {
         constexpr int kPer = KS / Tile<TYPE, D>::KN;  // operands of a load of keys
         step([&](int u, int s) { return key_operand<TYPE>(t.k[u][s / kPer], t.ke[u], s % kPer); },
              [&](int j, bf16x8_t* a) { value_operands<TYPE>(t.v[j], t.ve[TYPE == kFp4 ? j : 0], a); },
-             t.ks, t.vs, partial, seen);
+             t.ks, t.vs, partial, [&](int) { return seen; });
     }
 
     // The same where columns differ in what they attend: the lane's own is [first, end); all
@@ -509,7 +515,7 @@ struct Wave {
         constexpr int kPer = KS / Tile<TYPE, D>::KN;
         step([&](int u, int s) { return key_operand<TYPE>(t.k[u][s / kPer], t.ke[u], s % kPer); },
              [&](int j, bf16x8_t* a) { value_operands<TYPE>(t.v[j], t.ve[TYPE == kFp4 ? j : 0], a); },
-             t.ks, t.vs, partial, seen);
+             t.ks, t.vs, partial, [&](int) { return seen; });
     }
 
     // Lane n: the page of the wavefront's n-th step of the tokens [t0, t1).
@@ -1233,7 +1239,7 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
                                    v[x] = __builtin_bit_cast(
                                        bf16x8_t, operands[buf][2 * KS + j * VX + x][lane]);
                            },
-                           ks, vs, partial, seen);
+                           ks, vs, partial, [&](int) { return seen; });
                 }
                 __syncthreads();
             }
@@ -1254,6 +1260,309 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     }
 }
 
+// Cuts of many columns (the pieces of a prompt): a block takes a cut's, up to 256, and the
+// tokens of a chunk of its list, as k_attn_shared_wide does; what a column sees ends with
+// its own token, so a wavefront leaves out the steps that none of its columns sees.
+// Outputs of a list that has one chunk and shares nothing are written here, the others'
+// parts are added up by k_attn_join.
+//
+// Few lists, whose lengths only the device knows: every block counts the tokens of all,
+// cuts them into chunks of a length that leaves each CU about one, and takes every
+// gridDim-th of these.  (A grid of every chunk that there might be instead, most of them
+// none: the others lie two on a CU beside CUs that have none, 28 us instead of 20.)
+constexpr int kFewCuts = kWideThreads;
+
+// A cut and what is known of its list.
+struct CutItem {
+    int real, b, h, token0, n;    // n tokens from token0 of row b on, the list's number
+    int base, window, list_first; // tokens before row b's new ones, the window, the list's `first`
+    __device__ __forceinline__ CutItem() {}
+    // Cut number t: the last ones of all rows first, of lists in their order.
+    __device__ __forceinline__ CutItem(const AttnCall& a, int t) {
+        const int at = place(a, t);
+        real = a.own.order ? min(max(a.own.order[at], 0), a.own.lists / a.cuts * a.c.heads - 1) : at;
+        base = list_len(a.own, a.c.ptok, real);
+        window = a.window ? a.window[real] : 0;
+        list_first = a.own.first ? max(a.own.first[real], 0) : 0;
+        row(a);
+        n = Cut(a, b * a.cuts + token0 / a.cut).n;
+    }
+    __device__ __forceinline__ int place(const AttnCall& a, int t) {
+        const int lists = a.own.lists / a.cuts * a.c.heads, from_last = t / lists;
+        token0 = (a.cuts - 1 - from_last) * a.cut;
+        return t - from_last * lists;
+    }
+    __device__ __forceinline__ void row(const AttnCall& a) {
+        b = real / a.c.heads;
+        h = real - b * a.c.heads;
+    }
+    __device__ __forceinline__ int first_of(int token) const {
+        return window > 0 ? max(list_first, base + token0 + token + 1 - window) : list_first;
+    }
+    // Its span, in as many chunks as `most` tokens make, of about equal length: *chunk tokens.
+    __device__ __forceinline__ Span span(const AttnCall& a, int most, int* chunk) const {
+        Span s;
+        s.first = first_of(0);
+        s.len = min(base + token0 + n, a.own.max_pages * a.c.ptok);
+        s.start = s.first & ~(kStep - 1);
+        s.chunks = 0;
+        *chunk = kStep;
+        if (s.len > s.first) {
+            const int tokens = s.len - s.start, chunks = (tokens + most - 1) / most;
+            *chunk = ((tokens + chunks - 1) / chunks + kStep - 1) / kStep * kStep;
+            s.chunks = (tokens + *chunk - 1) / *chunk;
+        }
+        return s;
+    }
+};
+
+struct Plan {
+    int ends[kFewCuts];  // chunks of the cuts up to this one
+    int sums[kWideWaves];
+    int real[kFewCuts], n[kFewCuts], base[kFewCuts], window[kFewCuts], first[kFewCuts];
+    __device__ __forceinline__ CutItem item(const AttnCall& a, int t) const {
+        CutItem c;
+        c.place(a, t);
+        c.real = real[t];
+        c.n = n[t];
+        c.base = base[t];
+        c.window = window[t];
+        c.list_first = first[t];
+        c.row(a);
+        return c;
+    }
+};
+
+// Fills p; the number of chunks of all cuts, and the tokens of one.
+__device__ __forceinline__ int plan_chunks(const AttnCall& a, Plan& p, int* chunk) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool is = tid < a.own.lists * a.c.heads;
+    const CutItem c(a, is ? tid : 0);
+    int even;
+    const Span s = c.span(a, kSharedMost, &even);
+    // (a sum that 32 bits hold; longer lists are cut into as many parts as there may be)
+    uint32_t sum = is && c.n > 0 && s.chunks > 0 ? min((uint32_t)(s.len - s.start), 1u << 22) : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+    if (lane == 0) p.sums[wave] = (int)sum;
+    p.real[tid] = c.real;
+    p.n[tid] = c.n;
+    p.base[tid] = c.base;
+    p.window[tid] = c.window;
+    p.first[tid] = c.list_first;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w) sum += (uint32_t)p.sums[w];
+    // a quarter more than each CU's share, so that lists of about equal length stay whole
+    const uint32_t want = (sum + sum / 4) / kCutBlocks;
+    *chunk = max((int)((want + kUnit - 1) / kUnit * kUnit), a.own_chunk);
+    int up = is && c.n > 0 ? max(1, c.span(a, *chunk, &even).chunks) : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int y = __shfl_up(up, o);
+        if (lane >= o) up += y;
+    }
+    __syncthreads();
+    if (lane == 63) p.sums[wave] = up;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w)
+        if (w < wave) up += p.sums[w];
+    p.ends[tid] = up;
+    __syncthreads();
+    return p.ends[kFewCuts - 1];
+}
+
+// Operands of two steps in turn; INT8: the scales lie behind them.
+template <int TYPE, int D>
+using CutOperands = u32x4_t[2][2 * (D / 32) + D / 16 + (TYPE == kInt8 ? 2 : 0)][64];
+
+template <int TYPE, int D>
+__device__ __forceinline__ void cut_block(const AttnCall& a, const CutItem& c, int chunk,
+                                          CutOperands<TYPE, D>& operands) {
+    using T = Tile<TYPE, D>;
+    constexpr int W = kWideWaves, NB = kCutCols / (16 * W);
+    constexpr int KS = D / 32, DB = D / 16, VX = DB / T::VN;
+    constexpr int kScales = 2 * KS + DB;  // INT8: scales lie behind the operands
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (c.n <= 0) return;
+    int most;
+    const Span s = c.span(a, a.own_chunk, &most);
+    if (chunk >= max(s.chunks, 1)) return;
+    const int t0 = s.start + chunk * most, t1 = min(s.len, t0 + most);
+    // lane n: page of step n of a piece of the chunk, which has 64
+    auto pages_of = [&](int begin) {
+        const int at = begin + lane * kStep;
+        return s.chunks > 0 && at < t1
+                   ? a.own.pages[(int64_t)c.real * a.own.max_pages + (at >> a.c.pshift)] : -1;
+    };
+    int page = pages_of(t0);
+
+    const int cols = c.n * a.heads;
+    const int w0 = wave * 16 * NB;  // the wavefront's first column
+    auto end_of = [&](int token) { return min(c.base + c.token0 + token + 1, t1); };
+    auto token_of = [&](int col) { return min(col, cols - 1) / a.heads; };
+    const int low = token_of(w0), high = token_of(w0 + 16 * NB - 1);
+    const int any_first = c.first_of(low), any_end = end_of(high);
+    const int all_first = c.first_of(high), all_end = end_of(low);
+    Wave<TYPE, D, NB> w;
+    w.clear();
+    int first[NB], end[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int col = min(w0 + 16 * n + (lane & 15), cols - 1);
+        const int token = token_of(col);
+        first[n] = c.first_of(token);
+        end[n] = end_of(token);
+        const uint16_t* q = a.q + c.b * a.q_stride + (c.token0 + token) * a.q_token +
+                            (c.h * a.heads + col - token * a.heads) * D;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            w.q[n][k] = *reinterpret_cast<const bf16x8_t*>(q + key_dim<TYPE, D>(k, lane >> 4));
+    }
+    Share<TYPE, D> share(a.c, wave, lane);
+    for (int begin = t0;;) {
+        const uint64_t steps = __builtin_amdgcn_ballot_w64(page >= 0 && page < a.c.num_pages);
+        uint64_t to_fetch = steps;
+        int held = 0;  // the step whose loads are held
+        auto fetch = [&] {  // past the last step, that one again
+            if (to_fetch) held = __builtin_ctzll(to_fetch);
+            to_fetch &= to_fetch - 1;
+            share.fetch(a.pool + __builtin_amdgcn_readlane(page, held) * a.c.page_bytes,
+                        (begin + held * kStep) & (a.c.ptok - 1));
+        };
+        auto produce = [&](int into) {
+            const int tk = begin + held * kStep;
+            const bool partial = tk < s.first || tk + kStep > t1;
+            const uint32_t seen = partial ? seen_of(tk, s.first, t1, lane) : 0xffu;
+            share.convert(operands[into], kScales, partial, seen, wave, lane);
+            fetch();
+        };
+        auto consume = [&](int buf, int n) {
+            const int tk = begin + n * kStep;
+            if (w0 >= cols || tk >= any_end || tk + kStep <= any_first) return;
+            const bool partial = tk < all_first || tk + kStep > all_end;
+            uint32_t seen[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+                seen[n] = partial ? seen_of(tk, first[n], end[n], lane) : 0xffu;
+            u32x4_t ks{}, vs{};
+            if constexpr (TYPE == kInt8) {
+                ks = operands[buf][kScales][lane];
+                vs = operands[buf][kScales + 1][lane];
+            }
+            w.step([&](int u, int k) {
+                       return __builtin_bit_cast(bf16x8_t, operands[buf][u * KS + k][lane]);
+                   },
+                   [&](int j, bf16x8_t* v) {
+#pragma unroll
+                       for (int x = 0; x < VX; ++x)
+                           v[x] = __builtin_bit_cast(bf16x8_t,
+                                                     operands[buf][2 * KS + j * VX + x][lane]);
+                   },
+                   ks, vs, partial, [&](int n) { return seen[n]; });
+        };
+        if (steps) {
+            fetch();
+            produce(0);
+            __syncthreads();
+            int buf = 0;
+            for (uint64_t todo = steps; todo; todo &= todo - 1, buf ^= 1) {
+                produce(buf ^ 1);
+                consume(buf, __builtin_ctzll(todo));
+                __syncthreads();
+            }
+        }
+        if (t1 - begin <= kSharedMost) break;
+        begin += kSharedMost;
+        page = pages_of(begin);
+    }
+
+    const bool direct = s.chunks <= 1 && prefix_parts(a, c.b, c.h) == 0;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int col = w0 + 16 * n + (lane & 15);
+        const float sum = over_quarters(w.sum[n], [](float x, float y) { return x + y; });
+        if (col >= cols) continue;
+        const int token = col / a.heads;
+        if (direct) {
+            const int64_t row = (((int64_t)c.b * a.tokens + c.token0 + token) * a.c.heads + c.h) * a.heads +
+                                col - token * a.heads;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int j = 0; j < DB; ++j) w.acc[n][j] *= inv;
+            w.to_row(n, lane >> 4, a.out + row * D);
+            if (a.lse && lane < 16)
+                a.lse[row] = sum == 0.f ? -INFINITY
+                                        : (w.m[n] + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+        } else {
+            const int lh = (c.b * a.cuts + c.token0 / a.cut) * a.c.heads + c.h;
+            const int64_t slot = ((int64_t)lh * a.c.group + col) * a.own_parts + chunk;
+            w.to_row(n, lane >> 4, a.part + slot * D);
+            if (lane < 16) a.ml[slot] = f32x2_t{w.m[n], sum};
+        }
+    }
+}
+
+template <int TYPE, int D, bool FEW>
+__global__ __launch_bounds__(kWideThreads) void k_attn_cut_wide(AttnCall a, int* chunk_of_all) {
+    __shared__ CutOperands<TYPE, D> operands;
+    if constexpr (FEW) {
+        __shared__ Plan plan;
+        int chunk;
+        const int all = plan_chunks(a, plan, &chunk);
+        a.own_chunk = chunk;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *chunk_of_all = chunk;
+        for (int item = blockIdx.x; item < all; item += gridDim.x) {
+            int t = 0;  // the first cut whose chunks end behind it
+#pragma unroll
+            for (int o = kFewCuts / 2; o > 0; o /= 2)
+                if (plan.ends[t + o - 1] <= item) t += o;
+            t = __builtin_amdgcn_readfirstlane(t);
+            cut_block<TYPE, D>(a, plan.item(a, t), item - (t ? plan.ends[t - 1] : 0), operands);
+            __syncthreads();  // the operands are written again
+        }
+    } else {
+        const int item = a.list0 + blockIdx.x, cuts = a.own.lists * a.c.heads;
+        cut_block<TYPE, D>(a, CutItem(a, item % cuts), item / cuts, operands);
+    }
+}
+
+// Adds up the parts of cuts, of their own lists and of the prefixes that they share: a
+// thread for each four dims of an output.
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_attn_join(AttnCall a, const int* chunk_of_all) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t row = i / (D / 4) + a.row0;
+    const int d = (int)(i % (D / 4)) * 4;
+    const int lh = (int)(row / a.c.group), col = (int)(row - (int64_t)lh * a.c.group);
+    if (chunk_of_all) a.own_chunk = *chunk_of_all;
+    if (lh >= a.own.lists * a.c.heads) return;
+    const int v = lh / a.c.heads, h = lh - v * a.c.heads;
+    const Cut cut(a, v);
+    if (col >= cut.n * a.heads) return;
+    CutItem c;
+    c.real = cut.b * a.c.heads + h;
+    c.token0 = cut.token0;
+    c.n = cut.n;
+    c.base = list_len(a.own, a.c.ptok, c.real);
+    c.window = a.window ? a.window[c.real] : 0;
+    c.list_first = a.own.first ? max(a.own.first[c.real], 0) : 0;
+    int most;
+    const int chunks = max(c.span(a, a.own_chunk, &most).chunks, 1);
+    const int prefix = prefix_parts(a, cut.b, h);
+    if (chunks == 1 && prefix == 0) return;  // there already
+    Sum all;
+    const int64_t slot = row * a.own_parts;
+    all.add_parts(
+        chunks, [&](int j) { return *reinterpret_cast<const f32x4_t*>(a.part + (slot + j) * D + d); },
+        [&](int j) { return a.ml[slot + j]; });
+    add_prefix<D, false>(a, all, row, prefix, d);
+    write_out(a, out_row<true>(a, lh, col), d, D, all.v, all.m, all.s);
+}
+
 // ------------------------------------------------------------------- launch
 constexpr int kCus = 256;
 
@@ -1266,7 +1575,7 @@ constexpr int kCus = 256;
 // Shared lists: as many blocks as there are CUs, beside which own lists find room (64
 // rows on a prefix of 2048 INT8 tokens: 256 blocks 54.3 us, 384 53.4, 512 55.1; the own
 // lists' blocks first 70).
-constexpr int kLeastChunk = 2 * kUnit, kOwnMost = 8 * kUnit, kSharedMost = 64 * kStep;
+constexpr int kLeastChunk = 2 * kUnit, kOwnMost = 8 * kUnit;
 int chunk_of(int max_len, int64_t want, int most) {
     const int64_t chunk = ((max_len + want - 1) / want + kUnit - 1) / kUnit * kUnit;
     return (int)std::min<int64_t>(std::max<int64_t>(chunk, kLeastChunk), most);
@@ -1281,6 +1590,12 @@ int64_t most_parts(int max_len, int64_t want, int least, int most) {
     return std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(parts_of(max_len, least), want),
                                                   parts_of(max_len, most)));
 }
+
+// Parts that the lists of few cuts of many columns have at most.
+constexpr int kCutParts = 16;
+// Tokens of a block's chunk at most, pages in the lanes of four wavefronts: where lists are
+// so many that a CU has several blocks, however long, parts would only take space.
+constexpr int kOwnLongest = 64 * kUnit, kManyLists = 16 * kCus;
 
 struct Split {
     int own_chunk, own_parts, shared_chunk, shared_parts;
@@ -1321,19 +1636,33 @@ struct Split {
     // 256 12.3 and 12.9; 4096 of 512 27.8 and 24.8; BF16, d = 128, 512 of 32 5.7 and 6.5, 1024
     // of 64 11.0 and 9.7; 2048 of 192 28.7 and 28.3, 256 33.4 and 35.2.
     bool single;
+    bool own_wide;
     // offsets, and the total
-    size_t ml, part, shared_ml, shared_part, bytes;
+    size_t ml, part, shared_ml, shared_part, chunk, bytes;
 };
 
-Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shared) {
+// cuts: own lists are those of cuts; wide ones go to k_attn_cut_wide.
+Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shared,
+               bool cuts = false) {
     Split s{};
     const size_t lists = (size_t)own.lists * c.heads, rows = lists * c.group;
     auto wanted = [](int64_t blocks, int64_t items) { return std::max<int64_t>(1, blocks / items); };
-    const int64_t own_want = wanted(2 * kCus, lists);
-    s.own_chunk = chunk_of(own.max_len, own_want, kOwnMost);
+    s.own_wide = cuts && c.group > 16;
+    s.single = !s.own_wide && (int64_t)own.max_len * 6 + 640 <= (int64_t)lists &&
+               (!cuts || own.max_len <= kSharedMost);
+    int64_t own_want = wanted(cuts ? 4 * kCus : 2 * kCus, lists);
+    int most_chunk = kOwnMost;
+    if (s.own_wide) {
+        own_want = lists <= kFewCuts ? kCutParts : 1;
+        most_chunk = 1 << 30;
+    } else if (cuts && s.single) {
+        most_chunk = kSharedMost;  // one part
+    } else if (cuts && lists >= kManyLists) {
+        most_chunk = kOwnLongest;
+    }
+    s.own_chunk = chunk_of(own.max_len, own_want, most_chunk);
     s.own_parts = std::max(1, parts_of(own.max_len, s.own_chunk));
-    s.single = (int64_t)own.max_len * 6 + 640 <= (int64_t)lists;
-    const size_t own_most = most_parts(own.max_len, own_want, kLeastChunk, kOwnMost);
+    const size_t own_most = most_parts(own.max_len, own_want, kLeastChunk, most_chunk);
     size_t shared_most = 0;
     if (shared) {
         const int64_t mean = ((int64_t)own.lists * c.group + shared->lists - 1) / shared->lists;
@@ -1355,12 +1684,13 @@ Split split_of(const PagedDims& c, const PagedLists& own, const PagedLists* shar
     s.part = s.ml + up(own_places * sizeof(f32x2_t));
     s.shared_ml = s.part + up(own_places * c.d * sizeof(float));
     s.shared_part = s.shared_ml + up(rows * shared_most * sizeof(f32x2_t));
-    s.bytes = s.shared_part + rows * shared_most * c.d * sizeof(float);
+    s.chunk = s.shared_part + rows * shared_most * c.d * sizeof(float);
+    s.bytes = s.chunk + (cuts ? 256 : 0);
     return s;
 }
 
 template <int TYPE, int D, bool TOK>
-int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
+int attn_launch(AttnCall a, bool wide, bool single, bool own_wide, hipStream_t st) {
     const int lists = a.own.lists * a.c.heads;
     // (a launch has fewer than 2^32 threads)
     constexpr int64_t kMost = (1ll << 31) / kThreads, kWideMost = (1ll << 31) / kWideThreads;
@@ -1373,7 +1703,7 @@ int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
         const int64_t blocks = (int64_t)a.shared.lists * a.c.heads * a.shared_parts * a.tiles;
         if (blocks >= 1ll << 31) return kTooLarge;
         if (!wide) {  // with the own lists, where one launch holds them all
-            a.lists = lists <= most ? lists : 0;
+            a.lists = lists <= most && !own_wide ? lists : 0;
             if (blocks + own_blocks() > kMost) a.lists = 0;
         }
         const int64_t part = wide ? kWideMost : kMost;
@@ -1391,6 +1721,34 @@ int attn_launch(AttnCall a, bool wide, bool single, hipStream_t st) {
             if (int e = (int)hipGetLastError()) return e;
         }
         if (a.lists) return 0;
+    }
+    if constexpr (TOK) {
+        if (own_wide) {
+            const int64_t blocks = (int64_t)lists * a.own_parts;
+            if (blocks >= 1ll << 31) return kTooLarge;
+            int* chunk = lists <= kFewCuts ? a.chunk_of_all : nullptr;
+            if (chunk) {
+                k_attn_cut_wide<TYPE, D, true><<<(unsigned)std::min<int64_t>(blocks, kCutBlocks),
+                                                 kWideThreads, 0, st>>>(a, chunk);
+                if (int e = (int)hipGetLastError()) return e;
+            }
+            for (int64_t b0 = 0; b0 < blocks && !chunk; b0 += kWideMost) {
+                a.list0 = (int)b0;
+                k_attn_cut_wide<TYPE, D, false><<<(unsigned)std::min(blocks - b0, kWideMost),
+                                                  kWideThreads, 0, st>>>(a, nullptr);
+                if (int e = (int)hipGetLastError()) return e;
+            }
+            const bool parts = a.own_parts > 1 || a.shared_parts;
+            const int64_t rows = parts ? (int64_t)lists * a.c.group : 0;  // (below 2^32)
+            constexpr int64_t kPer = 1 << 24;
+            for (int64_t r0 = 0; r0 < rows; r0 += kPer) {
+                a.row0 = r0;
+                const int64_t n = std::min(rows - r0, kPer) * (D / 4);
+                k_attn_join<D><<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, st>>>(a, chunk);
+                if (int e = (int)hipGetLastError()) return e;
+            }
+            return 0;
+        }
     }
     for (int l0 = 0; l0 < lists; l0 += most) {
         a.list0 = l0;
@@ -1417,6 +1775,7 @@ static int launch_call(AttnCall a, const Split& s, void* ws, bool tok, void* str
     a.part = reinterpret_cast<float*>(w + s.part);
     a.shared_ml = reinterpret_cast<f32x2_t*>(w + s.shared_ml);
     a.shared_part = reinterpret_cast<float*>(w + s.shared_part);
+    a.chunk_of_all = reinterpret_cast<int*>(w + s.chunk);
     a.own_chunk = s.own_chunk;
     a.own_parts = s.own_parts;
     a.shared_chunk = s.shared_chunk;
@@ -1425,8 +1784,8 @@ static int launch_call(AttnCall a, const Split& s, void* ws, bool tok, void* str
     hipStream_t st = (hipStream_t)stream;
     auto run = [&](auto type, auto dim) {
         constexpr int TYPE = decltype(type)::value, D = decltype(dim)::value;
-        return tok ? attn_launch<TYPE, D, true>(a, s.wide, s.single, st)
-                   : attn_launch<TYPE, D, false>(a, s.wide, s.single, st);
+        return tok ? attn_launch<TYPE, D, true>(a, s.wide, s.single, s.own_wide, st)
+                   : attn_launch<TYPE, D, false>(a, s.wide, s.single, false, st);
     };
     auto of_dim = [&](auto dim) {
         return a.c.type == kBf16   ? run(std::integral_constant<int, kBf16>{}, dim)
@@ -1453,20 +1812,63 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
     return launch_call(a, split_of(c, own, shared), ws, false, stream);
 }
 
-// Cuts in the place of rows.
-static bool cut_rows(PagedDims* c, PagedLists* own, int tokens, int* cuts, int* cut) {
-    *cut = std::max(1, std::min(16 / c->group, tokens));
+// Cuts in the place of rows.  Of up to 16 columns, for own_block, or up to kCutCols for
+// k_attn_cut_wide, which converts a list's tokens for all of them once but takes some 8 us
+// more however short the list is.  Times of the first over the second, tokens from memory,
+// the longest list four times the shortest, one call after the other:
+//   columns of a row and head     24    32    48    64    96   128
+//   1024 lists of up to 2048 INT8 1.05  1.05  1.38  1.65  1.82  2.12
+//                            FP4  .74   .74   .97  1.19  1.31  1.60
+//                            BF16 1.83  1.79  2.45  3.13  3.87  4.47
+//   1024 of up to 256        INT8 1.00  1.01  1.17  1.18  1.32  1.48
+//                            FP4  .84   .83   .98  1.13   .95  1.06
+//                            BF16 1.25  1.25  1.52  1.67  2.05  2.37
+//   32 of up to 2048         INT8 .79   .80   .88   .81   .83   .94
+//                            FP4  .71   .71   .76   .68   .69   .73
+//                            BF16 .95   .94  1.06  1.04  1.10  1.20
+// so by the columns and by the work, in tiles of 16 columns and tokens of a list.
+static bool is_wide(const PagedDims& c, int64_t lists, int64_t columns, int64_t reach) {
+    const bool fp4 = c.type == kFp4;
+    return columns >= (fp4 ? 49 : 17) &&
+           lists * ((columns + 15) / 16) * reach >= (fp4 ? 1 << 20 : 1 << 19);
+}
+static bool cut_rows(PagedDims* c, PagedLists* own, int tokens, bool wide, int* cuts, int* cut) {
+    *cut = std::max(1, std::min((wide ? kCutCols : 16) / c->group, tokens));
     *cuts = (tokens + *cut - 1) / *cut;
     if ((int64_t)own->lists * *cuts * c->heads > 1 << 24) return false;
     own->lists *= *cuts;
-    own->max_len = (int)std::min<int64_t>((int64_t)own->max_len + tokens, (int64_t)own->max_pages * c->ptok);
     c->group *= *cut;
     return true;
 }
+static int reach_of(const PagedDims& c, const PagedLists& own, int tokens) {
+    return (int)std::min<int64_t>((int64_t)own.max_len + tokens, (int64_t)own.max_pages * c.ptok);
+}
 
-size_t paged_attn_tokens_workspace(PagedDims c, PagedLists own, const PagedLists* shared, int tokens) {
-    int cuts, cut;
-    return cut_rows(&c, &own, std::max(tokens, 1), &cuts, &cut) ? split_of(c, own, shared).bytes : 0;
+// Enough for every shorter length too: narrow cuts up to where wide ones take over.
+size_t paged_attn_tokens_workspace(const PagedDims& c, const PagedLists& own, const PagedLists* shared,
+                                   int tokens) {
+    tokens = std::max(tokens, 1);
+    const int64_t lists = (int64_t)own.lists * c.heads, columns = (int64_t)tokens * c.group;
+    const int reach = reach_of(c, own, tokens);
+    size_t bytes = 0;
+    for (bool wide : {false, true}) {
+        PagedDims d = c;
+        PagedLists o = own;
+        int cuts, cut;
+        o.max_len = reach;
+        if (is_wide(c, lists, columns, reach) != wide) {
+            if (wide) continue;
+            int64_t lo = 0, hi = reach;  // narrow at lo, wide at hi
+            while (hi - lo > 1) {
+                const int64_t mid = lo + (hi - lo) / 2;
+                (is_wide(c, lists, columns, mid) ? hi : lo) = mid;
+            }
+            o.max_len = (int)lo;
+        }
+        if (!cut_rows(&d, &o, tokens, wide, &cuts, &cut)) return 0;
+        bytes = std::max(bytes, split_of(d, o, shared, true).bytes);
+    }
+    return bytes;
 }
 
 int launch_paged_attn_tokens(const PagedTokens& t, const PagedDims& c, const char* pool,
@@ -1475,9 +1877,11 @@ int launch_paged_attn_tokens(const PagedTokens& t, const PagedDims& c, const cha
     AttnCall a{};
     a.c = c;
     a.own = own;
-    if (!cut_rows(&a.c, &a.own, t.tokens, &a.cuts, &a.cut)) return kTooLarge;
-    const Split s = split_of(a.c, a.own, shared);
-    a.reach = a.own.max_len;
+    a.reach = reach_of(c, own, t.tokens);
+    const bool wide = is_wide(c, (int64_t)own.lists * c.heads, (int64_t)t.tokens * c.group, a.reach);
+    if (!cut_rows(&a.c, &a.own, t.tokens, wide, &a.cuts, &a.cut)) return kTooLarge;
+    a.own.max_len = a.reach;
+    const Split s = split_of(a.c, a.own, shared, true);
     a.own.max_len = own.max_len;
     a.heads = c.group;
     a.pool = pool;

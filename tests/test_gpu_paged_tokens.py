@@ -194,6 +194,45 @@ def test_long_lists_in_chunks(kind):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d,group,tokens", ((128, 1, 300), (64, 3, 90), (128, 7, 37), (64, 16, 33)))
+def test_pieces_of_prompts(kind, d, group, tokens):
+    # cuts of many columns: of one chunk and of several, windows that begin inside them,
+    # rows that end before a cut does or have none, prefixes, dropped pages
+    counts = [tokens, tokens // 2, 1, 0]
+    lens = [[0, 130], [97, 31], [5, 0], [3, 4]]
+    Case(kind, d, lens, tokens, counts=counts, group=group, seed=20).check()
+    Case(kind, d, lens, tokens, counts=counts, group=group, windows=[[50, 7], [0, 64]] * 2,
+         first=[[3, 33], [0, 90], [6, 0], [0, 0]], dropped=[(0, 1, 1), (1, 0, 0)], seed=21).check()
+    Case(kind, d, lens, tokens, counts=counts, group=group, prefix=[[70, 600], [0, 0]],
+         share=[0, 1, 0, 0], seed=22).check()
+    Case(kind, d, [[1500, 1030]], tokens, group=group, ptok=256, windows=[[0, 900]], seed=23).check()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d,group,tokens,most", ((128, 4, 64, 9000), (64, 1, 130, 15000)))
+def test_pieces_of_prompts_behind_long_lists(kind, d, group, tokens, most):
+    # cuts of 128 columns (their work is enough): lists of several pieces of 2048 tokens and
+    # of a few tokens, in chunks of a length that follows from all of them
+    counts = [tokens, tokens - 1, 7, 0]
+    lens = [[most, 130], [97, most // 3], [5, 0], [3, 4]]
+    Case(kind, d, lens, tokens, counts=counts, group=group, ptok=256, seed=24).check()
+    Case(kind, d, lens, tokens, counts=counts, group=group, windows=[[2100, 7], [0, 64]] * 2,
+         first=[[3, 33], [0, 2050], [6, 0], [0, 0]], dropped=[(0, 0, 40), (0, 0, 33), (1, 0, 0)],
+         prefix=[[70, 600], [0, 0]], share=[0, 1, -1, 0], seed=25).check()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_more_cuts_than_are_planned_together(kind):
+    # 513 cuts of 128 columns and more, each a block's; lists of more than 2048 tokens
+    g = torch.Generator().manual_seed(26)
+    lens = torch.randint(0, 90, (65, 4), generator=g).tolist()
+    lens[3] = [2300, 10, 2048, 0]
+    counts = [(130, 64, 1, 0, 129)[i % 5] for i in range(65)]
+    Case(kind, 64, lens, 130, counts=counts, group=1, windows=[[0, 30, 2200, 0]] * 65,
+         seed=26).check()
+
+
+@pytest.mark.parametrize("kind", TYPES)
 def test_a_prompt_from_nothing(kind):
     Case(kind, 128, [[0, 0]] * 3, 100, counts=[100, 33, 1], group=2, seed=11).check()
 

@@ -44,12 +44,26 @@ def test_plan():
     assert plan(_cfg(), _lists(), None, -1, size) == I
     assert plan(_cfg(), _lists(), None, 1, None) == I
     assert plan(_cfg(), _lists(lists=1 << 21), None, 20, size) == U
-    # a length's workspace holds every shorter one's
+
+
+@pytest.mark.parametrize("kind", ("BF16", "INT8", "FP4"))
+@pytest.mark.parametrize("rows,heads,group,tokens", (
+    (3, 4, 2, 9), (1, 1, 1, 17), (1, 8, 4, 8), (4, 8, 4, 256), (40, 32, 1, 5), (512, 32, 1, 3),
+    (300, 32, 4, 64), (2000, 8, 1, 1), (1, 2, 16, 500)))
+@pytest.mark.parametrize("shared", (False, True))
+def test_workspaces_hold_every_shorter_length(kind, rows, heads, group, tokens, shared):
+    # also where longer lists go to the other kind of blocks, and in what a launch asks for
+    cfg = _cfg(kv_type=getattr(B, f"HEADKV_KV_{kind}"), kv_heads=heads, group=group)
+    more = _lists(lists=2, max_len=2000, max_pages=40) if shared else None
     last = 0
-    for n in range(0, 20000, 96):
-        need = B.headkv_paged_attn_tokens_plan(_cfg(), _lists(max_pages=400, max_len=n), None, 9)
-        assert need >= last
+    for n in list(range(0, 4200, 60)) + list(range(4200, 140000, 1777)):
+        own = _lists(lists=rows, max_pages=1 << 12, max_len=n)
+        need = B.headkv_paged_attn_tokens_plan(cfg, own, more, tokens)
+        assert need >= last, n
         last = need
+    # what lists of many rows take does not grow with their length
+    if rows * heads * tokens >= 1 << 14 and not shared:
+        assert last < 1 << 31
 
 
 def test_grids(call):  # noqa: F811
@@ -57,9 +71,17 @@ def test_grids(call):  # noqa: F811
            "{most}), None, None, {tokens}, None, None, FAKE, 0, 0, FAKE, None, FAKE, 1 << 62, None)")
     # 16 / group tokens to a cut
     for rows, heads, group, tokens, cuts in ((3, 2, 1, 16, 1), (3, 2, 1, 17, 2), (3, 2, 3, 5, 1),
-                                             (3, 2, 3, 6, 2), (3, 2, 16, 7, 7)):
+                                             (3, 2, 3, 6, 2), (3, 2, 16, 3, 3)):
         st, got = call(run.format(rows=rows, heads=heads, group=group, tokens=tokens, most=100))
         assert st == B.HEADKV_OK and got == [(rows * heads * cuts, 256)], got
+    # 128 / group of them, in blocks of 512 threads, where there is work for them
+    for rows, heads, group, tokens, cuts in ((300, 2, 4, 64, 2), (300, 2, 4, 65, 3),
+                                             (300, 2, 3, 86, 3), (300, 2, 16, 16, 2)):
+        st, got = call(run.format(rows=rows, heads=heads, group=group, tokens=tokens, most=200))
+        assert st == B.HEADKV_OK and got == [(rows * heads * cuts, 512)], got
+    # few cuts: one block for each CU at most, and the sum of parts
+    st, got = call(run.format(rows=4, heads=8, group=4, tokens=256, most=3000))
+    assert st == B.HEADKV_OK and got[0] == (256, 512) and got[1][1] == 256 and len(got) == 2, got
     st, got = call(run.format(rows=1 << 14, heads=1024, group=16, tokens=1, most=4000))
     assert st == B.HEADKV_OK and all(g * b < 1 << 32 for g, b in got)
 
