@@ -1817,19 +1817,19 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
 // more however short the list is.  Times of the first over the second, tokens from memory,
 // the longest list four times the shortest, one call after the other:
 //   columns of a row and head     24    32    48    64    96   128
-//   1024 lists of up to 2048 INT8 1.05  1.05  1.38  1.65  1.82  2.12
-//                            FP4  .74   .74   .97  1.19  1.31  1.60
-//                            BF16 1.83  1.79  2.45  3.13  3.87  4.47
-//   1024 of up to 256        INT8 1.00  1.01  1.17  1.18  1.32  1.48
-//                            FP4  .84   .83   .98  1.13   .95  1.06
-//                            BF16 1.25  1.25  1.52  1.67  2.05  2.37
-//   32 of up to 2048         INT8 .79   .80   .88   .81   .83   .94
-//                            FP4  .71   .71   .76   .68   .69   .73
-//                            BF16 .95   .94  1.06  1.04  1.10  1.20
+//   1024 lists of up to 2048 INT8 1.30  1.31  1.74  1.98  2.11  2.40
+//                            FP4  .93   .92  1.22  1.48  1.62  1.87
+//                            BF16 2.10  2.08  2.93  3.77  4.28  4.97
+//   1024 of up to 256        INT8 1.03  1.03  1.19  1.23  1.34  1.52
+//                            FP4  .84   .84   .99  1.12   .95  1.05
+//                            BF16 1.25  1.29  1.51  1.58  2.04  2.37
+//   32 of up to 2048         INT8                   .82   .83   .95
+//                            FP4                    .69   .70   .72
+//                            BF16                        1.09  1.18
 // so by the columns and by the work, in tiles of 16 columns and tokens of a list.
 static bool is_wide(const PagedDims& c, int64_t lists, int64_t columns, int64_t reach) {
     const bool fp4 = c.type == kFp4;
-    return columns >= (fp4 ? 49 : 17) &&
+    return columns >= (fp4 ? 33 : 17) &&
            lists * ((columns + 15) / 16) * reach >= (fp4 ? 1 << 20 : 1 << 19);
 }
 static bool cut_rows(PagedDims* c, PagedLists* own, int tokens, bool wide, int* cuts, int* cut) {

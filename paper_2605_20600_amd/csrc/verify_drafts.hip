@@ -2,14 +2,13 @@
 // the decisions, and the next token by a running sum over one position.
 //
 // Decisions next to a border must not depend on the order of a sum, so exponentials and
-// sums have 64 bits: 2^y by its Taylor series about the nearest whole power, which is off
-// by 2^-47 at most.  (The vector ALU does a product and sum of 64 bits in the time of one
+// sums have 64 bits.  (The vector ALU does a product and sum of 64 bits in the time of one
 // of 32.)
 // k_verify_sums: a block takes a segment of one position's target or draft logits into
 // registers and leaves its maximum and its sum relative to that; the block that brings the
 // last part of a row adds them up, decides on the drafts and writes all results but the next
-// token.  k_verify_next: a block for each segment of the one position that the next token
-// is drawn from leaves its sum of r; the last one of a row finds the segment, takes its
+// token.  k_verify_next: a wavefront for each piece of the one position that the next token
+// is drawn from leaves its sum of r; one of the row's last block finds the piece, takes its
 // logits again and finds the token in it.
 #include <hip/hip_runtime.h>
 
@@ -43,27 +42,48 @@ struct Next {
     double p_inv, q_inv;  // 1 / sum; q_inv = 0: no draft to subtract
 };
 
-// 2^y for y <= 0.
-__device__ __forceinline__ double exp2_below(double y) {
-    y = fmax(y, -1100.0);  // (0 from there on)
-    const double n = __builtin_rint(y), f = (y - n) * kLn2;
-    double p = 1.0 / 39916800;  // 1 / 11!
-    p = fma(p, f, 1.0 / 3628800);
-    p = fma(p, f, 1.0 / 362880);
-    p = fma(p, f, 1.0 / 40320);
-    p = fma(p, f, 1.0 / 5040);
-    p = fma(p, f, 1.0 / 720);
-    p = fma(p, f, 1.0 / 120);
-    p = fma(p, f, 1.0 / 24);
-    p = fma(p, f, 1.0 / 6);
-    p = fma(p, f, 0.5);
-    p = fma(p, f, 1.0);
-    p = fma(p, f, 1.0);
-    return __builtin_ldexp(p, (int)n);
-}
-// e^((x - m) / temperature), m the largest logit (not -inf)
-__device__ __forceinline__ double share_of(float x, float m, double k) {
-    return exp2_below(((double)x - (double)m) * k);
+// 2^(j / 32), rounded.
+__constant__ const double kPowers[32] = {
+    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
+    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+};
+struct Powers {
+    double of[32];
+    __device__ __forceinline__ void fill() {  // before a barrier
+        if (threadIdx.x < 32) of[threadIdx.x] = kPowers[threadIdx.x];
+    }
+    // e^((x - m) / temperature), m the largest logit (not -inf): 2^y, y = k times the difference
+    // with k = log2(e) / T, in 32nds.  A sum with 1.5 2^52 leaves the nearest whole number of
+    // them in its low bits; what is left, at most half a 32nd, has a Taylor series whose sixth
+    // term is below 2^-48; 32nds come from a table, whose entries lie in different banks
+    // each, and whole powers are added to the exponent.  Below 2^-1020 it is that, which no
+    // sum with the largest logit's 1 in it sees.
+    __device__ __forceinline__ double share(float x, float m, double k) const {
+        constexpr double kLeast = -1020.0 * 32, kMagic = 0x1.8p52, c = 0.69314718055994530942 / 32;
+        const double y = fmax(((double)x - (double)m) * (32 * k), kLeast);
+        const double t = y + kMagic, f = y - (t - kMagic);
+        const int n = (int)__builtin_bit_cast(uint64_t, t);
+        double p = c * c * c * c * c / 120;
+        p = fma(p, f, c * c * c * c / 24);
+        p = fma(p, f, c * c * c / 6);
+        p = fma(p, f, c * c / 2);
+        p = fma(p, f, c);
+        p = fma(p, f, 1.0);
+        p *= of[n & 31];
+        const uint64_t bits = __builtin_bit_cast(uint64_t, p);
+        const uint32_t high = (uint32_t)(bits >> 32) + ((uint32_t)(n >> 5) << 20);
+        return __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)bits);
+    }
+};
+// The same where what is 0 matters: 0 from 2^-1020 on.
+__device__ __forceinline__ double share_of(const Powers& p, float x, float m, double k) {
+    return ((double)x - (double)m) * k > -1020.0 ? p.share(x, m, k) : 0.0;
 }
 
 __device__ __forceinline__ double wave_add(double v) {
@@ -139,9 +159,13 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int segm
     __shared__ double row_sum[kMaxSlots];
     __shared__ uint64_t row_key[HEADKV_MAX_DRAFTS + 1];
     __shared__ int flag;
+    __shared__ Powers powers;
+    powers.fill();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool model = !GREEDY && a.draft;
-    const int seg = blockIdx.x % segments, rest = blockIdx.x / segments;
+    // (blocks go to the XCDs in turn: the same segments of all rows, which may be the only ones
+    // that are not masked, must not all go to the same)
+    const int rest = blockIdx.x / segments, seg = (blockIdx.x - rest * segments + rest) % segments;
     const int r = rest % a.rows, slot = rest / a.rows;
     // target and draft of a position beside each other
     const int pos = model ? slot >> 1 : slot;
@@ -213,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int segm
 #pragma unroll
             for (int v = 0; v < Values::NV; ++v)
 #pragma unroll
-                for (int e = 0; e < Values::N; ++e) s += share_of(x.at(v, e), m, a.k);
+                for (int e = 0; e < Values::N; ++e) s += powers.share(x.at(v, e), m, a.k);
         }
         s = wave_add(s);
         if (lane == 0) sums[wave] = s;
@@ -251,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int segm
             for (int j = lane; j < segments; j += 64) {
                 const float t = __uint_as_float((uint32_t)read(p[j].w + 1));
                 if (t > -INFINITY)
-                    s += __builtin_bit_cast(double, read(p[j].w)) * share_of(t, top, a.k);
+                    s += __builtin_bit_cast(double, read(p[j].w)) * share_of(powers, t, top, a.k);
             }
             s = wave_add(s);
             none = __builtin_amdgcn_ballot_w64(none) != 0;
@@ -291,13 +315,13 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int segm
                 next.q_inv = row_sum[p + 1] > 0 ? 1.0 / row_sum[p + 1] : 0.0;
                 q = 0.0;
                 if (!fails && next.q_inv > 0)
-                    q = share_of(value_at(draft_row<T>(a, r, lane), token), m, a.k) * next.q_inv;
+                    q = share_of(powers, value_at(draft_row<T>(a, r, lane), token), m, a.k) * next.q_inv;
             } else {
                 next.gone = token;
             }
             if (!fails) {
                 const float x = value_at(target_row<T>(a, r, lane), token);
-                const double share = share_of(x, next.p_max, a.k) * next.p_inv;
+                const double share = share_of(powers, x, next.p_max, a.k) * next.p_inv;
                 const double u = a.uniforms[(int64_t)r * (a.drafts + 1) + lane];
                 keeps = u < 1.0 && fmax(u, 0.0) * q < share;
                 logprob = (float)((((double)x - (double)next.p_max) * a.k + log2(next.p_inv)) * kLn2);
@@ -319,131 +343,11 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int segm
     }
 }
 
-// r of a segment: the sum of each thread's vectors.
-template <typename T, int EPT>
-struct Rest {
-    using Values = Logits<T, kThreads, EPT>;
-    static constexpr int NV = Values::NV, N = Values::N, SEG = kThreads * EPT;
-    Values p, q;
-    int first, lo, hi;
-
-    // one value's r; both rows' vectors may start at different values of the row
-    __device__ __forceinline__ double at(const VerifyArgs& a, const Next& n, const T* draft, int v,
-                                         int e, int tid) const {
-        const int i = first + (v * kThreads + tid) * N + e;  // in the row
-        double r = 0;
-        const float x = p.at(v, e);
-        if (x > -INFINITY && i != n.gone) r = share_of(x, n.p_max, a.k) * n.p_inv;
-        if (n.q_inv > 0 && r > 0) {
-            const float y = value_at(draft, i);
-            if (y > -INFINITY) r = fmax(r - share_of(y, n.q_max, a.k) * n.q_inv, 0.0);
-        }
-        return r;
-    }
-};
-
-template <typename T, int EPT>
-__global__ __launch_bounds__(kThreads) void k_verify_next(VerifyArgs a, int segments,
-                                                          uint64_t* segment_sums, const Next* nexts,
-                                                          int* arrived) {
-    using Values = Rest<T, EPT>;
-    constexpr int NV = Values::NV, N = Values::N, SEG = Values::SEG;
-    __shared__ double chunks[NV * kWaves];
-    __shared__ int flag, where;
-    __shared__ double before;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int seg = blockIdx.x % segments, r = blockIdx.x / segments;
-    Next n = nexts[r];
-    if (n.pos < 0) return;
-    const T* row = target_row<T>(a, r, n.pos);
-    const T* draft = n.q_inv > 0 ? draft_row<T>(a, r, n.pos) : nullptr;
-    Values x;
-    double s[NV];  // of the thread's vectors
-    // the segment's sum, the same for all threads; chunks holds those of its parts
-    auto sum_of = [&](int seg) {
-        const Place<T> at(row, a.vocab, seg, SEG);
-        x.first = at.first;
-        x.p.load(at.p, at.lo, at.hi, tid);
-        __syncthreads();  // chunks is read no more
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            s[v] = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) s[v] += x.at(a, n, draft, v, e, tid);
-            const double t = wave_add(s[v]);
-            if (lane == 0) chunks[v * kWaves + wave] = t;
-        }
-        __syncthreads();
-        double all = 0;
-        for (int i = 0; i < NV * kWaves; ++i) all += chunks[i];
-        return all;
-    };
-    const double mine = sum_of(seg);
-    uint64_t* of_row = segment_sums + (int64_t)r * segments;
-    if (tid == 0) publish(of_row + seg, __builtin_bit_cast(uint64_t, mine));
-    if (!last_of(arrived + r, segments, &flag)) return;
-
-    // the segment that holds the token: every wavefront for itself
-    double u = a.uniforms[(int64_t)r * (a.drafts + 1) + a.drafts];
-    u = u < 1.0 ? fmax(u, 0.0) : 0x1.fffffep-1;  // (NaN: the largest, too)
-    auto sum_at = [&](int i) {
-        return i < segments ? __builtin_bit_cast(double, read(of_row + i)) : 0.0;
-    };
-    double total = 0;
-    for (int i = 0; i < segments; i += 64) total += wave_add(sum_at(i + lane));
-    int found = -1;
-    double sum = 0, want = u * total;
-    if (total < 0x1p-40) {  // nothing to speak of: p itself
-        n.gone = -1;
-        n.q_inv = 0;
-        want = u;
-        for (int i = 0; i < segments; ++i) {
-            const double t = sum_of(i);
-            if (t > 0) found = i, before = sum;  // the last of them, if rounding leaves none
-            if (sum + t > want) break;
-            sum += t;
-        }
-    } else {
-        for (int i = 0; i < segments; i += 64) {
-            const double t = sum_at(i + lane);
-            double up = t;
-#pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                const double y = __shfl_up(up, o);
-                if (lane >= o) up += y;
-            }
-            const uint64_t over = __builtin_amdgcn_ballot_w64(t > 0 && sum + up > want);
-            const uint64_t some = __builtin_amdgcn_ballot_w64(t > 0);
-            const int pick = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : -1;
-            if (pick >= 0) {
-                found = i + pick;
-                const double b = sum + __shfl(up - t, pick);
-                if (tid == 0) before = b;
-            }
-            if (over) break;
-            sum += __shfl(up, 63);
-        }
-    }
-    __syncthreads();
-    sum_of(found);
-    // the vectors of a wavefront that hold it
-    if (tid == 0) {
-        double sum = before;
-        int pick = 0;
-        for (int i = 0; i < NV * kWaves; ++i) {
-            const double t = chunks[i];
-            if (t > 0) pick = i, before = sum;
-            if (t > 0 && sum + t > want) break;
-            sum += t;
-        }
-        where = pick;
-    }
-    __syncthreads();
-    if (wave != where % kWaves) return;
-    const int v = where / kWaves;
-    double t = s[0];
-#pragma unroll
-    for (int i = 1; i < NV; ++i) t = v == i ? s[i] : t;
+// The first of 64 lanes, or the last with any, at which the running sum from `before` on
+// passes `want`; *passed: it does.  -1: no lane has any.
+__device__ __forceinline__ int find_lane(double t, double before, double want, bool* passed,
+                                         double* at, double* total) {
+    const int lane = threadIdx.x & 63;
     double up = t;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
@@ -452,21 +356,141 @@ __global__ __launch_bounds__(kThreads) void k_verify_next(VerifyArgs a, int segm
     }
     const uint64_t over = __builtin_amdgcn_ballot_w64(t > 0 && before + up > want);
     const uint64_t some = __builtin_amdgcn_ballot_w64(t > 0);
-    if (lane != (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) return;
-    double at = before + (up - t);
-    int token = -1;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (i != v) continue;
-        bool done = false;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const double y = x.at(a, n, draft, i, e, tid);
-            if (done || !(y > 0)) continue;
-            token = x.first + (i * kThreads + tid) * N + e;
-            at += y;
-            done = at > want;
+    const int pick = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : -1;
+    *passed = over != 0;
+    *at = before + __shfl(up - t, max(pick, 0));
+    *total = __shfl(up, 63);
+    return pick;
+}
+
+// A wavefront for `per` pieces of a row one after the other, kPiece values each: a block
+// costs some 9 us, most of them for its sums to arrive, so there are no more than a few for each
+// CU (128 rows of 65536: 38 us with 4096 blocks, 30 with 1024).  There is one place that computes a
+// piece's r: with one for each of its uses the code does not stay in the instruction cache.
+constexpr int kPieceEpt = 8, kPiece = 64 * kPieceEpt;
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_verify_next(VerifyArgs a, int blocks, int per,
+                                                          uint64_t* sums, const Next* nexts,
+                                                          int* arrived) {
+    using Values = Logits<T, 64, kPieceEpt>;
+    constexpr int NV = Values::NV, N = Values::N;
+    __shared__ int flag;
+    __shared__ Powers powers;
+    __shared__ double values[kWaves][kPiece];  // r of a wavefront's piece
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = blockIdx.x / blocks, pieces = blocks * kWaves * per;
+    Next n = nexts[r];
+    if (n.pos < 0) return;
+    powers.fill();
+    __syncthreads();
+    const T* row = target_row<T>(a, r, n.pos);
+    const T* draft = n.q_inv > 0 ? draft_row<T>(a, r, n.pos) : nullptr;
+    uint64_t* of_row = sums + (int64_t)r * pieces;
+    auto sum_at = [&](int i) {
+        return i < pieces ? __builtin_bit_cast(double, read(of_row + i)) : 0.0;
+    };
+    double u = a.uniforms[(int64_t)r * (a.drafts + 1) + a.drafts];
+    u = u < 1.0 ? fmax(u, 0.0) : 0x1.fffffep-1;  // (NaN: the largest, too)
+
+    // first every wavefront its own piece; then, by one, the piece that holds the token (and
+    // where there is no r to speak of, one after the other with p in its place)
+    enum { kOwn, kEach, kFound } now = kOwn;
+    int piece = ((blockIdx.x - r * blocks) * kWaves + wave) * per, found = 0, first;
+    const int end = piece + per;
+    double before = 0, sum = 0, want = 0;
+    for (;;) {
+        const Place<T> at(row, a.vocab, piece, kPiece);
+        first = at.first;
+        Values p, q;
+        p.load(at.p, at.lo, at.hi, lane);
+        bool beside = false;  // the draft's vectors start at the same values
+        if (draft) {
+            const Place<T> other(draft, a.vocab, piece, kPiece);
+            beside = other.first == at.first;
+            if (beside) q.load(other.p, other.lo, other.hi, lane);
         }
+        double mine = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int j = (v * 64 + lane) * N + e;
+                const float x = p.at(v, e);
+                double y = 0;
+                if (x > -INFINITY && first + j != n.gone) {
+                    y = share_of(powers, x, n.p_max, a.k) * n.p_inv;
+                    if (draft) {
+                        const float z = beside ? q.at(v, e) : value_at(draft, first + j);
+                        y = fmax(y - share_of(powers, z, n.q_max, a.k) * n.q_inv, 0.0);
+                    }
+                }
+                values[wave][j] = y;
+                mine += y;
+            }
+        mine = wave_add(mine);
+        if (now == kFound) break;
+        if (now == kOwn) {
+            if (lane == 0) publish(of_row + piece, __builtin_bit_cast(uint64_t, mine));
+            if (++piece < end) continue;
+            if (!last_of(arrived + r, blocks, &flag) || wave > 0) return;
+            double total = 0;
+            for (int i = 0; i < pieces; i += 64) total += wave_add(sum_at(i + lane));
+            if (total < 0x1p-40) {
+                n.gone = -1;
+                draft = nullptr;
+                want = u;
+                now = kEach;
+                piece = 0;
+                continue;
+            }
+            want = u * total;
+            for (int i = 0; i < pieces; i += 64) {
+                bool passed;
+                double at, all;
+                const int pick = find_lane(sum_at(i + lane), sum, want, &passed, &at, &all);
+                if (pick >= 0) found = i + pick, before = at;
+                if (passed) break;
+                sum += all;
+            }
+        } else {
+            if (mine > 0) found = piece, before = sum;  // the last of them, if rounding leaves none
+            sum += mine;
+            if (!(sum > want) && piece + 1 < pieces) {
+                ++piece;
+                continue;
+            }
+        }
+        piece = found;
+        now = kFound;
+    }
+    // lane i: the vector's values i N to i N + N - 1
+    int at_v = 0, at_lane = 0;
+    sum = before;
+#pragma unroll 1
+    for (int v = 0; v < NV; ++v) {
+        double t = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) t += values[0][(v * 64 + lane) * N + e];
+        bool passed;
+        double at, all;
+        const int pick = find_lane(t, sum, want, &passed, &at, &all);
+        if (pick >= 0) at_v = v, at_lane = pick, before = at;
+        if (passed) break;
+        sum += all;
+    }
+    if (lane != at_lane) return;
+    int token = -1;
+    bool done = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const int j = (at_v * 64 + lane) * N + e;
+        const double y = values[0][j];
+        if (done || !(y > 0)) continue;
+        token = first + j;
+        before += y;
+        done = before > want;
     }
     const int64_t o = (int64_t)r * (a.drafts + 1) + n.pos;
     a.out_tokens[o] = token;
@@ -476,9 +500,10 @@ __global__ __launch_bounds__(kThreads) void k_verify_next(VerifyArgs a, int segm
 }
 
 constexpr int kLeastSegment = kThreads * 8;
+constexpr int kNextBlocks = 1024, kMostPieces = 16;
 
-// Segments of a row, which may start up to seven values into a vector.
-int segments_of(int vocab, int size) { return (vocab + 7 + size - 1) / size; }
+// Segments of a row that may start `lead` values into a vector.
+int segments_of(int vocab, int size, int lead = 7) { return (vocab + lead + size - 1) / size; }
 
 struct VerifyPlan {
     size_t nexts, sums, parts, bytes;  // offsets, and the total
@@ -489,7 +514,7 @@ VerifyPlan plan_of(int rows, int drafts, int vocab) {
     VerifyPlan p;
     p.nexts = kCounterBytes;
     p.sums = p.nexts + up(n * sizeof(Next));
-    p.parts = p.sums + up(n * segments * sizeof(uint64_t));
+    p.parts = p.sums + up(n * (segments + kMostPieces) * kWaves * sizeof(uint64_t));
     p.bytes = p.parts + n * (2 * drafts + 1) * segments * sizeof(Part);
     return p;
 }
@@ -500,7 +525,10 @@ int run(const VerifyArgs& a, const VerifyPlan& p, char* w, hipStream_t st) {
     auto* nexts = reinterpret_cast<Next*>(w + p.nexts);
     auto* sums = reinterpret_cast<uint64_t*>(w + p.sums);
     auto* parts = reinterpret_cast<Part*>(w + p.parts);
-    const int segments = segments_of(a.vocab, kThreads * EPT);
+    const bool even = (reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.draft) |
+                       ((a.row | a.token | a.draft_row | a.draft_token) * sizeof(T))) % 16 == 0;
+    const int lead = even ? 0 : 16 / (int)sizeof(T) - 1;
+    const int segments = segments_of(a.vocab, kThreads * EPT, lead);
     const int64_t slots = a.drafts + 1 + (a.draft && a.k ? a.drafts : 0);
     const unsigned grid = (unsigned)(slots * a.rows * segments);
     if (a.k == 0) {
@@ -509,8 +537,11 @@ int run(const VerifyArgs& a, const VerifyPlan& p, char* w, hipStream_t st) {
     }
     k_verify_sums<T, EPT, false><<<grid, kThreads, 0, st>>>(a, segments, parts, nexts, arrived);
     if (int e = (int)hipGetLastError()) return e;
-    k_verify_next<T, EPT><<<(unsigned)(a.rows * segments), kThreads, 0, st>>>(a, segments, sums,
-                                                                            nexts, arrived);
+    const int all = segments_of(a.vocab, kWaves * kPiece, lead);
+    const int per = (int)std::min<int64_t>(kMostPieces, ((int64_t)a.rows * all + kNextBlocks - 1) / kNextBlocks);
+    const int blocks = (all + per - 1) / per;
+    k_verify_next<T><<<(unsigned)(a.rows * blocks), kThreads, 0, st>>>(a, blocks, per, sums, nexts,
+                                                                      arrived);
     return (int)hipGetLastError();
 }
 
