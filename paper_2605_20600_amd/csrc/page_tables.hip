@@ -1,10 +1,12 @@
 // Page tables brought from one step to the next (what is done: headkv.h).
 //
-// A list's pages are looked at by one thread.  A prefix sum over the lists says where each
-// puts the pages that it frees, and after all of them are in the ring a second one which
-// ones it takes.  Few lists are one block's work, in one launch; many are cut among blocks,
-// which count in a first launch, free in a second and take in a third.  The start order is a
-// stable counting sort by a key of 8 bits, a block for each layer, beside the last part.
+// A list's places are looked at by four threads, a quarter each: one that ends has many.  A
+// prefix sum over the threads says where each puts the pages that it frees, and after all of
+// them are in the ring a second one which ones it takes.  Few lists are one block's work, in
+// one launch; many are cut among blocks, which count in a first launch, free in a second and
+// take in a third.  The start order is a stable counting sort by a key of 8 bits, a block for
+// each layer, beside the last part.  Bound by the loads that wait for each other, and the
+// launches: a few words are read and written for a list.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,6 +18,7 @@ namespace headkv {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kParts = 4, kLists = kThreads / kParts;  // threads of a list, lists of a block's turn
 constexpr int kBlocks = 512;  // at most, of many lists
 constexpr int kMostSorts = 4096;  // blocks that sort layers
 constexpr int kKeys = 256;
@@ -62,12 +65,16 @@ __device__ __forceinline__ bool held(const Call& c, int page) {
     return (uint32_t)page < (uint32_t)c.t.num_pages;
 }
 
-// f(place, page number) for places [p0, p1) of list i's table, the loads of eight at a time
-// in flight.
+// f(place, page number) for the thread's part of places [p0, p1) of list i's table, the
+// loads of eight at a time in flight.
 template <typename F>
 __device__ __forceinline__ void places(const Call& c, int i, int p0, int p1, F f) {
     const int32_t* table = c.t.pages + (int64_t)i * c.t.max_pages;
     p1 = min(p1, c.t.max_pages);
+    if (p0 >= p1) return;
+    const int n = p1 - p0, part = threadIdx.x % kParts;  // the thread's part of them
+    p1 = p0 + (int)((int64_t)n * (part + 1) / kParts);
+    p0 += (int)((int64_t)n * part / kParts);
     for (int p = p0; p < p1; p += 8) {
         int page[8];
 #pragma unroll
@@ -137,8 +144,8 @@ __device__ __forceinline__ uint32_t free_pages(const Call& c, int i0, int i1, ui
                                                uint32_t count, uint32_t before, uint32_t* scratch) {
     const uint32_t size = c.t.num_pages, end = (uint32_t)(((uint64_t)head + count) % size);
     uint32_t all = 0;
-    for (int base = i0; base < i1; base += kThreads) {
-        const int i = base + threadIdx.x;
+    for (int base = i0; base < i1; base += kLists) {
+        const int i = base + threadIdx.x / kParts;
         uint32_t mine = 0, total;
         List l;
         if (i < i1) {
@@ -159,8 +166,10 @@ __device__ __forceinline__ uint32_t free_pages(const Call& c, int i0, int i1, ui
                     table[p] = -1;
                 }
             });
-        c.t.len[i] = l.len;
-        c.t.first[i] = l.first;
+        if (threadIdx.x % kParts == 0) {  // (all have read them before the sum)
+            c.t.len[i] = l.len;
+            c.t.first[i] = l.first;
+        }
     }
     return all;
 }
@@ -176,8 +185,8 @@ __device__ __forceinline__ uint32_t take_pages(const Call& c, int i0, int i1, ui
                                                uint32_t count, uint32_t before, uint32_t* scratch) {
     const uint32_t size = c.t.num_pages;
     uint32_t all = 0;
-    for (int base = i0; base < i1; base += kThreads) {
-        const int i = base + threadIdx.x;
+    for (int base = i0; base < i1; base += kLists) {
+        const int i = base + threadIdx.x / kParts;
         uint32_t mine = 0, total;
         int len = 0, n = 0;
         if (i < i1) {
@@ -289,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void k_extend_count(Call c, Shared* sh) {
     __shared__ int sums[2][kWaves];
     const int i0 = blockIdx.x * c.chunk, i1 = min(i0 + c.chunk, c.lists);
     int frees = 0, needs = 0;
-    for (int i = i0 + threadIdx.x; i < i1; i += kThreads) {
+    for (int i = i0 + threadIdx.x / kParts; i < i1; i += kLists) {
         const List l = list_at(c, i);
         freed_places(c, i, l, [&](int, int page) { frees += held(c, page); });
         next_places(c, i, l.len, l.n, [&](int, int page) { needs += l.ends || !held(c, page); });
@@ -336,8 +345,10 @@ __global__ __launch_bounds__(kThreads) void k_extend_take(Call c, const Shared* 
     if (blockIdx.x == 0 && threadIdx.x == 0) write_state(c, sh->head, count, all);
 }
 
-// Lists up to which one block does all.
-constexpr int kFew = 2048;
+// Lists up to which one block does all, in one turn (one block and three launches, every
+// eighth list of 2480 tokens ending, in a graph: 512 lists 21 and 18 us, 1024 36 and 17, 2048
+// 69 and 19, 65536 - and 25; 256 of which none ends 8 in one block).
+constexpr int kFew = kLists;
 
 }  // namespace
 
@@ -358,7 +369,7 @@ int launch_extend(const headkv_paged_tables& t, const int32_t* advance, const in
         k_extend<<<1, kThreads, 0, st>>>(c);
         return (int)hipGetLastError();
     }
-    c.chunk = std::max(kThreads, (c.lists + kBlocks - 1) / kBlocks);
+    c.chunk = std::max(kLists, (c.lists + kBlocks - 1) / kBlocks);
     c.blocks = (c.lists + c.chunk - 1) / c.chunk;
     auto* sh = static_cast<Shared*>(ws);
     k_extend_count<<<c.blocks, kThreads, 0, st>>>(c, sh);

@@ -167,7 +167,7 @@ class PagedKV:
         if call.index != self.index:
             raise ValueError(f"q and k on cuda:{call.index} for a cache on {self.device}")
         B.headkv_paged_write_rotary(self.cfg, self.pool.data_ptr(), lists.arg, rotary.cfg,
-                                    _ptr(rotary.turns), _ptr(positions), tokens, _ptr(counts),
+                                    rotary._turns, _ptr(positions), tokens, _ptr(counts),
                                     call.q, call.k, v.data_ptr(), row_strides(v, "v", self.index),
                                     _stream(self.index))
         return call.q_out

@@ -41,23 +41,53 @@ def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str, index: int
 
 def row_strides(t: torch.Tensor, name: str, index: int) -> Tuple[int, int, int]:
     """Strides of bf16 [rows][tokens][heads][head_dim] with contiguous head rows."""
-    if t.dim() != 4 or t.dtype != torch.bfloat16 or t.get_device() != index or index < 0 \
-            or (t.stride(3) != 1 and t.shape[3] > 1):
+    stride = t.stride()
+    if len(stride) != 4 or t.dtype != torch.bfloat16 or t.get_device() != index or index < 0 \
+            or (stride[3] != 1 and t.shape[3] > 1):
         raise ValueError(f"{name} must be bf16 [rows][tokens][heads][head_dim] with contiguous "
                          f"heads on {'a GPU' if index < 0 else f'cuda:{index}'}, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
-    # the stride of a dimension of one is never used, and may be anything
-    a, b, c = (s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape))
-    return a, b, c
+    a, b, c, _ = t.shape
+    if a == 1 or b == 1 or c == 1:
+        # the stride of a dimension of one is never used, and may be anything
+        return (stride[0] if a > 1 else 0), (stride[1] if b > 1 else 0), (stride[2] if c > 1 else 0)
+    return stride[:3]
 
 
-class NormWeights(NamedTuple):
+class _Pair:
+    """A weight and a bias, checked once."""
+    __slots__ = ("weight", "bias", "arg", "heads", "dim", "index")
+
+    def __init__(self, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], name: str):
+        self.weight, self.bias = weight, bias  # kept alive with the pointers into them
+        self.heads = self.dim = self.index = None
+        for w in (weight, bias):
+            if w is None:
+                continue
+            if w.dtype != torch.float32 or w.dim() not in (1, 2) or w.get_device() < 0 \
+                    or not w.is_contiguous():
+                raise ValueError(f"{name}'s weights must be contiguous float32 [head_dim] or "
+                                 f"[heads][head_dim] on the GPU, got {w.dtype} {tuple(w.shape)} "
+                                 f"on {w.device}")
+            self.heads = w.shape[0] if w.dim() == 2 else None
+            self.dim, self.index = w.shape[-1], w.get_device()
+        if weight is not None and bias is not None \
+                and (weight.shape != bias.shape or weight.device != bias.device):
+            raise ValueError(f"{name}'s weight and bias must have one shape and device")
+        self.arg = _ptr(weight), _ptr(bias), int(self.heads is not None)
+
+
+class NormWeights:
     """Weights and biases of the norms: float32 [head_dim] for all heads or [heads][head_dim]
     for each (both of a pair the same), contiguous; None: ones and zeros."""
-    q_weight: Optional[torch.Tensor] = None
-    q_bias: Optional[torch.Tensor] = None
-    k_weight: Optional[torch.Tensor] = None
-    k_bias: Optional[torch.Tensor] = None
+
+    def __init__(self, q_weight: Optional[torch.Tensor] = None,
+                 q_bias: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 k_bias: Optional[torch.Tensor] = None):
+        self.q, self.k = _Pair(q_weight, q_bias, "q"), _Pair(k_weight, k_bias, "k")
+
+
+_ONES = NormWeights()
 
 
 class _Call(NamedTuple):
@@ -96,34 +126,27 @@ class Rotary:
         self.turns = torch.tensor(B.headkv_rotary_plan(self.cfg), dtype=torch.float64,
                                   device=device)
         self.index = self.turns.get_device()
+        self._turns = _ptr(self.turns)
 
-    def _arg(self, t, out, weight, bias, name) -> B.RotaryRowsArg:
-        strides = row_strides(t, name, self.index)
-        if t.shape[3] != self.head_dim:
-            raise ValueError(f"{name} has heads of {t.shape[3]} dims, not {self.head_dim}")
-        to = (0, 0, 0)
+    def _arg(self, t, out, pair, name) -> B.RotaryRowsArg:
+        index, shape = self.index, t.shape
+        strides = row_strides(t, name, index)
+        if shape[3] != self.head_dim:
+            raise ValueError(f"{name} has heads of {shape[3]} dims, not {self.head_dim}")
+        to, at = (0, 0, 0), None
         if out is not None:
-            if out.shape != t.shape:
-                raise ValueError(f"{name}_out must be {tuple(t.shape)}, got {tuple(out.shape)}")
-            to = row_strides(out, name + "_out", self.index)
-        heads = t.shape[2]
-        per_head = 0
-        if self.normed:
-            for w in (weight, bias):
-                if w is None:
-                    continue
-                if w.dtype != torch.float32 or w.get_device() != self.index \
-                        or not w.is_contiguous() \
-                        or w.shape not in ((self.head_dim,), (heads, self.head_dim)):
-                    raise ValueError(f"{name}'s weights must be contiguous float32 [head_dim] or "
-                                     f"[{heads}][head_dim] on cuda:{self.index}, got {w.dtype} "
-                                     f"{tuple(w.shape)} on {w.device}")
-                per_head = w.dim() - 1
-            if weight is not None and bias is not None and weight.shape != bias.shape:
-                raise ValueError(f"{name}'s weight and bias must have one shape")
-        return B.RotaryRowsArg(t.data_ptr(), _ptr(out), *strides, *to,
-                               _ptr(weight) if self.normed else None,
-                               _ptr(bias) if self.normed else None, heads, per_head)
+            if out.shape != shape:
+                raise ValueError(f"{name}_out must be {tuple(shape)}, got {tuple(out.shape)}")
+            to, at = row_strides(out, name + "_out", index), out.data_ptr()
+        heads, w = shape[2], (None, None, 0)
+        if self.normed and pair.dim is not None:
+            if pair.dim != self.head_dim or pair.index != index \
+                    or (pair.heads is not None and pair.heads != heads):
+                raise ValueError(f"{name}'s weights must be [{self.head_dim}] or [{heads}]"
+                                 f"[{self.head_dim}] on cuda:{index}, got [{pair.heads}]"
+                                 f"[{pair.dim}] on cuda:{pair.index}")
+            w = pair.arg
+        return B.RotaryRowsArg(t.data_ptr(), at, *strides, *to, w[0], w[1], heads, w[2])
 
     def rows(self, q, k, positions, weights, counts, q_out, k_out, cached=False) -> _Call:
         """The checked arguments of a call; cached: the keys' results go to a cache."""
@@ -143,15 +166,15 @@ class Rotary:
             _device_int32(positions, shape, "positions", self.index)
         if counts is not None:
             _device_int32(counts, (rows,), "counts", self.index)
-        w = weights or NormWeights()
+        w = weights or _ONES
         # what counts leave out is left as it is: zeros in what is allocated here
         empty = torch.empty if counts is None else torch.zeros
         if q is not None and q_out is None:
             q_out = empty(q.shape, dtype=torch.bfloat16, device=q.device)
         if k is not None and k_out is None and not cached:
             k_out = empty(k.shape, dtype=torch.bfloat16, device=k.device)
-        return _Call(None if q is None else self._arg(q, q_out, w.q_weight, w.q_bias, "q"),
-                     None if k is None else self._arg(k, k_out, w.k_weight, w.k_bias, "k"),
+        return _Call(None if q is None else self._arg(q, q_out, w.q, "q"),
+                     None if k is None else self._arg(k, k_out, w.k, "k"),
                      q_out, k_out, self.index, rows, tokens)
 
     def __call__(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor],
@@ -165,6 +188,6 @@ class Rotary:
         tokens of each row, behind which results are left as they are.  q_out and k_out may
         be q and k themselves."""
         call = self.rows(q, k, positions, weights, counts, q_out, k_out)
-        B.headkv_rotary(self.cfg, _ptr(self.turns), _ptr(positions), call.rows, call.tokens,
+        B.headkv_rotary(self.cfg, self._turns, _ptr(positions), call.rows, call.tokens,
                         _ptr(counts), call.q, call.k, _stream(self.index))
         return call.q_out, call.k_out

@@ -177,7 +177,7 @@ def test_what_a_table_should_not_hold():
 
 
 def test_as_many_lists_as_blocks_take_turns():
-    # a block of 512 takes its lists 1024 at a time
+    # a block of 512 takes its lists 256 at a time
     heads, rows, most = 64, 9000, 2
     tables = PageTables(heads, most, rows * heads * 2, rows, page_tokens=32)
     want = _state(tables, 32)

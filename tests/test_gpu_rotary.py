@@ -296,10 +296,12 @@ def test_refusals():
            dict(positions=pos.cpu()), dict(counts=pos[:1, 0]), dict(q=None, k=None),
            dict(q_out=x[:1]), dict(q_out=x.cpu()), dict(q=x.transpose(2, 3)),
            dict(weights=NormWeights(torch.ones(32, device="cuda"))),
-           dict(weights=NormWeights(torch.ones(64, device="cuda").double())),
-           dict(weights=NormWeights(torch.ones(64))),
-           dict(weights=NormWeights(torch.ones(64, device="cuda"),
-                                    torch.ones((4, 64), device="cuda")))]
+           dict(weights=NormWeights(k_bias=torch.ones((5, 64), device="cuda")))]
+    for w in ((torch.ones(64, device="cuda").double(),), (torch.ones(64),),
+              (torch.ones(64, device="cuda"), torch.ones((4, 64), device="cuda")),
+              (torch.ones((64, 4), device="cuda").t(),), (torch.ones((1, 4, 64), device="cuda"),)):
+        with pytest.raises(ValueError):
+            NormWeights(*w)
     for kw in bad:
         with pytest.raises(ValueError):
             rot(**{**ok, **kw})
