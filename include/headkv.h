@@ -617,7 +617,8 @@ headkv_status headkv_verify_drafts(const void* logits, const void* draft_logits,
  *   HEADKV_SCALE_BANDS   by m, the turns in original_len positions: omega if m >= high,
  *                        omega / factor if m <= low, between them the mean of the two by
  *                        how far on m is
- * (scale is 1 but for methods that sharpen or flatten the attention with it.)  Angles are
+ * (A row whose squares' sum passes fp32's range has an infinite one.  scale is 1 but for
+ * methods that sharpen or flatten the attention with it.)  Angles are
  * computed in 64 bits, for any int32 coordinate; results are rounded to bf16 once. */
 
 #define HEADKV_ROPE_HALF 0
@@ -671,7 +672,7 @@ headkv_status headkv_rotary_plan(const headkv_rotary_config* cfg, double* turns)
  * tokens of each row; what lies behind them in `out` is left as it is.  turns: device,
  * [rotary_dims / 2]; positions: int32 [rows][tokens][axes], device (both NULL allowed if
  * rotary_dims is 0).  q or k may be NULL or have no heads.  rows * tokens * (heads / 8 + 1)
- * may be 2^25; calls of four times that and more get HEADKV_ERR_UNSUPPORTED. */
+ * may be 2^25 (HEADKV_ERR_UNSUPPORTED where more does not fit a launch). */
 headkv_status headkv_rotary(const headkv_rotary_config* cfg, const double* turns,
                             const int32_t* positions, int32_t rows, int32_t tokens,
                             const int32_t* counts, const headkv_rotary_rows* q,

@@ -6,6 +6,7 @@ import math
 import pytest
 
 from paper_2605_20600_amd import binding as B
+from test_paged_launch_host import call  # noqa: F401  (a fixture)
 
 FAKE = 0x7F0000000000  # 256-byte aligned, never dereferenced by these calls
 I, U = B.HEADKV_ERR_INVALID_ARG, B.HEADKV_ERR_UNSUPPORTED
@@ -162,3 +163,26 @@ def test_other_arguments():
     assert _write(positions=None) == I
     assert _status("headkv_paged_write_rotary", _cfg(), FAKE, _lists(), _rot(), FAKE, FAKE, 1,
                    None, None, None, FAKE, 0, 0, 0, None) == I
+
+
+ROWS_ARG = "B.RotaryRowsArg(FAKE, FAKE, 128, 128, 128, 128, 128, 128, None, None, {heads}, 0)"
+
+
+def test_grids(call):  # noqa: F811
+    rot = "B.RotaryConfig({d}, 64, 0, 1, 0, 0, 1, 0, 0, 1, 0, 0, 0)"
+    run = "L.headkv_rotary(" + rot + ", FAKE, FAKE, {rows}, {tokens}, None, " + ROWS_ARG + ", None, None)"
+    # a token's heads among as many wavefronts as there are steps of 8, or as fill the card
+    for rows, tokens, heads, waves in ((1, 1, 1, 1), (8, 1, 64, 64), (8, 1, 65, 72),
+                                       (100, 100, 64, 10000)):
+        st, got = call(run.format(d=128, rows=rows, tokens=tokens, heads=heads))
+        assert st == B.HEADKV_OK and got == [((waves + 3) // 4, 256)], got
+    st, got = call(run.format(d=64, rows=1 << 12, tokens=1 << 13, heads=1))
+    assert st == B.HEADKV_OK and got[0][0] * got[0][1] < 1 << 32
+    st, got = call(run.format(d=64, rows=1 << 14, tokens=1 << 13, heads=1))
+    assert st == U and not got
+    write = ("L.headkv_paged_write_rotary(cfg(head_dim={d}, kv_heads={heads}), FAKE, lists({rows}), "
+             + rot + ", FAKE, FAKE, {tokens}, None, None, " + ROWS_ARG + ", FAKE, 128, 128, 128, None)")
+    for d in (64, 128):
+        for tokens in (1, 4, 5):  # as many lists as there may be
+            st, got = call(write.format(d=d, rows=1 << 14, heads=1024, tokens=tokens))
+            assert st == B.HEADKV_OK and len(got) == 1 and got[0][0] * got[0][1] < 1 << 32
