@@ -8,15 +8,14 @@
 // 16) heads of one token at a time, works the token's angles out once and goes on to its
 // other heads.  Queries and keys are one sequence of heads; a token's heads are shared by
 // as many wavefronts as it takes to fill the card.
-// Angles: turns = position * (omega / 2 pi) in 64 bits, of which the nearest whole number
-// is taken off before what is left, at most 1/2, is rounded to 32, for a sine and a cosine
-// that the hardware gives to 2^-22.9 there.  The rest is fp32, the one rounding to bf16 at the
+// Angles: turns = position * (omega / 2 pi) in 64 bits, of which the nearest quarter is taken
+// off before what is left is rounded to 32.  The rest is fp32, the one rounding to bf16 at the
 // end; a cache quantises the bf16 values, as it would those of a call of its own, so that both
 // ways give the same bits.
 // One MI355X: 32768 tokens of 40 heads of 128, half of a head turned, RMS norms: 160 us, 4.2
 // TB/s, of the 5.2 that a copy reaches, the vector ALU's norm and conversions beside it; 16
 // prompts of up to 2352 tokens, 32 heads of 128, queries back, keys and values into INT8: 88
-// us; five tokens of 256 rows, 20 heads of 64 into FP4: 10 us; one token of 8 rows 5 us, the
+// us; five tokens of 256 rows, 20 heads of 64 into FP4: 11 us; one token of 8 rows 5.5 us, the
 // loads that wait for each other.
 #include <hip/hip_runtime.h>
 
@@ -53,6 +52,28 @@ __device__ __forceinline__ float lanes_add(float v) {
 
 __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)a, (__bf16)b});
+}
+
+// Sine and cosine of t turns: what is left of the nearest quarter, in 32 bits, by their Taylor
+// series, whose next terms are below 2^-29, and the quarter by which is which and its sign.
+// (The hardware's own, of a rest of up to half a turn, are off by 2^-22.9, and a token of 8 rows
+// takes 4.9 us with them: more of what is quantised after them comes out a step away.)
+__device__ __forceinline__ void sine_of_turns(double t, float* sine, float* cosine) {
+    const double quarters = __builtin_rint(4 * t);
+    const float x = 6.2831853071795865f * (float)(t - 0.25 * quarters), y = x * x;
+    const int n = (int)(quarters - 4 * __builtin_floor(0.25 * quarters));
+    float s = fmaf(y, 1.f / 362880, -1.f / 5040);
+    s = fmaf(y, s, 1.f / 120);
+    s = fmaf(y, s, -1.f / 6);
+    s = fmaf(x * y, s, x);
+    float c = fmaf(y, -1.f / 3628800, 1.f / 40320);
+    c = fmaf(y, c, -1.f / 720);
+    c = fmaf(y, c, 1.f / 24);
+    c = fmaf(y, c, -0.5f);
+    c = fmaf(y, c, 1.f);
+    const float u = n & 1 ? c : s, v = n & 1 ? s : c;
+    *sine = n & 2 ? -u : u;
+    *cosine = (n + 1) & 2 ? -v : v;
 }
 
 struct Call {
@@ -162,9 +183,10 @@ __device__ __forceinline__ void turn_rows(const Call& call, uint16_t* tops) {
         for (int j = 0; j < 8; ++j) {
             const int pair = 8 * u + j;
             const double t = (double)(pair < a.r / 2 / a.axes ? first : second) * a.turns[pair];
-            const float rest = (float)(t - __builtin_rint(t));
-            cs[j] = a.scale * __builtin_amdgcn_cosf(rest);
-            sn[j] = a.scale * __builtin_amdgcn_sinf(rest);
+            float s, c;
+            sine_of_turns(t, &s, &c);
+            cs[j] = a.scale * c;
+            sn[j] = a.scale * s;
         }
     }
 

@@ -13,8 +13,7 @@ from typing import Dict, Optional, Tuple
 import torch
 
 from . import binding as B
-from .paged import _LOGITS, _new_workspace
-from .rotary import _device_int32, _stream
+from .paged import _LOGITS, _device_int32, _new_workspace, _stream
 from .session import _ptr
 
 _verify_ws: Dict[Tuple[int, int], torch.Tensor] = {}  # per device and stream

@@ -12,8 +12,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from .paged import Lists
-from .rotary import _device_int32, _stream
+from .paged import Lists, _device_int32, _stream
 from .session import _ptr
 
 

@@ -8,13 +8,54 @@ current device and its current stream; tensors that lie elsewhere are refused.
 from __future__ import annotations
 
 from functools import lru_cache
-from typing import Dict, List, Optional, Tuple, Union
+from typing import TYPE_CHECKING, Dict, List, Optional, Tuple, Union
 
 import torch
 
 from . import binding as B
-from .rotary import NormWeights, Rotary, _device_int32, _stream, row_strides
 from .session import _ptr
+
+if TYPE_CHECKING:
+    from .rotary import NormWeights, Rotary
+
+
+# torch's public calls where a torch has no such private ones, which cost less (see
+# Session.stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _stream(index: int) -> int:
+    """The current stream, of device `index`."""
+    if _current_device() != index:
+        raise ValueError(f"tensors on cuda:{index}, but the current device is "
+                         f"cuda:{_current_device()}")
+    return _raw_stream(index)
+
+
+def _device_int32(t: torch.Tensor, shape: Tuple[int, ...], name: str, index: int) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.shape != shape or t.get_device() != index or index < 0 \
+            or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on "
+                         f"{'a GPU' if index < 0 else f'cuda:{index}'}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+def row_strides(t: torch.Tensor, name: str, index: int) -> Tuple[int, int, int]:
+    """Strides of bf16 [rows][tokens][heads][head_dim] with contiguous head rows."""
+    stride = t.stride()
+    if len(stride) != 4 or t.dtype != torch.bfloat16 or t.get_device() != index or index < 0 \
+            or (stride[3] != 1 and t.shape[3] > 1):
+        raise ValueError(f"{name} must be bf16 [rows][tokens][heads][head_dim] with contiguous "
+                         f"heads on {'a GPU' if index < 0 else f'cuda:{index}'}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    a, b, c, _ = t.shape
+    if a == 1 or b == 1 or c == 1:
+        # the stride of a dimension of one is never used, and may be anything
+        return (stride[0] if a > 1 else 0), (stride[1] if b > 1 else 0), (stride[2] if c > 1 else 0)
+    return stride[:3]
 
 
 def _new_workspace(need: int, device) -> torch.Tensor:

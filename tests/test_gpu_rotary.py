@@ -321,3 +321,36 @@ def test_refusals():
             c.write_rotary(**{**dict(lists=lists, rotary=rot, q=x, k=x, v=x, positions=pos), **kw})
     # nothing to write
     assert c.write_rotary(lists, rot, x[:, :0], x[:, :0], x[:, :0], pos[:, :0]).shape[1] == 0
+
+
+def test_other_devices(monkeypatch):
+    # nothing is launched unless every tensor and the current device are one (another device
+    # is stood in for: the check runs before anything is launched)
+    from paper_2605_20600_amd import paged
+    from paper_2605_20600_amd.drafts import verify_drafts
+    from paper_2605_20600_amd.page_tables import PageTables
+    rot = Rotary(64)
+    x = torch.ones((1, 4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros((1, 4), dtype=torch.int32, device="cuda")
+    cache = _cache("bf16", 64, 2, 6, page_tokens=32)
+    lists = cache.lists(torch.arange(6, dtype=torch.int32, device="cuda").view(1, 2, 3), None, 0)
+    tables = PageTables(2, 3, 6, 1)
+    logits = torch.zeros((1, 2, 9), device="cuda")
+    state = [t.clone() for t in (x, cache.pool, tables.buffer)]
+    monkeypatch.setattr(paged, "_current_device", lambda: cache.index + 1)
+    for f in (lambda: rot(x, None, pos, q_out=x), lambda: tables.extend(3),
+              lambda: cache.write_rotary(lists, rot, x, x, x, pos),
+              lambda: cache.attn_tokens(lists, x),
+              lambda: verify_drafts(logits, pos[:, :1], logits[:, :, 0].contiguous())):
+        with pytest.raises(ValueError, match="current device"):
+            f()
+    torch.cuda.synchronize()
+    for a, b in zip(state, (x, cache.pool, tables.buffer)):
+        assert torch.equal(a, b)
+    monkeypatch.undo()
+    other = cache.lists(lists.pages, None, 0)
+    cache.index += 1
+    for f in (lambda: cache.write_rotary(other, rot, x, x, x, pos),
+              lambda: cache.attn_tokens(other, x)):
+        with pytest.raises(ValueError):
+            f()
