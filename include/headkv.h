@@ -652,7 +652,8 @@ typedef struct headkv_rotary_config {
 /* Query or key rows of a call: head h of token i of row b starts in_row b + in_token i +
  * in_head h elements on (strides >= 0, multiples of 8; bf16, device, 16-byte aligned),
  * and so its result in `out`.  out may be in with the same strides; else they must not
- * overlap. */
+ * overlap.  Rows of out must not overlap each other (a stride below d where there are two is
+ * refused; the caller sees to the rest). */
 typedef struct headkv_rotary_rows {
     const uint16_t* in;
     uint16_t* out;
