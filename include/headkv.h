@@ -445,10 +445,12 @@ headkv_status headkv_paged_attn(const headkv_paged_config* cfg, const void* pool
  * q: bf16, device, 16-byte aligned, token i of row b at q + b q_row_stride + i q_token_stride
  * (multiples of 8, >= 0), there [kv_heads * group][d].  out: [batch][tokens][kv_heads *
  * group][d] fp32, 16-byte aligned; lse: [batch][tokens][kv_heads * group] fp32 or NULL; rows
- * of tokens behind counts[b] are left as they are.  What else is said of headkv_paged_attn
- * holds, the workspace's size being headkv_paged_attn_tokens_plan's, which need not grow with
- * `tokens`.  With 16 / group (rounded down, at least 1) tokens to a cut, batch * kv_heads *
- * cuts of a row may be 2^24, and tokens too (HEADKV_ERR_UNSUPPORTED beyond). */
+ * of tokens behind counts[b] are left as they are.  What a token does not attend does not reach
+ * its results, infinities and NaN neither; for an infinite value that it attends it may get NaN.
+ * What else is said of headkv_paged_attn holds, the workspace's size being
+ * headkv_paged_attn_tokens_plan's, which need not grow with `tokens`.  With 16 / group
+ * (rounded down, at least 1) tokens to a cut, batch * kv_heads * cuts of a row may be 2^24,
+ * and tokens too (HEADKV_ERR_UNSUPPORTED beyond). */
 headkv_status headkv_paged_attn_tokens_plan(const headkv_paged_config* cfg,
                                             const headkv_paged_lists* own,
                                             const headkv_paged_lists* shared, int32_t tokens,

@@ -329,6 +329,29 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // The reference before any score: below all, and finite, so that nothing is NaN.
 constexpr float kLow = -3.402823466e38f;
 
+// All ones in each half of w that is no finite bf16.
+__device__ __forceinline__ u32x4_t odd_of(const u32x4_t& w) {
+    u32x4_t odd;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        odd[e] = ((w[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
+                 ((w[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+    return odd;
+}
+// The largest bits so far of each half, without signs; and whether any lane has one of those.
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const u32x4_t& w) {
+    typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        top = __builtin_bit_cast(
+            uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, top),
+                                                __builtin_bit_cast(u16x2_t, w[e] & 0x7fff7fffu)));
+    return top;
+}
+__device__ __forceinline__ bool any_odd(uint32_t top) {
+    return __builtin_amdgcn_ballot_w64((top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u) != 0;
+}
+
 // State of a wavefront: column i = lane % 16 of each of its NB tiles.
 template <int TYPE, int D, int NB>
 struct Wave {
@@ -500,7 +523,80 @@ struct Wave {
              t.ks, t.vs, partial, [&](int) { return seen; });
     }
 
-    // The same where columns differ in what they attend: the lane's own is [first, end); all
+    // Where columns differ in what they attend, a value that is no finite number must not
+    // reach those that do not attend it, whose weight is 0.  It is taken out of the operand,
+    // and the outputs of the columns that do attend one are NaN from here on: ones in the places
+    // of such values (odd: all ones there) times ones for what the lane's column attends count
+    // them, for output block `block`.
+    __device__ __forceinline__ void spoil(const u32x4_t& odd, uint32_t seen, int block) {
+        constexpr uint32_t kOnes = 0x3f803f80u;
+        const u32x4_t there{odd[0] & kOnes, odd[1] & kOnes, odd[2] & kOnes, odd[3] & kOnes};
+        const u32x4_t mine = Tile<TYPE, D>::blank16(u32x4_t{kOnes, kOnes, kOnes, kOnes}, seen);
+        const f32x4_t count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8_t, there), __builtin_bit_cast(bf16x8_t, mine),
+            f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[0][block][r] = count[r] > 0.f ? NAN : acc[0][block][r];
+    }
+    // The same for a tile, of which the lane's column attends `seen`.  (A look at each value of
+    // the steps that columns differ in, one or two a list: 64 x 32 lists of 64 to 1024 tokens
+    // FP4 32.6 us, with it 33.5, BF16 79.7 and 79.8, INT8 no change; cuts of 128 columns, where
+    // whoever converts a value looks at it, 24 rows of 256 tokens FP4 121.2 and 123.1, BF16
+    // 116.3 and 119.3.)
+    __device__ __forceinline__ void keep_apart(Tile<TYPE, D>& t, uint32_t seen) {
+        using T = Tile<TYPE, D>;
+        if constexpr (TYPE == kInt8) {  // scales, which the lane gives its column's weights
+            t.vs = T::blank16(t.vs, seen);
+        } else if constexpr (TYPE == kBf16) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < T::VN; ++j) top = top_of(top, t.v[j]);
+            if (__builtin_expect(!any_odd(top), 1)) return;
+#pragma unroll
+            for (int j = 0; j < T::VN; ++j) {
+                __builtin_amdgcn_sched_barrier(0);  // (in the registers of one at a time)
+                const u32x4_t odd = odd_of(t.v[j]);
+                spoil(odd, seen, j);
+                t.v[j] &= ~odd;
+            }
+        } else {
+            // exponents from 253 on, of which 4 and 6 are infinite (and all of 255): a lane has
+            // those of its quarter's tokens for dims of the first or the second half of a load's
+            // 16 rows, and its outputs' rows lie in the first or the second half by its quarter
+            auto full = [](uint32_t e) { return ((e & 0x7f7f7f7fu) + 0x03030303u) & e & 0x80808080u; };
+            uint32_t some = 0;
+#pragma unroll
+            for (int j = 0; j < T::VN; ++j) some |= full(t.ve[j][0]) | full(t.ve[j][1]);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(some != 0) == 0, 1)) return;
+            // (worked out here: no register holds it from step to step)
+            const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+#pragma unroll
+            for (int j = 0; j < T::VN; ++j) {
+                uint32_t tokens = 0;  // bit n: the lane's token n
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t m = full(t.ve[j][h]) >> 7;
+                    t.ve[j][h] &= ~(m * 255u);
+                    tokens |= ((m | m >> 7 | m >> 14 | m >> 21) & 15u) << (4 * h);
+                }
+                bool mine = false;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t of_half = (uint32_t)__shfl((int)tokens, (lane & 48) + 8 * half);
+                    const uint64_t hit = __builtin_amdgcn_ballot_w64((of_half & seen) != 0);
+                    const uint32_t columns = (uint32_t)(hit | hit >> 16 | hit >> 32 | hit >> 48);
+                    if (lane >> 5 == half) mine = columns >> (lane & 15) & 1;
+                }
+#pragma unroll
+                for (int x = 0; x < VX; ++x)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[0][VX * j + x][r] = mine ? NAN : acc[0][VX * j + x][r];
+            }
+        }
+    }
+
+    // A step where columns differ in what they attend: the lane's own is [first, end); all
     // of them attend [all_first, all_end), none outside [any_first, any_end).
     struct Seen {
         int first, end, all_first, all_end, any_first, any_end;
@@ -511,6 +607,7 @@ struct Wave {
         if (partial) {
             t.blank(seen_of(at, s.any_first, s.any_end, lane));
             seen = seen_of(at, s.first, s.end, lane);
+            keep_apart(t, seen);
         }
         constexpr int kPer = KS / Tile<TYPE, D>::KN;
         step([&](int u, int s) { return key_operand<TYPE>(t.k[u][s / kPer], t.ke[u], s % kPer); },
@@ -1031,6 +1128,14 @@ void k_attn_with_shared(AttnCall a) {
     else own_block<TYPE, D, true, W, TOK>(a, block - a.shared_blocks, lds, ints.found);
 }
 
+// Which values of a step's operands are no finite numbers: any, of each of the four wavefronts
+// that convert them, and where (of a wavefront that has none nothing is written).
+template <int TYPE, int D>
+struct Odd {
+    __align__(16) uint32_t any[4];
+    u32x4_t of[TYPE == kInt8 ? 1 : D / 16][64];
+};
+
 // What a wavefront of k_attn_shared_wide does of a step's operands: the first four
 // wavefronts convert those of the keys, the others those of the values, D / 64 each
 // (FP4 values: two), which lie together in the page.  One load for all of them, at
@@ -1108,8 +1213,11 @@ struct Share {
 
     // Its operands, into the lane's places of the slots; values that are not seen as
     // zeros (INT8: with scales of zero, which go to slot `at_scales` and the next).
+    // odd, if given: values that are no finite numbers are taken out, all ones in their places
+    // go to odd's slots, and odd->any says whether there are some.
     __device__ __forceinline__ void convert(u32x4_t (*to)[64], int at_scales, bool partial,
-                                            uint32_t seen, int wave, int lane) {
+                                            uint32_t seen, int wave, int lane,
+                                            Odd<TYPE, D>* odd = nullptr) {
         if (values && partial) {
             if constexpr (TYPE == kBf16) {
 #pragma unroll
@@ -1119,6 +1227,7 @@ struct Share {
             if constexpr (TYPE == kFp4) powers = T::blank8(powers, seen);
         }
         if constexpr (TYPE == kBf16) {
+            if (odd && values) take_out<N>(raw, *odd, wave, lane);
 #pragma unroll
             for (int x = 0; x < N; ++x) to[slot + x][lane] = raw[x];
         } else if constexpr (TYPE == kInt8) {
@@ -1133,8 +1242,10 @@ struct Share {
         } else if (values) {
             bf16x8_t o[2];
             fp4_pair(raw[0][0], raw[0][1], powers, o);
-            to[slot][lane] = __builtin_bit_cast(u32x4_t, o[0]);
-            to[slot + 1][lane] = __builtin_bit_cast(u32x4_t, o[1]);
+            u32x4_t w[2]{__builtin_bit_cast(u32x4_t, o[0]), __builtin_bit_cast(u32x4_t, o[1])};
+            if (odd) take_out<2>(w, *odd, wave, lane);
+            to[slot][lane] = w[0];
+            to[slot + 1][lane] = w[1];
         } else {
             const uint64_t all = (uint64_t)whole(powers[1]) << 32 | whole(powers[0]);
             const uint32_t e = (uint32_t)(all >> (8 * more)) & 0xffu;
@@ -1143,6 +1254,22 @@ struct Share {
                 const uint32_t w = N == 2 ? raw[0][x] : (wave & 1) ? raw[0][1] : raw[0][0];
                 to[slot + x][lane] = __builtin_bit_cast(u32x4_t, key_operand<kFp4>(u32x4_t{w, 0, 0, 0}, e, 0));
             }
+        }
+    }
+
+    template <int M>
+    __device__ __forceinline__ void take_out(u32x4_t* w, Odd<TYPE, D>& odd, int wave, int lane) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int x = 0; x < M; ++x) top = top_of(top, w[x]);
+        const bool any = any_odd(top);
+        if (lane == 0) odd.any[wave & 3] = any;
+        if (__builtin_expect(!any, 1)) return;
+#pragma unroll
+        for (int x = 0; x < M; ++x) {
+            const u32x4_t none = odd_of(w[x]);
+            odd.of[slot - 2 * KS + x][lane] = none;
+            w[x] &= ~none;
         }
     }
 };
@@ -1380,7 +1507,7 @@ using CutOperands = u32x4_t[2][2 * (D / 32) + D / 16 + (TYPE == kInt8 ? 2 : 0)][
 
 template <int TYPE, int D>
 __device__ __forceinline__ void cut_block(const AttnCall& a, const CutItem& c, int chunk,
-                                          CutOperands<TYPE, D>& operands) {
+                                          CutOperands<TYPE, D>& operands, Odd<TYPE, D>* odd) {
     using T = Tile<TYPE, D>;
     constexpr int W = kWideWaves, NB = kCutCols / (16 * W);
     constexpr int KS = D / 32, DB = D / 16, VX = DB / T::VN;
@@ -1407,6 +1534,8 @@ __device__ __forceinline__ void cut_block(const AttnCall& a, const CutItem& c, i
     const int low = token_of(w0), high = token_of(w0 + 16 * NB - 1);
     const int any_first = c.first_of(low), any_end = end_of(high);
     const int all_first = c.first_of(high), all_end = end_of(low);
+    // steps that some columns of the cut may attend and others not: those that end past this
+    const int all_see = c.window > 0 ? 0 : end_of(0);
     Wave<TYPE, D, NB> w;
     w.clear();
     int first[NB], end[NB];
@@ -1437,7 +1566,8 @@ __device__ __forceinline__ void cut_block(const AttnCall& a, const CutItem& c, i
             const int tk = begin + held * kStep;
             const bool partial = tk < s.first || tk + kStep > t1;
             const uint32_t seen = partial ? seen_of(tk, s.first, t1, lane) : 0xffu;
-            share.convert(operands[into], kScales, partial, seen, wave, lane);
+            share.convert(operands[into], kScales, partial, seen, wave, lane,
+                          tk + kStep > all_see ? &odd[into] : nullptr);
             fetch();
         };
         auto consume = [&](int buf, int n) {
@@ -1452,6 +1582,22 @@ __device__ __forceinline__ void cut_block(const AttnCall& a, const CutItem& c, i
             if constexpr (TYPE == kInt8) {
                 ks = operands[buf][kScales][lane];
                 vs = operands[buf][kScales + 1][lane];
+            }
+            if constexpr (TYPE == kInt8) {
+                static_assert(NB == 1, "one tile of columns a wavefront");
+                if (partial) vs = T::blank16(vs, seen[0]);
+            } else if (tk + kStep > all_see) {
+                const u32x4_t any = *reinterpret_cast<const u32x4_t*>(odd[buf].any);
+                if (__builtin_expect(__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]), 0)) {
+                    constexpr int kOf = TYPE == kFp4 ? 2 : D / 64;  // operands of a wavefront
+#pragma unroll
+                    for (int j = 0; j < DB; ++j) {
+                        __builtin_amdgcn_sched_barrier(0);  // (in the registers of one at a time)
+                        if (__builtin_amdgcn_readfirstlane(any[j / kOf]))
+                            w.spoil(odd[buf].of[j][lane], seen[0], j);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             w.step([&](int u, int k) {
                        return __builtin_bit_cast(bf16x8_t, operands[buf][u * KS + k][lane]);
@@ -1509,6 +1655,7 @@ __device__ __forceinline__ void cut_block(const AttnCall& a, const CutItem& c, i
 template <int TYPE, int D, bool FEW>
 __global__ __launch_bounds__(kWideThreads) void k_attn_cut_wide(AttnCall a, int* chunk_of_all) {
     __shared__ CutOperands<TYPE, D> operands;
+    __shared__ __align__(16) Odd<TYPE, D> odd[2];
     if constexpr (FEW) {
         __shared__ Plan plan;
         int chunk;
@@ -1521,12 +1668,12 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_cut_wide(AttnCall a, int*
             for (int o = kFewCuts / 2; o > 0; o /= 2)
                 if (plan.ends[t + o - 1] <= item) t += o;
             t = __builtin_amdgcn_readfirstlane(t);
-            cut_block<TYPE, D>(a, plan.item(a, t), item - (t ? plan.ends[t - 1] : 0), operands);
+            cut_block<TYPE, D>(a, plan.item(a, t), item - (t ? plan.ends[t - 1] : 0), operands, odd);
             __syncthreads();  // the operands are written again
         }
     } else {
         const int item = a.list0 + blockIdx.x, cuts = a.own.lists * a.c.heads;
-        cut_block<TYPE, D>(a, CutItem(a, item % cuts), item / cuts, operands);
+        cut_block<TYPE, D>(a, CutItem(a, item % cuts), item / cuts, operands, odd);
     }
 }
 
