@@ -31,7 +31,9 @@ def generate(decoder: Decoder, prompt: torch.Tensor, images: int, steps: int, dr
              ) -> Dict[str, torch.Tensor]:
     """`steps` tokens of `images` images after prompt (int64 [tokens], on the GPU), images
     being row_len tokens wide.  Returns "tokens" and "logprob" [images][steps], "passes", the
-    times that the decoder has run, and "order": the images, the most probable first."""
+    times that the decoder has run, and "order": the images, the most probable first.
+    RuntimeError where the decoder's logits give an image no next token (NaN, +inf, or all
+    -inf)."""
     if prompt.dim() != 1 or len(prompt) < 1 or images < 1 or steps < 1 or drafts < 0 \
             or row_len < 1:
         raise ValueError("prompt must be [tokens], and tokens, images, steps and row_len at least "
@@ -88,9 +90,11 @@ def _generate(decoder, prompt, images, steps, drafts, row_len, kv, temperature, 
     done = torch.zeros(images, dtype=torch.int64, device=device)
     ahead = torch.arange(places, device=device)
     rows = torch.arange(images, device=device)[:, None]
+    stuck = torch.zeros(images, dtype=torch.bool, device=device)  # no next token
 
     def keep(got):
         """Writes what was gained behind what is there; images that are done go nowhere."""
+        stuck.logical_or_((got["count"] == 0) & (done < steps))
         at = (done[:, None] + ahead[:got["tokens"].shape[1]]).clamp(max=width - 1)
         tokens[rows, at] = got["tokens"].clamp(min=0).long()
         logprob[rows, at] = got["logprob"]
@@ -102,9 +106,15 @@ def _generate(decoder, prompt, images, steps, drafts, row_len, kv, temperature, 
                        temperature=temperature))
     passes, advance = 0, None
     while True:
-        # (one look at the host every few steps: a step gains a token at least)
-        if passes % 8 == 0 and int(done.min()) >= steps:
-            break
+        # (one look at the host every few steps, the first before any token is fed: a step
+        # gains a token at least, but for images that have no next one)
+        if passes % 8 == 0:
+            least, *lost = torch.cat((done.min()[None], stuck)).tolist()
+            if any(lost):
+                raise RuntimeError("the decoder's logits give no next token for images "
+                                   f"{[i for i, x in enumerate(lost) if x]}")
+            if least >= steps:
+                break
         tables.extend(places, advance=advance)
         above = done[:, None] - row_len + ahead[:drafts]  # the tokens over those to come
         guess = torch.where(above >= 0, tokens.gather(1, above.clamp(min=0)), 0)
@@ -114,7 +124,7 @@ def _generate(decoder, prompt, images, steps, drafts, row_len, kv, temperature, 
         logits = forward(fed, at, lists, share=share)
         got = verify_drafts(logits, guess.to(torch.int32),
                             torch.rand((images, places), generator=g, device=device),
-                            counts=torch.where(done >= steps, -1, drafts).to(torch.int32),
+                            counts=torch.where((done >= steps) | stuck, -1, drafts).to(torch.int32),
                             temperature=temperature)
         keep(got)
         advance = got["count"]
