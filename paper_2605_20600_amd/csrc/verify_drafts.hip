@@ -65,9 +65,10 @@ struct Powers {
     // each, and whole powers are added to the exponent.  Below 2^-1020 it is that, which no
     // sum with the largest logit's 1 in it sees.
     __device__ __forceinline__ double share(float x, float m, double k) const {
-        constexpr double kLeast = -1020.0 * 32, kMagic = 0x1.8p52, c = 0.69314718055994530942 / 32;
-        const double y = fmax(((double)x - (double)m) * (32 * k), kLeast);
-        const double t = y + kMagic, f = y - (t - kMagic);
+        constexpr double kMagic = 0x1.8p52, c = 0.69314718055994530942 / 32;
+        // (32nds after the product: 32 k may pass what 64 bits hold where k does not)
+        const double y = fmax(((double)x - (double)m) * k, -1020.0);
+        const double t = fma(32.0, y, kMagic), f = fma(32.0, y, kMagic - t);
         const int n = (int)__builtin_bit_cast(uint64_t, t);
         double p = c * c * c * c * c / 120;
         p = fma(p, f, c * c * c * c / 24);
