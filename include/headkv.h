@@ -619,9 +619,11 @@ headkv_status headkv_verify_drafts(const void* logits, const void* draft_logits,
  *   HEADKV_SCALE_BANDS   by m, the turns in original_len positions: omega if m >= high,
  *                        omega / factor if m <= low, between them the mean of the two by
  *                        how far on m is
- * (A row whose squares' sum passes fp32's range has an infinite one.  scale is 1 but for
- * methods that sharpen or flatten the attention with it.)  Angles are
- * computed in 64 bits, for any int32 coordinate; results are rounded to bf16 once. */
+ * (A row whose squares' sum passes fp32's range has an infinite one.  A mean of squares below
+ * 2^-120 is held in part or not at all: with an eps that is not above that, rows of which it is
+ * one may come out infinite or NaN.  scale is 1 but for methods that sharpen or flatten the
+ * attention with it.)  Angles are computed in 64 bits, for any int32 coordinate; results are
+ * rounded to bf16 once. */
 
 #define HEADKV_ROPE_HALF 0
 #define HEADKV_ROPE_PAIRS 1
