@@ -1387,7 +1387,7 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
     }
 }
 
-// Cuts of many columns (the pieces of a prompt): a block takes a cut's, up to 256, and the
+// Cuts of many columns (the pieces of a prompt): a block takes a cut's, up to 128, and the
 // tokens of a chunk of its list, as k_attn_shared_wide does; what a column sees ends with
 // its own token, so a wavefront leaves out the steps that none of its columns sees.
 // Outputs of a list that has one chunk and shares nothing are written here, the others'
@@ -1396,7 +1396,8 @@ __global__ __launch_bounds__(kWideThreads) void k_attn_shared_wide(AttnCall a) {
 // Few lists, whose lengths only the device knows: every block counts the tokens of all,
 // cuts them into chunks of a length that leaves each CU about one, and takes every
 // gridDim-th of these.  (A grid of every chunk that there might be instead, most of them
-// none: the others lie two on a CU beside CUs that have none, 28 us instead of 20.)
+// none: the others lie two on a CU beside CUs that have none, 28 us instead of 20 when both
+// were there; by a trace of the present build 24.5.)
 constexpr int kFewCuts = kWideThreads;
 
 // A cut and what is known of its list.
@@ -1960,19 +1961,19 @@ int launch_paged_attn(const PagedDims& c, const char* pool, const PagedLists& ow
 }
 
 // Cuts in the place of rows.  Of up to 16 columns, for own_block, or up to kCutCols for
-// k_attn_cut_wide, which converts a list's tokens for all of them once but takes some 8 us
+// k_attn_cut_wide, which converts a list's tokens for all of them once but takes some 4 to 8 us
 // more however short the list is.  Times of the first over the second, tokens from memory,
 // the longest list four times the shortest, one call after the other:
 //   columns of a row and head     24    32    48    64    96   128
-//   1024 lists of up to 2048 INT8 1.30  1.31  1.74  1.98  2.11  2.40
-//                            FP4  .93   .92  1.22  1.48  1.62  1.87
-//                            BF16 2.10  2.08  2.93  3.77  4.28  4.97
-//   1024 of up to 256        INT8 1.03  1.03  1.19  1.23  1.34  1.52
-//                            FP4  .84   .84   .99  1.12   .95  1.05
-//                            BF16 1.25  1.29  1.51  1.58  2.04  2.37
-//   32 of up to 2048         INT8                   .82   .83   .95
-//                            FP4                    .69   .70   .72
-//                            BF16                        1.09  1.18
+//   1024 lists of up to 2048 INT8 1.25  1.33  1.70  1.90  1.96  2.25
+//                            FP4  .93   .96  1.28  1.19  1.32  1.49
+//                            BF16 2.11  2.10  2.92  3.47  4.03  4.73
+//   1024 of up to 256        INT8 1.03  1.03  1.18  1.16  1.30  1.45
+//                            FP4  .84   .84  1.00  1.05   .95  1.05
+//                            BF16 1.28  1.28  1.47  1.75  2.06  2.47
+//   32 of up to 2048         INT8 .79   .78   .89   .83   .86   .97
+//                            FP4  .71   .70   .74   .67   .68   .73
+//                            BF16 .90   .91  1.00   .98  1.07  1.20
 // so by the columns and by the work, in tiles of 16 columns and tokens of a list.
 static bool is_wide(const PagedDims& c, int64_t lists, int64_t columns, int64_t reach) {
     const bool fp4 = c.type == kFp4;

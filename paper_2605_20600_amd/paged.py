@@ -234,7 +234,10 @@ class PagedKV:
         """Planned once for the lists' tables, for any length that they can hold (fp32
         parts of every query head, of 256 to 1024 own and up to 2048 shared tokens:
         128 rows of 32 query heads of 128 dims with tables of 131072 tokens 270 MB).
-        tokens: of attn_tokens()."""
+        tokens: of attn_tokens(), whose parts are those of as many query heads for each of up
+        to 16 columns: as many rows of 16 tokens 550 MB, as a part has up to 8192 tokens from
+        4096 lists on, but 127 of them 4.3 GB, of 5 tokens 1.4 GB; with tables of 2^20 tokens
+        eight times that.  Tables no longer than the lists get save it."""
         key = (own.pages.shape, None if shared is None else shared.pages.shape, tokens)
         if key == self._planned:
             return self._ws
